@@ -425,7 +425,7 @@ def _own(s):
         dsla.dsla_cache_extend(cache, batch[0], pools, ws)
         dsla.dsla_qk_rope(s["h_rope"], s["q"], s["k"], s["v"], s["q_out"], None, cache, batch[0], k_pages, v_pages)
         dsla.dsla_attention_paged(cache, batch[0], s["q_out"], k_pages, v_pages, s["o"], s["d"] ** -0.5, s["longest"], tree=s["mask"], workspace=ws)
-        dsla.dsla_cache_accept(cache, batch[0], s["path"], s["accepted"], pools)
+        dsla.dsla_cache_accept(cache, batch[0], s["path"], s["accepted"], pools, ws)
     elif kind == "step":
         dsla.dsla_cache_truncate(cache, s["keep"])
         dsla.dsla_cache_extend(cache, batch[0], pools, ws)
