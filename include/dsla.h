@@ -365,6 +365,154 @@ DSLA_API dsla_status dsla_attention_prefill(int32_t B, int32_t H, int32_t d, int
                                    const void *q, const void *k, const void *v, void *o, void *stream);
 
 /*
+ * A paged key/value cache for the softmax layers of a partly converted model.  The requests of a serving system (Section
+ * 4.5) are of different lengths and come and go; their keys and values lie in pages of `page` tokens of a pool, and what
+ * the conversion of a layer frees (Section 4.3) is pages.  The book-keeping is on the device: no call reads anything back,
+ * so that a step (room for the next tokens, rotation and writing, attention) can be captured into a graph and replayed.
+ *   pool  : [n_pages][H_kv][page][d] of the cache's type; one for the keys and one for the values of every layer that shares
+ *           the table.  Rows of a page past the end of its sequence may hold anything, NaN included
+ *   table : [n_seqs][max_pages], page number of the tokens page * c .. page * (c + 1) - 1 of sequence s; entries past the
+ *           end of a sequence are -1 where the library leaves them
+ *   lens  : [n_seqs], tokens of every sequence
+ *   refs  : [n_pages], how many table entries name each page (forked sequences share pages); 0 = the page is free.  New pages
+ *           are taken in ascending order from the lowest free one, so that the result of a call does not depend on timing
+ * A program may also fill table, lens and refs itself; every call checks the numbers it reads against n_seqs, max_pages and
+ * n_pages before it uses them.  Calls that change the cache go on one stream, or are ordered by the caller.
+ */
+typedef struct {
+    int32_t n_pages;    /* pages of a pool                                                      */
+    int32_t page;       /* tokens of a page: 16, 32, 64 or 128                                  */
+    int32_t H_kv;       /* key/value heads                                                      */
+    int32_t d;          /* head size, 64 or 128                                                 */
+    int32_t dtype;      /* dsla_dtype of the pools                                              */
+    int32_t n_seqs;     /* rows of the table                                                    */
+    int32_t max_pages;  /* columns of the table; max_pages * page <= 2^31 - 1                   */
+    int32_t *table;     /* DEVICE [n_seqs][max_pages]                                           */
+    int32_t *lens;      /* DEVICE [n_seqs]                                                      */
+    int32_t *refs;      /* DEVICE [n_pages]                                                     */
+    int32_t *status;    /* optional DEVICE word or NULL; the calls set bits in it and never clear any:
+                           DSLA_STATUS_CACHE_FULL   an entry was left out for want of pages or of columns of the table
+                           DSLA_STATUS_CACHE_ENTRY  something was left out because what was given for it is not valid        */
+} dsla_cache;
+#define DSLA_STATUS_CACHE_FULL 2
+#define DSLA_STATUS_CACHE_ENTRY 4
+
+/*
+ * The entries of a step: entry b is tokens cu[b] .. cu[b+1] - 1 of the packed token tensors, and these are tokens
+ * start[b], start[b] + 1, ... of the sequence in row row[b] of the cache.  One description goes through all calls of a step;
+ * dsla_cache_extend writes start.  An entry with start[b] < 0 takes part in nothing (its rows of outputs stay as they were),
+ * and one whose offsets or row are out of range is left out and reported (DSLA_STATUS_CACHE_ENTRY).
+ */
+typedef struct {
+    int32_t B;           /* entries, 1 .. n_seqs                                                                   */
+    int32_t max_n;       /* an upper bound of the tokens of an entry (used by dsla_attention_paged only)           */
+    int64_t total;       /* tokens of the packed tensors, <= 2^31 - 1; rows from cu[B] on are not touched          */
+    const int32_t *cu;   /* DEVICE [B + 1], non-decreasing, 0 <= cu[b] <= total; NULL = one token each (total = B) */
+    const int32_t *row;  /* DEVICE [B], distinct; NULL = row b                                                     */
+    int32_t *start;      /* DEVICE [B]                                                                             */
+} dsla_batch;
+
+/* Pools that a call works on: HOST array [n_pools] of DEVICE pointers, 0 <= n_pools <= DSLA_MAX_POOLS, 16-byte aligned. */
+#define DSLA_MAX_POOLS 256
+
+/* Scratch of dsla_cache_extend, dsla_cache_accept (for up to B entries) and dsla_cache_compact, 16-byte aligned; 0 for an invalid
+ * cache.  Calls that may overlap, also replayed ones, need buffers of their own. */
+DSLA_API size_t dsla_cache_workspace_bytes(const dsla_cache *cache, int32_t B);
+
+/* dsla_cache_init - all pages free, all sequences empty: refs = 0, lens = 0, table = -1. */
+DSLA_API dsla_status dsla_cache_init(const dsla_cache *cache, void *stream);
+
+/*
+ * dsla_cache_extend - makes room for the tokens of every entry at the end of its sequence: start[b] = lens[row], lens[row] +=
+ * the tokens of b, and pages for them.  A last page that is not full and that other sequences name too is first replaced by a
+ * page of its own, to which the rows that the sequence has in it are copied in every pool.  Entries are served in order; those
+ * that the free pages do not reach, and all later ones that need pages, stay as they are: start[b] = -1, reported as
+ * DSLA_STATUS_CACHE_FULL.  Of two entries that name one row the first takes part.
+ */
+DSLA_API dsla_status dsla_cache_extend(const dsla_cache *cache, const dsla_batch *batch, int32_t n_pools, void *const *pools,
+                                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * dsla_cache_fork - sequence s becomes a copy of sequence parent[s] that shares all of its pages (DEVICE [n_seqs]; negative:
+ * sequence s stays as it is).  s has to be empty, and its parent no child of the same call; others are left out and reported.
+ */
+DSLA_API dsla_status dsla_cache_fork(const dsla_cache *cache, const int32_t *parent, void *stream);
+
+/*
+ * dsla_cache_truncate - cuts sequence s to its first new_lens[s] tokens (DEVICE [n_seqs]; negative, or not below its length:
+ * it stays as it is; 0 ends it).  Pages that no sequence names any more are free.
+ */
+DSLA_API dsla_status dsla_cache_truncate(const dsla_cache *cache, const int32_t *new_lens, void *stream);
+
+/*
+ * dsla_cache_accept - of the tokens of entry b, which are the last of their sequence, keeps the n_accepted[b] ones at places
+ * path[cu[b]], path[cu[b] + 1], ... (ascending), such as the accepted path of a tree of drafted tokens: their rows move to
+ * start[b], start[b] + 1, ... in every pool, and the sequence is cut behind them.
+ *   path       : DEVICE [total]      n_accepted : DEVICE [B], 0 .. tokens of b; negative: entry b stays as it is
+ * An entry whose path is not ascending or out of range, whose tokens are not the last, or that would change a page which other
+ * sequences name, stays as it is and is reported.
+ */
+DSLA_API dsla_status dsla_cache_accept(const dsla_cache *cache, const dsla_batch *batch, const int32_t *path, const int32_t *n_accepted,
+                                       int32_t n_pools, void *const *pools, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * dsla_cache_compact - moves pages so that the pages in use are the first ones: with L pages in use, the i-th of them from
+ * page L on moves to the i-th free page below L, in every pool, table and refs follow, and *n_live (DEVICE) = L.  The pool's
+ * memory from page L on can then go to something else, such as the states of layers that are converted.
+ */
+DSLA_API dsla_status dsla_cache_compact(const dsla_cache *cache, int32_t *n_live, int32_t n_pools, void *const *pools,
+                                        void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * dsla_qk_rope - what stands between the projections and a softmax layer: every head of q and k normalised by its root mean
+ * square and multiplied by a weight (optional), its first rot_dim features rotated by the token's position, and the keys and
+ * values written into their pages, in one pass:
+ *     y = x / sqrt(mean(x^2) + eps) * w        (y_a, y_b) <- (y_a cos - y_b sin, y_a sin + y_b cos),  angle = position * inv_freq[i]
+ *     pairs i = 0 .. rot_dim/2 - 1: (a, b) = (i, i + rot_dim/2), or (2i, 2i + 1) with interleaved != 0
+ * fp32 arithmetic, angles in fp64; results are rounded once.
+ *   q      : [total][H][d]      k, v : [total][H_kv][d]
+ *   q_out  : [total][H][d], written; may be q      k_out : the same for k, or NULL where only the pages need them
+ *   cache, batch, k_pages, v_pages : where keys and values go (cache->status as above), or all NULL: then every token takes
+ *            part and v may be NULL.  A token's place is start[b] + its number in the entry
+ *   position = start[b] + offsets[m] (start = 0 without a batch), offsets NULL: the number in its entry (without a batch: m)
+ * total_rows: tokens of the tensors; with a batch it is batch->total.
+ */
+typedef struct {
+    int32_t H, H_kv, d;       /* d in {64, 128}                                                                          */
+    int32_t io_dtype;         /* dsla_dtype of q, k, v and the outputs; with a cache also its type                       */
+    int32_t rot_dim;          /* features rotated: a multiple of 16, 0 .. d                                              */
+    int32_t interleaved;      /* which features form pairs                                                               */
+    float eps;                /* > 0 with weights                                                                        */
+    const float *inv_freq;    /* DEVICE [rot_dim / 2], radians per position; NULL where rot_dim = 0                      */
+    const float *q_weight;    /* DEVICE [d], norm of q; NULL = no norm                                                   */
+    const float *k_weight;    /* DEVICE [d], norm of k; NULL = no norm                                                   */
+    const int32_t *offsets;   /* DEVICE [total] or NULL, e.g. the depths of a tree's nodes                               */
+} dsla_rope;
+DSLA_API dsla_status dsla_qk_rope(const dsla_rope *rope, int64_t total_rows, const void *q, const void *k, const void *v,
+                                  void *q_out, void *k_out, const dsla_cache *cache, const dsla_batch *batch,
+                                  void *k_pages, void *v_pages, void *stream);
+
+/*
+ * dsla_attention_paged - softmax attention of the last tokens of every sequence over a paged cache: the decode step of a
+ * layer that has not been converted, and the check of several drafted tokens at once.  Query j of entry b (token cu[b] + j)
+ * sees every token before start[b], and of the entry's own tokens i = 0 .. n - 1, whose keys and values are in their pages,
+ *     tree != NULL : those with bit i of tree[cu[b] + j] set (a tree of drafted tokens: a node's ancestors and itself)
+ *     tree == NULL : i <= j
+ *     o_j = sum_{i seen} softmax_i(scale * q_j . k_i) v_i
+ * A query that sees nothing gets zeros; a token that a query does not see has no part in its result, whatever it holds.
+ *   H       : query heads, a multiple of H_kv; head h reads key/value head h / (H / H_kv)
+ *   max_len : an upper bound of the lengths start[b] + n, used for planning only
+ *   q, o    : [total][H][d] of the cache's type      tree : DEVICE [total] or NULL
+ *   batch->max_n : 1 .. 64; an entry with more tokens is left out and reported
+ * Tokens of a page that the table gives no valid number for are not seen (reported).
+ * io bf16: bf16 operands on MFMA, fp32 accumulation and softmax statistics; io f32: fp32 throughout.
+ */
+DSLA_API size_t dsla_attention_paged_workspace_bytes(const dsla_cache *cache, const dsla_batch *batch, int32_t H, int64_t max_len);
+DSLA_API dsla_status dsla_attention_paged(const dsla_cache *cache, const dsla_batch *batch, int32_t H, int64_t max_len, float scale,
+                                          const void *q, const void *k_pages, const void *v_pages, const uint64_t *tree, void *o,
+                                          void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Host-side conversion logic (paper Section 4.3 "Adaptive Layer-wise Conversion").  Plain host functions, HOST
  * pointers, no device work: they decide which layers of a model run in DSLA form for a request; the calls above
  * then run those layers (the entropy that ranks them comes from dsla_attention_entropy).
@@ -412,7 +560,8 @@ DSLA_API const char *dsla_last_hip_error(void);
  * so the launch path still allocates nothing).
  * Kernel ids: 0 state_init, 1 prefill_segment_state, 2 prefill_segment_scan,
  * 3 prefill_chunk_loop, 4 decode, 5 prefill_segment_list (packed sequences only), 6 attention_entropy,
- * 7 attention_decode (each with its merge kernel), 8 decode_multi, 9 attention_prefill, 10 project.
+ * 7 attention_decode (each with its merge kernel), 8 decode_multi, 9 attention_prefill, 10 project,
+ * 11 cache (every launch of the dsla_cache calls), 12 qk_rope, 13 attention_paged (with its merge kernel).
  */
 #define DSLA_KERNEL_STATE_INIT 0
 #define DSLA_KERNEL_PREFILL_SEGMENT_STATE 1
@@ -425,7 +574,10 @@ DSLA_API const char *dsla_last_hip_error(void);
 #define DSLA_KERNEL_DECODE_MULTI 8
 #define DSLA_KERNEL_ATTENTION_PREFILL 9
 #define DSLA_KERNEL_PROJECT 10
-#define DSLA_KERNEL_COUNT 11
+#define DSLA_KERNEL_CACHE 11
+#define DSLA_KERNEL_QK_ROPE 12
+#define DSLA_KERNEL_ATTENTION_PAGED 13
+#define DSLA_KERNEL_COUNT 14
 
 /* enable != 0: create the event pool (max_records launches can be recorded between two
  * collects) and start recording; enable == 0: stop and destroy the pool. */

@@ -14,3 +14,6 @@ from .binding import (DslaDesc, DslaError, DslaMulti, dsla_decode_multi, dsla_pr
                       dsla_decode, dsla_decode_slots, dsla_prefill, dsla_prefill_static_ws,  # noqa: F401
                       dsla_prefill_varlen, dsla_prefill_varlen_workspace_bytes, dsla_prefill_workspace_bytes,
                       dsla_state_init, library_path, load_library, make_desc, profile_collect, profile_enable)
+from .binding import (DslaBatch, DslaCache, DslaRope, make_batch, make_cache, make_pools, make_rope,  # noqa: F401
+                      dsla_attention_paged, dsla_attention_paged_workspace_bytes, dsla_cache_accept, dsla_cache_compact, dsla_cache_extend,
+                      dsla_cache_fork, dsla_cache_init, dsla_cache_truncate, dsla_cache_workspace_bytes, dsla_qk_rope)

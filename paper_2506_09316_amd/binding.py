@@ -27,12 +27,15 @@ _native = _General   # _marshal once the library is loaded, where it can be used
 
 DSLA_F32, DSLA_BF16 = 0, 1
 KERNEL_NAMES = ("state_init", "prefill_segment_state", "prefill_segment_scan", "prefill_chunk_loop", "decode",
-                "prefill_segment_list", "attention_entropy", "attention_decode", "decode_multi", "attention_prefill", "project")
+                "prefill_segment_list", "attention_entropy", "attention_decode", "decode_multi", "attention_prefill", "project",
+                "cache", "qk_rope", "attention_paged")
 EXPORTS = ("dsla_state_init", "dsla_prefill_workspace_bytes", "dsla_prefill", "dsla_prefill_static_ws", "dsla_decode",
            "dsla_prefill_varlen_workspace_bytes", "dsla_prefill_varlen", "dsla_decode_slots",
            "dsla_decode_multi", "dsla_prefill_multi_workspace_bytes", "dsla_prefill_multi",
            "dsla_attention_entropy_workspace_bytes", "dsla_attention_entropy",
            "dsla_attention_decode_workspace_bytes", "dsla_attention_decode", "dsla_attention_prefill", "dsla_project",
+           "dsla_cache_workspace_bytes", "dsla_cache_init", "dsla_cache_extend", "dsla_cache_fork", "dsla_cache_truncate",
+           "dsla_cache_accept", "dsla_cache_compact", "dsla_qk_rope", "dsla_attention_paged_workspace_bytes", "dsla_attention_paged",
            "dsla_rank_layers", "dsla_max_conversion_rate", "dsla_kv_cache_bytes", "dsla_conversion_plan",
            "dsla_status_string", "dsla_last_hip_error", "dsla_profile_enable", "dsla_profile_collect")
 
@@ -51,6 +54,26 @@ class DslaMulti(ctypes.Structure):
     _fields_ = [("n_states", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("g_alpha", ctypes.POINTER(ctypes.c_void_p)),
                 ("g_beta", ctypes.POINTER(ctypes.c_void_p)), ("S", ctypes.POINTER(ctypes.c_void_p)),
                 ("weights", ctypes.POINTER(ctypes.c_float)), ("weights_per_head", ctypes.c_void_p)]
+
+
+class DslaCache(ctypes.Structure):
+    """Mirror of `dsla_cache` in include/dsla.h."""
+    _fields_ = [("n_pages", ctypes.c_int32), ("page", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("refs", ctypes.c_void_p), ("status", ctypes.c_void_p)]
+
+
+class DslaBatch(ctypes.Structure):
+    """Mirror of `dsla_batch` in include/dsla.h."""
+    _fields_ = [("B", ctypes.c_int32), ("max_n", ctypes.c_int32), ("total", ctypes.c_int64), ("cu", ctypes.c_void_p), ("row", ctypes.c_void_p),
+                ("start", ctypes.c_void_p)]
+
+
+class DslaRope(ctypes.Structure):
+    """Mirror of `dsla_rope` in include/dsla.h."""
+    _fields_ = [("H", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("d", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float), ("inv_freq", ctypes.c_void_p), ("q_weight", ctypes.c_void_p),
+                ("k_weight", ctypes.c_void_p), ("offsets", ctypes.c_void_p)]
 
 
 class DslaError(RuntimeError):
@@ -116,6 +139,28 @@ def load_library():
     lib.dsla_project.restype = ctypes.c_int
     lib.dsla_attention_prefill.argtypes = [ctypes.c_int32] * 3 + [ctypes.c_int64, ctypes.c_int32, ctypes.c_float] + [vp] * 5
     lib.dsla_attention_prefill.restype = ctypes.c_int
+    cp, bp, pools = ctypes.POINTER(DslaCache), ctypes.POINTER(DslaBatch), [ctypes.c_int32, ctypes.POINTER(ctypes.c_void_p)]
+    scratch = [vp, ctypes.c_size_t, vp]
+    lib.dsla_cache_workspace_bytes.argtypes = [cp, ctypes.c_int32]
+    lib.dsla_cache_workspace_bytes.restype = ctypes.c_size_t
+    lib.dsla_cache_init.argtypes = [cp, vp]
+    lib.dsla_cache_init.restype = ctypes.c_int
+    lib.dsla_cache_extend.argtypes = [cp, bp, *pools, *scratch]
+    lib.dsla_cache_extend.restype = ctypes.c_int
+    lib.dsla_cache_fork.argtypes = [cp, vp, vp]
+    lib.dsla_cache_fork.restype = ctypes.c_int
+    lib.dsla_cache_truncate.argtypes = [cp, vp, vp]
+    lib.dsla_cache_truncate.restype = ctypes.c_int
+    lib.dsla_cache_accept.argtypes = [cp, bp, vp, vp, *pools, *scratch]
+    lib.dsla_cache_accept.restype = ctypes.c_int
+    lib.dsla_cache_compact.argtypes = [cp, vp, *pools, *scratch]
+    lib.dsla_cache_compact.restype = ctypes.c_int
+    lib.dsla_qk_rope.argtypes = [ctypes.POINTER(DslaRope), ctypes.c_int64] + [vp] * 5 + [cp, bp] + [vp] * 3
+    lib.dsla_qk_rope.restype = ctypes.c_int
+    lib.dsla_attention_paged_workspace_bytes.argtypes = [cp, bp, ctypes.c_int32, ctypes.c_int64]
+    lib.dsla_attention_paged_workspace_bytes.restype = ctypes.c_size_t
+    lib.dsla_attention_paged.argtypes = [cp, bp, ctypes.c_int32, ctypes.c_int64, ctypes.c_float] + [vp] * 5 + scratch
+    lib.dsla_attention_paged.restype = ctypes.c_int
     lib.dsla_rank_layers.argtypes = [ctypes.c_int32, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_int32)]
     lib.dsla_rank_layers.restype = ctypes.c_int
     lib.dsla_max_conversion_rate.argtypes = [ctypes.c_int64]
@@ -359,6 +404,159 @@ def dsla_attention_prefill(q, k, v, o, scale: float):
     B, T, H, d = q.shape
     _check(lib.dsla_attention_prefill(int(B), int(H), int(d), int(T), _dtype_code(q), float(scale), _ptr(q),
                                                  _ptr(k), _ptr(v), _ptr(o), _stream()))
+
+
+def _here(t, dtype, numel=None, optional=False):
+    """Pointer of a contiguous tensor on the current device, of that type and number of elements."""
+    if t is None:
+        if optional:
+            return None
+        raise ValueError("a required tensor is None")
+    p = _ptr(t)
+    if t.dtype != dtype:
+        raise TypeError(f"{t.dtype} in the place of {dtype}")
+    if numel is not None and t.numel() != numel:
+        raise ValueError(f"{t.numel()} elements in the place of {numel}")
+    if t.get_device() != _torch._cuda_getDevice():
+        raise ValueError(f"a tensor of device {t.get_device()}, and the current one is {_torch._cuda_getDevice()}")
+    return p
+
+
+def _io_dtype(code):
+    import torch
+    return torch.bfloat16 if code == DSLA_BF16 else torch.float32
+
+
+def make_cache(table, lens, refs, *, page, H_kv, d, dtype, status=None) -> DslaCache:
+    """dsla_cache from int32 GPU tensors: table [n_seqs, max_pages], lens [n_seqs], refs [n_pages], status [1] or None.  dtype:
+    DSLA_F32 or DSLA_BF16, the type of the pools.  The structure keeps the tensors alive."""
+    import torch
+    load_library()
+    n_seqs, max_pages = table.shape
+    c = DslaCache(int(refs.numel()), int(page), int(H_kv), int(d), int(dtype), int(n_seqs), int(max_pages), _here(table, torch.int32),
+                  _here(lens, torch.int32, n_seqs), _here(refs, torch.int32), _here(status, torch.int32, 1, optional=True))
+    c._keep = (table, lens, refs, status)
+    return c
+
+
+def make_batch(start, total, *, cu=None, row=None, max_n=1) -> DslaBatch:
+    """dsla_batch from int32 GPU tensors: start [B], cu [B + 1] or None (one token each), row [B] or None.  max_n: an upper bound of the
+    tokens of an entry.  The structure keeps the tensors alive."""
+    import torch
+    load_library()
+    B = start.numel()
+    x = DslaBatch(int(B), int(max_n), int(total), _here(cu, torch.int32, B + 1, optional=True), _here(row, torch.int32, B, optional=True),
+                  _here(start, torch.int32))
+    x._keep = (start, cu, row)
+    return x
+
+
+class Pools:
+    """The pools of a cache as the calls take them; keeps the tensors alive."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        for t in self.tensors:
+            _here(t, t.dtype)
+        self.array = (ctypes.c_void_p * max(1, len(self.tensors)))(*[t.data_ptr() for t in self.tensors])
+
+    def of(self, cache: DslaCache):
+        want, dtype = cache.n_pages * cache.H_kv * cache.page * cache.d, _io_dtype(cache.dtype)
+        for t in self.tensors:
+            if t.numel() != want or t.dtype != dtype:
+                raise ValueError(f"a pool of {t.numel()} elements of {t.dtype}, the cache's have {want} of {dtype}")
+        return len(self.tensors), self.array
+
+
+def make_pools(tensors) -> Pools:
+    """From a list of GPU tensors [n_pages, H_kv, page, d]: keys and values of every layer that shares a cache's table."""
+    load_library()
+    return Pools(tensors)
+
+
+def _scratch(workspace):
+    return (None, 0) if workspace is None else (_here(workspace, workspace.dtype), workspace.numel() * workspace.element_size())
+
+
+def dsla_cache_workspace_bytes(cache: DslaCache, B: int) -> int:
+    return int(load_library().dsla_cache_workspace_bytes(ctypes.byref(cache), int(B)))
+
+
+def dsla_cache_init(cache: DslaCache):
+    """All pages free, all sequences empty (include/dsla.h: dsla_cache_init)."""
+    _check(load_library().dsla_cache_init(ctypes.byref(cache), _stream()))
+
+
+def dsla_cache_extend(cache: DslaCache, batch: DslaBatch, pools: Pools, workspace):
+    """Room for the tokens of every entry at the end of its sequence (include/dsla.h: dsla_cache_extend)."""
+    _check(load_library().dsla_cache_extend(ctypes.byref(cache), ctypes.byref(batch), *pools.of(cache), *_scratch(workspace), _stream()))
+
+
+def dsla_cache_fork(cache: DslaCache, parent):
+    """Sequences that share the pages of others (include/dsla.h: dsla_cache_fork).  parent: int32 GPU tensor [n_seqs]."""
+    import torch
+    _check(load_library().dsla_cache_fork(ctypes.byref(cache), _here(parent, torch.int32, cache.n_seqs), _stream()))
+
+
+def dsla_cache_truncate(cache: DslaCache, new_lens):
+    """Sequences cut to their first tokens, or ended (include/dsla.h: dsla_cache_truncate).  new_lens: int32 GPU tensor [n_seqs]."""
+    import torch
+    _check(load_library().dsla_cache_truncate(ctypes.byref(cache), _here(new_lens, torch.int32, cache.n_seqs), _stream()))
+
+
+def dsla_cache_accept(cache: DslaCache, batch: DslaBatch, path, n_accepted, pools: Pools, workspace):
+    """Keeps the accepted tokens of every entry (include/dsla.h: dsla_cache_accept).  path: int32 GPU tensor [total], n_accepted [B]."""
+    import torch
+    _check(load_library().dsla_cache_accept(ctypes.byref(cache), ctypes.byref(batch), _here(path, torch.int32, batch.total),
+                                            _here(n_accepted, torch.int32, batch.B), *pools.of(cache), *_scratch(workspace), _stream()))
+
+
+def dsla_cache_compact(cache: DslaCache, n_live, pools: Pools, workspace):
+    """Pages in use to the front of the pools (include/dsla.h: dsla_cache_compact).  n_live: int32 GPU tensor [1], written."""
+    import torch
+    _check(load_library().dsla_cache_compact(ctypes.byref(cache), _here(n_live, torch.int32, 1), *pools.of(cache), *_scratch(workspace), _stream()))
+
+
+def make_rope(H, H_kv, d, *, io_dtype, inv_freq=None, interleaved=False, q_weight=None, k_weight=None, eps=1e-6, offsets=None) -> DslaRope:
+    """dsla_rope: inv_freq fp32 GPU tensor [rot_dim / 2] or None (nothing rotated), q_weight and k_weight fp32 [d] or None (no norm), offsets
+    int32 [total] or None.  The structure keeps the tensors alive."""
+    import torch
+    load_library()
+    r = DslaRope(int(H), int(H_kv), int(d), int(io_dtype), 0 if inv_freq is None else 2 * inv_freq.numel(), int(bool(interleaved)), float(eps),
+                 _here(inv_freq, torch.float32, optional=True), _here(q_weight, torch.float32, d, optional=True),
+                 _here(k_weight, torch.float32, d, optional=True), _here(offsets, torch.int32, optional=True))
+    r._keep = (inv_freq, q_weight, k_weight, offsets)
+    return r
+
+
+def dsla_qk_rope(rope: DslaRope, q, k, v, q_out, k_out=None, cache: DslaCache = None, batch: DslaBatch = None, k_pages=None, v_pages=None):
+    """Norm and rotation of q and k, keys and values into their pages (include/dsla.h: dsla_qk_rope).  q, q_out [total, H, d];
+    k, v, k_out [total, H_kv, d]; k_pages, v_pages [n_pages, H_kv, page, d]."""
+    import torch
+    dtype, total = _io_dtype(rope.io_dtype), q.shape[0]
+    nq, nk = total * rope.H * rope.d, total * rope.H_kv * rope.d
+    if rope.offsets and rope._keep[3].numel() != total:
+        raise ValueError(f"{rope._keep[3].numel()} offsets for {total} tokens")
+    pool = None if cache is None else cache.n_pages * cache.H_kv * cache.page * cache.d
+    _check(load_library().dsla_qk_rope(ctypes.byref(rope), int(total), _here(q, dtype, nq), _here(k, dtype, nk), _here(v, dtype, nk, optional=True),
+                                       _here(q_out, dtype, nq), _here(k_out, dtype, nk, optional=True),
+                                       None if cache is None else ctypes.byref(cache), None if batch is None else ctypes.byref(batch),
+                                       _here(k_pages, dtype, pool, optional=True), _here(v_pages, dtype, pool, optional=True), _stream()))
+
+
+def dsla_attention_paged_workspace_bytes(cache: DslaCache, batch: DslaBatch, H: int, max_len: int) -> int:
+    return int(load_library().dsla_attention_paged_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), int(H), int(max_len)))
+
+
+def dsla_attention_paged(cache: DslaCache, batch: DslaBatch, q, k_pages, v_pages, o, scale: float, max_len: int, tree=None, workspace=None):
+    """Attention of the last tokens of every sequence over a paged cache (include/dsla.h: dsla_attention_paged).  q, o [total, H, d];
+    k_pages, v_pages [n_pages, H_kv, page, d]; tree: int64 GPU tensor [total] (its bits) or None."""
+    import torch
+    dtype, pool = _io_dtype(cache.dtype), cache.n_pages * cache.H_kv * cache.page * cache.d
+    H, n = q.shape[1], batch.total * q.shape[1] * cache.d
+    _check(load_library().dsla_attention_paged(ctypes.byref(cache), ctypes.byref(batch), int(H), int(max_len), float(scale), _here(q, dtype, n),
+                                               _here(k_pages, dtype, pool), _here(v_pages, dtype, pool),
+                                               _here(tree, torch.int64, batch.total, optional=True), _here(o, dtype, n), *_scratch(workspace), _stream()))
 
 
 PLAN_REASONS = ("no pressure", "memory relief", "quality limit", "all converted")

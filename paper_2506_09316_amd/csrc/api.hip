@@ -441,6 +441,178 @@ dsla_status dsla_attention_prefill(int32_t B, int32_t H, int32_t d, int64_t T, i
     return hip_status(launch_attn_prefill(B, H, d, T, scale, q, k, v, o, static_cast<hipStream_t>(stream)));
 }
 
+namespace {
+bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+dsla_status check_cache(const dsla_cache *c)
+{
+    if (!c) return DSLA_ERR_NULL;
+    if (c->n_pages <= 0 || c->n_pages > (1 << 30) || c->H_kv <= 0 || c->n_seqs <= 0 || c->max_pages <= 0) return DSLA_ERR_SHAPE;
+    if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return DSLA_ERR_UNSUPPORTED;
+    if (c->d != 64 && c->d != 128) return DSLA_ERR_UNSUPPORTED;
+    if (c->dtype != DSLA_F32 && c->dtype != DSLA_BF16) return DSLA_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(c->max_pages) * c->page > 0x7fffffffLL || c->H_kv > (1 << 16)) return DSLA_ERR_SHAPE;
+    if (!c->table || !c->lens || !c->refs) return DSLA_ERR_NULL;
+    if (!aligned4(c->table) || !aligned4(c->lens) || !aligned4(c->refs) || !aligned4(c->status)) return DSLA_ERR_SHAPE;
+    return DSLA_OK;
+}
+
+dsla_status check_batch(const dsla_cache &c, const dsla_batch *x)
+{
+    if (!x) return DSLA_ERR_NULL;
+    if (x->B <= 0 || x->B > c.n_seqs || x->total < 0 || x->total > 0x7fffffffLL) return DSLA_ERR_SHAPE;
+    if (!x->cu && x->total != x->B) return DSLA_ERR_SHAPE;
+    if (!x->start) return DSLA_ERR_NULL;
+    if (!aligned4(x->cu) || !aligned4(x->row) || !aligned4(x->start)) return DSLA_ERR_SHAPE;
+    return DSLA_OK;
+}
+
+dsla_status check_pools(const dsla_cache &c, int32_t n_pools, void *const *pools, int64_t entries)
+{
+    if (n_pools < 0) return DSLA_ERR_SHAPE;
+    if (n_pools > DSLA_MAX_POOLS) return DSLA_ERR_UNSUPPORTED;
+    if (entries * n_pools * c.H_kv > 0x7fffffffLL) return DSLA_ERR_SHAPE;   // one wavefront each
+    if (n_pools > 0 && !pools) return DSLA_ERR_NULL;
+    for (int i = 0; i < n_pools; ++i) {
+        if (!pools[i]) return DSLA_ERR_NULL;
+        if (!aligned16(pools[i])) return DSLA_ERR_SHAPE;
+        for (int j = 0; j < i; ++j)
+            if (pools[j] == pools[i]) return DSLA_ERR_SHAPE;   // a page would move twice
+    }
+    return DSLA_OK;
+}
+
+dsla_status check_scratch(size_t need, const void *workspace, size_t bytes)
+{
+    if (need == 0) return DSLA_OK;
+    if (!workspace || bytes < need) return DSLA_ERR_WORKSPACE;
+    return aligned16(workspace) ? DSLA_OK : DSLA_ERR_SHAPE;
+}
+}  // namespace
+
+#define DSLA_TRY(call)                                \
+    do {                                              \
+        const dsla_status st_ = (call);               \
+        if (st_ != DSLA_OK) return st_;               \
+    } while (0)
+
+size_t dsla_cache_workspace_bytes(const dsla_cache *cache, int32_t B)
+{
+    if (check_cache(cache) != DSLA_OK || B <= 0 || B > cache->n_seqs) return 0;
+    return cache_workspace_bytes(*cache, B);
+}
+
+dsla_status dsla_cache_init(const dsla_cache *cache, void *stream)
+{
+    DSLA_TRY(check_cache(cache));
+    return hip_status(launch_cache_init(*cache, static_cast<hipStream_t>(stream)));
+}
+
+dsla_status dsla_cache_extend(const dsla_cache *cache, const dsla_batch *batch, int32_t n_pools, void *const *pools, void *workspace,
+                              size_t workspace_bytes, void *stream)
+{
+    DSLA_TRY(check_cache(cache));
+    DSLA_TRY(check_batch(*cache, batch));
+    DSLA_TRY(check_pools(*cache, n_pools, pools, 0));
+    DSLA_TRY(check_scratch(cache_workspace_bytes(*cache, batch->B), workspace, workspace_bytes));
+    return hip_status(launch_cache_extend(*cache, *batch, n_pools, pools, workspace, static_cast<hipStream_t>(stream)));
+}
+
+dsla_status dsla_cache_fork(const dsla_cache *cache, const int32_t *parent, void *stream)
+{
+    DSLA_TRY(check_cache(cache));
+    if (!parent) return DSLA_ERR_NULL;
+    if (!aligned4(parent)) return DSLA_ERR_SHAPE;
+    return hip_status(launch_cache_fork(*cache, parent, static_cast<hipStream_t>(stream)));
+}
+
+dsla_status dsla_cache_truncate(const dsla_cache *cache, const int32_t *new_lens, void *stream)
+{
+    DSLA_TRY(check_cache(cache));
+    if (!new_lens) return DSLA_ERR_NULL;
+    if (!aligned4(new_lens)) return DSLA_ERR_SHAPE;
+    return hip_status(launch_cache_truncate(*cache, new_lens, static_cast<hipStream_t>(stream)));
+}
+
+dsla_status dsla_cache_accept(const dsla_cache *cache, const dsla_batch *batch, const int32_t *path, const int32_t *n_accepted,
+                              int32_t n_pools, void *const *pools, void *workspace, size_t workspace_bytes, void *stream)
+{
+    DSLA_TRY(check_cache(cache));
+    DSLA_TRY(check_batch(*cache, batch));
+    DSLA_TRY(check_pools(*cache, n_pools, pools, batch->B));
+    if (!path || !n_accepted) return DSLA_ERR_NULL;
+    if (!aligned4(path) || !aligned4(n_accepted)) return DSLA_ERR_SHAPE;
+    DSLA_TRY(check_scratch(cache_workspace_bytes(*cache, batch->B), workspace, workspace_bytes));
+    return hip_status(launch_cache_accept(*cache, *batch, path, n_accepted, n_pools, pools, workspace, static_cast<hipStream_t>(stream)));
+}
+
+dsla_status dsla_cache_compact(const dsla_cache *cache, int32_t *n_live, int32_t n_pools, void *const *pools, void *workspace,
+                               size_t workspace_bytes, void *stream)
+{
+    DSLA_TRY(check_cache(cache));
+    DSLA_TRY(check_pools(*cache, n_pools, pools, 0));
+    if (!n_live) return DSLA_ERR_NULL;
+    if (!aligned4(n_live)) return DSLA_ERR_SHAPE;
+    DSLA_TRY(check_scratch(cache_workspace_bytes(*cache, 1), workspace, workspace_bytes));
+    return hip_status(launch_cache_compact(*cache, n_live, n_pools, pools, workspace, static_cast<hipStream_t>(stream)));
+}
+
+dsla_status dsla_qk_rope(const dsla_rope *r, int64_t total_rows, const void *q, const void *k, const void *v, void *q_out, void *k_out,
+                         const dsla_cache *cache, const dsla_batch *batch, void *k_pages, void *v_pages, void *stream)
+{
+    if (!r) return DSLA_ERR_NULL;
+    if (r->H <= 0 || r->H_kv <= 0 || r->H > (1 << 16) || r->H_kv > (1 << 16) || total_rows < 0 || total_rows > 0x7fffffffLL) return DSLA_ERR_SHAPE;
+    if ((r->d != 64 && r->d != 128) || (r->io_dtype != DSLA_F32 && r->io_dtype != DSLA_BF16)) return DSLA_ERR_UNSUPPORTED;
+    if (r->rot_dim < 0 || r->rot_dim > r->d) return DSLA_ERR_SHAPE;
+    if (r->rot_dim % 16 != 0) return DSLA_ERR_UNSUPPORTED;
+    if ((r->q_weight || r->k_weight) && !(r->eps > 0.f && r->eps < 3.0e38f)) return DSLA_ERR_SHAPE;
+    if (r->rot_dim > 0 && !r->inv_freq) return DSLA_ERR_NULL;
+    if (!aligned16(r->inv_freq) || !aligned16(r->q_weight) || !aligned16(r->k_weight) || !aligned4(r->offsets)) return DSLA_ERR_SHAPE;
+    if (cache || batch || k_pages || v_pages) {
+        DSLA_TRY(check_cache(cache));
+        DSLA_TRY(check_batch(*cache, batch));
+        if (!k_pages || !v_pages) return DSLA_ERR_NULL;
+        if (cache->H_kv != r->H_kv || cache->d != r->d || batch->total != total_rows) return DSLA_ERR_SHAPE;
+        if (cache->dtype != r->io_dtype) return DSLA_ERR_UNSUPPORTED;
+        if (!aligned16(k_pages) || !aligned16(v_pages) || k_pages == v_pages) return DSLA_ERR_SHAPE;
+    }
+    if (total_rows == 0) return DSLA_OK;
+    if (!q || !k || !q_out || (cache && !v)) return DSLA_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(k_out)) return DSLA_ERR_SHAPE;
+    return hip_status(launch_qk_rope(*r, total_rows, q, k, v, q_out, k_out, cache, batch, k_pages, v_pages, static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+dsla_status check_attention_paged(const dsla_cache *cache, const dsla_batch *batch, int32_t H, int64_t max_len)
+{
+    DSLA_TRY(check_cache(cache));
+    DSLA_TRY(check_batch(*cache, batch));
+    if (H <= 0 || H % cache->H_kv != 0 || max_len < 0) return DSLA_ERR_SHAPE;
+    if (batch->max_n < 1) return DSLA_ERR_SHAPE;
+    if (batch->max_n > 64) return DSLA_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(batch->B) * H * batch->max_n > 0x7fffffffLL / 1024) return DSLA_ERR_SHAPE;
+    return DSLA_OK;
+}
+}  // namespace
+
+size_t dsla_attention_paged_workspace_bytes(const dsla_cache *cache, const dsla_batch *batch, int32_t H, int64_t max_len)
+{
+    if (check_attention_paged(cache, batch, H, max_len) != DSLA_OK) return 0;
+    return attention_paged_workspace_bytes(*cache, *batch, H, max_len);
+}
+
+dsla_status dsla_attention_paged(const dsla_cache *cache, const dsla_batch *batch, int32_t H, int64_t max_len, float scale, const void *q,
+                                 const void *k_pages, const void *v_pages, const uint64_t *tree, void *o, void *workspace,
+                                 size_t workspace_bytes, void *stream)
+{
+    DSLA_TRY(check_attention_paged(cache, batch, H, max_len));
+    if (batch->total == 0) return DSLA_OK;
+    if (!q || !k_pages || !v_pages || !o) return DSLA_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(o) || (reinterpret_cast<uintptr_t>(tree) & 7u)) return DSLA_ERR_SHAPE;
+    DSLA_TRY(check_scratch(attention_paged_workspace_bytes(*cache, *batch, H, max_len), workspace, workspace_bytes));
+    return hip_status(launch_attention_paged(*cache, *batch, H, max_len, scale, q, k_pages, v_pages, tree, o, workspace, static_cast<hipStream_t>(stream)));
+}
+
 dsla_status dsla_profile_enable(int enable, int max_records)
 {
     std::lock_guard<std::mutex> lk(g_prof.mu);

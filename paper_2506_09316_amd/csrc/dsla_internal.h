@@ -139,4 +139,19 @@ hipError_t launch_attn_prefill(int B, int H, int d, int64_t T, float scale, cons
 hipError_t launch_entropy(int B, int H, int d, int64_t T, int io_dtype, const EntropyPlan &plan, float scale,
                           const void *q_last, const void *k, float *entropy, void *workspace, hipStream_t stream);
 
+// The paged cache (cache.hip), what fills it (qk_rope.hip) and what reads it (attention_paged.hip); arguments checked by api.hip.
+size_t cache_workspace_bytes(const dsla_cache &c, int B);
+hipError_t launch_cache_init(const dsla_cache &c, hipStream_t stream);
+hipError_t launch_cache_extend(const dsla_cache &c, const dsla_batch &x, int n_pools, void *const *pools, void *workspace, hipStream_t stream);
+hipError_t launch_cache_fork(const dsla_cache &c, const int32_t *parent, hipStream_t stream);
+hipError_t launch_cache_truncate(const dsla_cache &c, const int32_t *new_lens, hipStream_t stream);
+hipError_t launch_cache_accept(const dsla_cache &c, const dsla_batch &x, const int32_t *path, const int32_t *n_accepted, int n_pools,
+                               void *const *pools, void *workspace, hipStream_t stream);
+hipError_t launch_cache_compact(const dsla_cache &c, int32_t *n_live, int n_pools, void *const *pools, void *workspace, hipStream_t stream);
+hipError_t launch_qk_rope(const dsla_rope &r, int64_t rows, const void *q, const void *k, const void *v, void *q_out, void *k_out,
+                          const dsla_cache *c, const dsla_batch *x, void *k_pages, void *v_pages, hipStream_t stream);
+size_t attention_paged_workspace_bytes(const dsla_cache &c, const dsla_batch &x, int H, int64_t max_len);
+hipError_t launch_attention_paged(const dsla_cache &c, const dsla_batch &x, int H, int64_t max_len, float scale, const void *q, const void *k_pages,
+                                  const void *v_pages, const uint64_t *tree, void *o, void *workspace, hipStream_t stream);
+
 }  // namespace dsla
