@@ -386,7 +386,7 @@ typedef struct {
     int32_t d;          /* head size, 64 or 128                                                 */
     int32_t dtype;      /* dsla_dtype of the pools                                              */
     int32_t n_seqs;     /* rows of the table                                                    */
-    int32_t max_pages;  /* columns of the table; max_pages * page <= 2^31 - 1                   */
+    int32_t max_pages;  /* columns of the table; max_pages * page <= 2^31 - 256                 */
     int32_t *table;     /* DEVICE [n_seqs][max_pages]                                           */
     int32_t *lens;      /* DEVICE [n_seqs]                                                      */
     int32_t *refs;      /* DEVICE [n_pages]                                                     */
@@ -503,7 +503,8 @@ DSLA_API dsla_status dsla_qk_rope(const dsla_rope *rope, int64_t total_rows, con
  *   H       : query heads, a multiple of H_kv; head h reads key/value head h / (H / H_kv)
  *   max_len : an upper bound of the lengths start[b] + n, used for planning only
  *   q, o    : [total][H][d] of the cache's type      tree : DEVICE [total] or NULL
- *   batch->max_n : 1 .. 64; an entry with more tokens is left out and reported
+ *   batch->max_n : 1 .. 64; an entry with more tokens is left out and reported.  B * H * max_n * max_pages * page is limited to about
+ *             10^12 (else DSLA_ERR_SHAPE)
  * Tokens of a page that the table gives no valid number for are not seen (reported).
  * io bf16: bf16 operands on MFMA, fp32 accumulation and softmax statistics; io f32: fp32 throughout.
  */

@@ -451,7 +451,7 @@ dsla_status check_cache(const dsla_cache *c)
     if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return DSLA_ERR_UNSUPPORTED;
     if (c->d != 64 && c->d != 128) return DSLA_ERR_UNSUPPORTED;
     if (c->dtype != DSLA_F32 && c->dtype != DSLA_BF16) return DSLA_ERR_UNSUPPORTED;
-    if (static_cast<int64_t>(c->max_pages) * c->page > 0x7fffffffLL || c->H_kv > (1 << 16)) return DSLA_ERR_SHAPE;
+    if (static_cast<int64_t>(c->max_pages) * c->page > 0x7fffff00LL || c->H_kv > (1 << 16)) return DSLA_ERR_SHAPE;
     if (!c->table || !c->lens || !c->refs) return DSLA_ERR_NULL;
     if (!aligned4(c->table) || !aligned4(c->lens) || !aligned4(c->refs) || !aligned4(c->status)) return DSLA_ERR_SHAPE;
     return DSLA_OK;
@@ -590,7 +590,7 @@ dsla_status check_attention_paged(const dsla_cache *cache, const dsla_batch *bat
     if (H <= 0 || H % cache->H_kv != 0 || max_len < 0) return DSLA_ERR_SHAPE;
     if (batch->max_n < 1) return DSLA_ERR_SHAPE;
     if (batch->max_n > 64) return DSLA_ERR_UNSUPPORTED;
-    if (static_cast<int64_t>(batch->B) * H * batch->max_n > 0x7fffffffLL / 1024) return DSLA_ERR_SHAPE;
+    if (static_cast<int64_t>(batch->B) * H * batch->max_n > 0x7fffffffLL / 1024 || !attention_paged_fits(*cache, *batch, H)) return DSLA_ERR_SHAPE;
     return DSLA_OK;
 }
 }  // namespace

@@ -1,9 +1,11 @@
 // Softmax attention of the last tokens of every sequence over a paged cache (include/dsla.h: dsla_attention_paged).
 //
 // The query heads of a key/value head and the entry's tokens are the rows of one matrix of queries (row = token * G + head of
-// the group), cut into tiles of 16 NT rows.  A workgroup takes a tile against a part of the sequence's keys; its four wavefronts
-// take blocks of keys in turn, each with a running maximum m, sum z and output tiles of its own, and merge at the end; parts leave
-// records that a second kernel merges.
+// the group), cut into tiles of 16 NT rows.  A tile of an entry's head against all keys of its sequence is a unit of work; units
+// lie one after another on a line of granules of kGranule keys, and every workgroup takes an equal stretch of that line, whatever
+// the lengths are (the host does not know them).  The one or two units that a stretch only has a part of leave a record there, and
+// a second kernel merges the records of a unit.  In a workgroup four wavefronts take blocks of keys in turn, each with a running
+// maximum m, sum z and output tiles of its own, and merge at the end of a unit.
 //
 // Keys and values go from memory to the matrix instructions' operands without passing through LDS.  Transposed score tiles
 // S^T[key][query] = K Q^T take rows of K as they lie; a result tile has the query in the lane's column and four keys in its
@@ -20,6 +22,7 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
@@ -27,14 +30,18 @@ constexpr int kWaves = 4;
 // The reference of a query's exponentials is raised only when a score exceeds it by more than this (log2): weights stay below 2^8.
 constexpr float kSlack = 8.f;
 
+constexpr int kGranule = 128;   // keys
+constexpr int kAhead = 1;       // what beginning and ending a unit costs, in granules
+
 struct PagedArgs {
     CacheArgs c;
     BatchArgs x;
     const void *q, *k, *v;
     const uint64_t *tree;
     void *o;
-    float *parts;          // [B][H_kv][P][max_n G][2 + D]: m, z, sums; where P > 1
-    int H, G, max_n, tiles, P, part_keys, units;
+    float *sums;           // [2 groups][tile_rows][D]: sums of the parts that the workgroups leave
+    float2 *stats;         // [2 groups][tile_rows]: their reference and the sum of their weights
+    int H, G, max_n, tile_rows, groups;
     float scale_log2e;
 };
 
@@ -66,7 +73,7 @@ struct Block<bf16_t, D> {
     __device__ __forceinline__ void load_k(int s, const bf16_t *rows, int lane)
     {
 #pragma unroll
-        for (int c = 0; c < NK; ++c) k[s][c] = *reinterpret_cast<const u32x4 *>(rows + (lane & 15) * D + 8 * (lane >> 4) + 32 * c);
+        for (int c = 0; c < NK; ++c) k[s][c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(rows + (lane & 15) * D + 8 * (lane >> 4) + 32 * c));
     }
     __device__ __forceinline__ void load_v(int s, const bf16_t *rows, int lane)
     {
@@ -74,7 +81,7 @@ struct Block<bf16_t, D> {
         for (int j = 0; j < 4; ++j) {
             const bf16_t *p = rows + (4 * (lane >> 4) + j) * D + (lane & 15) * TF;
             if constexpr (TF == 8) {
-                const u32x4 x = *reinterpret_cast<const u32x4 *>(p);
+                const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
 #pragma unroll
                 for (int w = 0; w < 4; ++w) v[4 * s + j][w] = x[w];
             } else {
@@ -124,13 +131,18 @@ struct Block<bf16_t, D> {
         }
         return r;
     }
-    // The weights are rounded to 16 bits for the second product (they are at most 2^8 and positive: 2^-9 of each, of either sign); their sum
-    // is taken before.
-    static __device__ __forceinline__ void accumulate(const Operand &v, const float (&p)[SLOTS], f32x4 (&acc)[TF])
+    // The weights are rounded to 16 bits for the second product, by at most 2^-8 of each; their sum is that of the rounded ones, so that
+    // what the roundings have in common (weights that are nearly alike) cancels.
+    static __device__ __forceinline__ void accumulate(const Operand &v, const float (&p)[SLOTS], float &z, f32x4 (&acc)[TF])
     {
         bf16x8 b;
 #pragma unroll
         for (int j = 0; j < SLOTS; ++j) b[j] = static_cast<__bf16>(p[j]);
+#pragma unroll
+        for (int j = 0; j < SLOTS; j += 2) {
+            const bf16x2 one = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)}, two = {b[j], b[j + 1]};
+            z = __builtin_amdgcn_fdot2_f32_bf16(two, one, z, false);
+        }
 #pragma unroll
         for (int t = 0; t < TF; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.a[t], b, acc[t], 0, 0, 0);
     }
@@ -197,8 +209,10 @@ struct Block<float, D> {
     }
     typedef Block<float, D> Operand;
     __device__ __forceinline__ const Operand &operand() const { return *this; }
-    static __device__ __forceinline__ void accumulate(const Operand &b, const float (&p)[SLOTS], f32x4 (&acc)[TF])
+    static __device__ __forceinline__ void accumulate(const Operand &b, const float (&p)[SLOTS], float &z, f32x4 (&acc)[TF])
     {
+#pragma unroll
+        for (int j = 0; j < SLOTS; ++j) z += p[j];
 #pragma unroll
         for (int j = 0; j < SLOTS; ++j)
 #pragma unroll
@@ -206,284 +220,378 @@ struct Block<float, D> {
     }
 };
 
-// What the workgroups of an entry need to know about it; live = false: it takes no part.
+// What is needed of an entry; units = 0: it takes no part.  A unit's length on the line is its granules and kAhead more, about what it
+// costs to begin and to end one.
 struct Work {
-    Entry e;
-    int start, L, parts;
-    bool live;
+    int cu, n, row, start, L, tiles, granules, units;
+    __device__ __forceinline__ int unit() const { return granules + kAhead; }
+    __device__ __forceinline__ int size() const { return units * unit(); }   // (fits: the host refuses what could not)
 };
-__device__ __forceinline__ Work read_work(const PagedArgs &a, int b)
+__device__ __forceinline__ Work work_of(const PagedArgs &a, int cu, int n, int row, int start)
 {
-    Work w;
-    w.e = read_entry(a.x, a.c, b);
-    w.start = a.x.start[b];
-    const bool fits = w.e.ok && w.e.n <= a.max_n && static_cast<long long>(w.start) + w.e.n <= row_room(a.c);
-    w.live = fits && w.start >= 0 && w.e.n > 0;
-    w.L = w.live ? w.start + w.e.n : 0;
-    const int parts = static_cast<int>((static_cast<long long>(w.L) + a.part_keys - 1) / a.part_keys);
-    w.parts = parts < a.P ? parts : a.P;   // (the last part takes what is left, also of a sequence that is longer than was announced)
-    if (!fits && (!w.e.ok || w.start >= 0) && threadIdx.x == 0) report(a.c.status, DSLA_STATUS_CACHE_ENTRY);
+    Work w{cu, n, row, start, start + n, (n * a.G + a.tile_rows - 1) / a.tile_rows, 0, 0};
+    w.granules = (w.L + kGranule - 1) / kGranule;
+    w.units = w.tiles * a.c.H_kv;
     return w;
+}
+__device__ __forceinline__ Work read_work(const PagedArgs &a, int b, bool tell)
+{
+    const Entry e = read_entry(a.x, a.c, b);
+    const int start = a.x.start[b];
+    const bool fits = e.ok & (e.n <= a.max_n) & (static_cast<long long>(start) + e.n <= row_room(a.c)), live = fits & (start >= 0);
+    if (tell && !fits && (!e.ok || start >= 0)) report(a.c.status, DSLA_STATUS_CACHE_ENTRY);
+    return work_of(a, e.cu, live ? e.n : 0, e.row, live ? start : 0);
+}
+
+__device__ __forceinline__ int wave_prefix(int x)   // inclusive
+{
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int y = __shfl_up(x, off);
+        x += static_cast<int>(threadIdx.x & 63) >= off ? y : 0;
+    }
+    return x;
+}
+
+// The line as every wavefront finds it for itself: how much there is of it and a workgroup takes, and one entry on it with what lies
+// ahead of it: the one that the stretch of workgroup `group` begins in, or (find >= 0) entry `find`.
+struct Line {
+    int total, per, b, before;
+    Work w;
+};
+__device__ __forceinline__ Line read_line(const PagedArgs &a, int group, int find, bool tell)
+{
+    const int lane = threadIdx.x & 63;
+    Line l;
+    Work w = read_work(a, lane < a.x.B ? lane : 0, tell && lane < a.x.B);
+    int n = lane < a.x.B ? w.size() : 0, sum = wave_prefix(n);
+    l.total = __builtin_amdgcn_readlane(sum, 63);
+    for (int b0 = 64; b0 < a.x.B; b0 += 64) {
+        const Work v = read_work(a, b0 + lane < a.x.B ? b0 + lane : 0, tell && b0 + lane < a.x.B);
+        l.total += __builtin_amdgcn_readlane(wave_prefix(b0 + lane < a.x.B ? v.size() : 0), 63);
+    }
+    l.per = (l.total + a.groups - 1) / a.groups;
+    const long long x = static_cast<long long>(l.per) * group;
+    int ahead = 0;
+    l.b = l.before = 0;
+    for (int b0 = 0;;) {
+        const unsigned long long hit = __ballot(find >= 0 ? b0 + lane == find : (x >= ahead + sum - n) & (x < ahead + sum));
+        if (hit) {
+            const int at = __builtin_ctzll(hit);
+            l.b = b0 + at;
+            l.before = ahead + __builtin_amdgcn_readlane(sum - n, at);
+            l.w = work_of(a, __builtin_amdgcn_readlane(w.cu, at), __builtin_amdgcn_readlane(w.n, at), __builtin_amdgcn_readlane(w.row, at),
+                          __builtin_amdgcn_readlane(w.start, at));
+            return l;
+        }
+        ahead += __builtin_amdgcn_readlane(sum, 63);
+        b0 += 64;
+        if (b0 >= a.x.B) break;
+        w = read_work(a, b0 + lane < a.x.B ? b0 + lane : 0, false);
+        n = b0 + lane < a.x.B ? w.size() : 0;
+        sum = wave_prefix(n);
+    }
+    l.total = 0;   // a stretch past the end
+    l.w = work_of(a, 0, 0, 0, 0);
+    return l;
 }
 
 template <class T, int D, int NT>
 __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void attention_paged_kernel(PagedArgs a)
 {
     using B = Block<T, D>;
-    constexpr int TF = B::TF, SLOTS = B::SLOTS, KEYS = B::KEYS;
+    constexpr int TF = B::TF, SLOTS = B::SLOTS, KEYS = B::KEYS, NS = B::NS;
     __shared__ f32x4 s_acc[kWaves / 2][NT * TF][64];
     __shared__ float s_m[kWaves / 2][NT][64], s_z[kWaves / 2][NT][64];
 
-    // Workgroups go round-robin over the 8 XCDs: the tiles of one part of one sequence's head come 8 apart, so that one L2 serves them
-    const int id = blockIdx.x, unit = id / (8 * a.tiles) * 8 + id % 8, tile = id / 8 % a.tiles;
-    if (unit >= a.units) return;
-    const int part = unit % a.P, kv = unit / a.P % a.c.H_kv, b = unit / a.P / a.c.H_kv;
-    const Work w = read_work(a, b);
-    if (!w.live || part >= w.parts || tile * 16 * NT >= w.e.n * a.G) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
     const int plog = a.c.page_log2, page = 1 << plog;
+    const Line line = read_line(a, blockIdx.x, -1, blockIdx.x == 0 && wave == 0);
+    if (line.total == 0) return;
+    int x0 = line.per * blockIdx.x, before = line.before, b = line.b;   // (no more than the total)
+    const int x1 = line.total - x0 < line.per ? line.total : x0 + line.per;
+    Work w = line.w;
 
-    typename B::Query q[NT];
-    uint64_t mask[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int r = (tile * NT + n) * 16 + i, j = r / a.G;
-        mask[n] = 0;
-        if (j < w.e.n) {
-            mask[n] = a.tree ? a.tree[w.e.cu + j] : ~0ull >> (63 - j);
-            q[n].load(static_cast<const T *>(a.q) + (static_cast<size_t>(w.e.cu + j) * a.H + kv * a.G + r % a.G) * D, lane);
-        } else {
-            q[n].zero();
+    while (x0 < x1) {
+        while (x0 - before >= w.size()) {   // (also over entries that take no part)
+            before += w.size();
+            w = read_work(a, ++b, false);
         }
-    }
+        // the unit at x0, and the granules of it that are the workgroup's
+        const int unit = (x0 - before) / w.unit(), at = x0 - before - unit * w.unit();
+        const int len = w.unit() - at < x1 - x0 ? w.unit() - at : x1 - x0;
+        const int g0 = at < kAhead ? 0 : at - kAhead, take = at + len - kAhead - g0;
+        const int tile = unit % w.tiles, kv = unit / w.tiles;
+        x0 += len;
+        if (take <= 0) continue;
+        __syncthreads();   // (the last unit's merge)
 
-    f32x4 acc[NT][TF];
-    float m[NT], z[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        m[n] = -FLT_MAX;
-        z[n] = 0.f;
-#pragma unroll
-        for (int t = 0; t < TF; ++t) acc[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-
-    const int from = part * a.part_keys, to = part == a.P - 1 || w.L - from < a.part_keys ? w.L : from + a.part_keys;
-    const T *kp = static_cast<const T *>(a.k) + ((static_cast<size_t>(kv) << plog) * D);
-    const T *vp = static_cast<const T *>(a.v) + ((static_cast<size_t>(kv) << plog) * D);
-    const size_t pitch = (static_cast<size_t>(a.c.H_kv) << plog) * D;
-    const int32_t *table = a.c.table + static_cast<size_t>(w.e.row) * a.c.max_pages;
-    const int pages = pages_of(w.L, plog);
-    int window = -64, ids = 0;
-    unsigned long long none = 0;   // pages of the window that the table gives no number for
-
-    for (int t0 = from + wave * KEYS; t0 < to; t0 += kWaves * KEYS) {
-        if (((t0 >> plog) & ~63) != window) {   // the numbers of 64 pages, one in a lane
-            window = (t0 >> plog) & ~63;
-            ids = window + lane < pages ? table[window + lane] : 0;
-            none = __ballot(ids < 0 || ids >= a.c.n_pages);
-            if (none) {
-                if (lane == 0) report(a.c.status, DSLA_STATUS_CACHE_ENTRY);
-                if (none >> lane & 1) ids = 0;
-            }
-        }
-        B x;
-        bool gap = false;
-        const T *rows[B::NS];
-#pragma unroll
-        for (int s = 0; s < B::NS; ++s) {   // (a tile of 16 keys lies in one page; past the end page 0 of the pool is read and nothing is made of it)
-            const int t = t0 + 16 * s, p = (t >> plog) - window;
-            gap |= none >> p & 1;
-            const int number = __builtin_amdgcn_readlane(ids, p);
-            const size_t at = static_cast<size_t>(number) * pitch + static_cast<size_t>(t & (page - 1)) * D;
-            x.load_k(s, kp + at, lane);
-            rows[s] = vp + at;
-        }
-#pragma unroll
-        for (int s = 0; s < B::NS; ++s) x.load_v(s, rows[s], lane);
-
-        const bool edge = t0 + KEYS > w.start || gap;   // (uniform)
-        uint32_t there = ~0u;                           // bit j: the key of slot j exists
-        float p[NT][SLOTS];
-        if (edge) {
-            there = 0;
-#pragma unroll
-            for (int j = 0; j < SLOTS; ++j) {
-                const int t = t0 + 16 * (j / 4) + 4 * g + j % 4;
-                if (t < to && !(none >> (((t0 + 16 * (j / 4)) >> plog) - window) & 1)) there |= 1u << j;
-            }
-        }
+        typename B::Query q[NT];
+        uint64_t mask[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float top = -FLT_MAX;
+            const int r = (tile * NT + n) * 16 + i, j = r / a.G;
+            const bool is = j < w.n;
+            mask[n] = a.tree ? a.tree[w.cu + (is ? j : 0)] : ~0ull >> (63 - (is ? j : 0));
+            q[n].load(static_cast<const T *>(a.q) + (static_cast<size_t>(w.cu + (is ? j : 0)) * a.H + kv * a.G + r % a.G) * D, lane);
+            if (!is) q[n].zero();
+        }
+
+        f32x4 acc[NT][TF];
+        float m[NT], z[NT];
 #pragma unroll
-            for (int s = 0; s < B::NS; ++s) {
-                const f32x4 sc = x.scores(s, q[n]);
+        for (int n = 0; n < NT; ++n) {
+            m[n] = -FLT_MAX;
+            z[n] = 0.f;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) p[n][4 * s + r] = sc[r] * a.scale_log2e;
-            }
-            if (edge) {
-#pragma unroll
-                for (int j = 0; j < SLOTS; ++j) {
-                    const int t = t0 + 16 * (j / 4) + 4 * g + j % 4;
-                    const bool seen = (there >> j & 1) && (t < w.start || (mask[n] >> ((t - w.start) & 63) & 1));
-                    p[n][j] = seen ? p[n][j] : -INFINITY;
+            for (int t = 0; t < TF; ++t) acc[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+
+        const int from = g0 * kGranule, to = w.granules - g0 == take ? w.L : from + take * kGranule;
+        const T *kp = static_cast<const T *>(a.k) + ((static_cast<size_t>(kv) << plog) * D);
+        const T *vp = static_cast<const T *>(a.v) + ((static_cast<size_t>(kv) << plog) * D);
+        const size_t pitch = (static_cast<size_t>(a.c.H_kv) << plog) * D;
+        const int32_t *table = a.c.table + static_cast<size_t>(w.row) * a.c.max_pages;
+        const int pages = pages_of(w.L, plog);
+        int window = -64, ids = 0;
+        unsigned long long none = 0;   // pages of the window that the table gives no number for
+
+        for (int t0 = from + wave * KEYS; t0 < to; t0 += kWaves * KEYS) {
+            if (((t0 >> plog) & ~63) != window) {   // the numbers of 64 pages, one in a lane
+                window = (t0 >> plog) & ~63;
+                ids = window + lane < pages ? table[window + lane] : 0;
+                none = __ballot((ids < 0) | (ids >= a.c.n_pages));
+                if (none) {
+                    if (lane == 0) report(a.c.status, DSLA_STATUS_CACHE_ENTRY);
+                    ids = none >> lane & 1 ? 0 : ids;
                 }
             }
+            B x;
+            int gap = 0;   // bit s: tile s has no page
+            const T *rows[NS];
 #pragma unroll
-            for (int j = 0; j < SLOTS; ++j) top = fmaxf(top, p[n][j]);
-            if (__ballot(top > m[n] + kSlack)) {   // the reference of some query is raised: for all of the tile, and the four lanes of each alike
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), m[n]);
-                const float c0 = exp2f(m[n] - top);
-                m[n] = top;
-                z[n] *= c0;
-#pragma unroll
-                for (int t = 0; t < TF; ++t) acc[n][t] *= c0;
+            for (int s = 0; s < NS; ++s) {   // (a tile of 16 keys lies in one page; past the end page 0 of the pool is read and nothing is made of it)
+                const int t = t0 + 16 * s, p = (t >> plog) - window;
+                gap |= static_cast<int>(none >> p & 1) << s;
+                const size_t off = static_cast<size_t>(__builtin_amdgcn_readlane(ids, p)) * pitch + static_cast<size_t>(t & (page - 1)) * D;
+                x.load_k(s, kp + off, lane);
+                rows[s] = vp + off;
             }
 #pragma unroll
-            for (int j = 0; j < SLOTS; ++j) {
-                p[n][j] = __builtin_amdgcn_exp2f(p[n][j] - m[n]);
-                z[n] += p[n][j];
+            for (int s = 0; s < NS; ++s) x.load_v(s, rows[s], lane);
+
+            // Past start, and where pages are missing: which keys exist and which a query sees, as bits counted from key t0 + 4 g (a lane's
+            // keys are 0 .. 3 and 16 .. 19 from there).
+            const bool edge = (t0 + KEYS > w.start) | (gap != 0);   // (uniform)
+            const int left = to - t0 - 4 * g, past = w.start - t0 - 4 * g;
+            uint32_t there = ~0u;
+            if (edge) {
+                there = left >= 32 ? ~0u : left > 0 ? (1u << left) - 1 : 0u;
+                if (gap & 1) there &= 0xffff0000u;
+                if (gap & 2) there &= 0x0000ffffu;
             }
-        }
-        if (edge) {
-            // What does not exist is zero, and an infinity or NaN among the drafted tokens too: zero times it would reach the queries that do not
-            // see it.  Those that do get their products one by one.
-            bool wild = false;
+            float p[NT][SLOTS];
 #pragma unroll
-            for (int j = 0; j < SLOTS; ++j) {
-                if (!(there >> j & 1)) x.clear_v(j);
-                else if (t0 + 16 * (j / 4) + 4 * g + j % 4 >= w.start) wild |= x.tame_v(j);
+            for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    const f32x4 sc = x.scores(s, q[n]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) p[n][4 * s + r] = sc[r] * a.scale_log2e;
+                }
+                if (edge) {
+                    const uint32_t drafted = past >= 32 ? ~0u : past > 0 ? static_cast<uint32_t>(mask[n]) << past | ((1u << past) - 1) : static_cast<uint32_t>(mask[n] >> (-past & 63));
+                    const uint32_t seen = drafted & there;
+#pragma unroll
+                    for (int j = 0; j < SLOTS; ++j) p[n][j] = seen & 1u << (16 * (j / 4) + j % 4) ? p[n][j] : -INFINITY;
+                }
+                float top = -FLT_MAX;
+#pragma unroll
+                for (int j = 0; j < SLOTS; ++j) top = fmaxf(top, p[n][j]);
+                if (__ballot(top > m[n] + kSlack)) {   // the reference of some query is raised: for all of the tile, and the four lanes of each alike
+                    top = fmaxf(top, __shfl_xor(top, 16));
+                    top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), m[n]);
+                    const float c0 = __builtin_amdgcn_exp2f(m[n] - top);
+                    m[n] = top;
+                    z[n] *= c0;
+#pragma unroll
+                    for (int t = 0; t < TF; ++t) acc[n][t] *= c0;
+                }
+#pragma unroll
+                for (int j = 0; j < SLOTS; ++j) p[n][j] = __builtin_amdgcn_exp2f(p[n][j] - m[n]);
             }
-            if (__ballot(wild)) {
-                float *s_p = reinterpret_cast<float *>(&s_acc[0][0][0]) + wave * (NT * SLOTS * 64);   // (a quarter of what the merge uses, at most)
+            if (edge) {
+                // What does not exist is zero, and where queries see different tokens an infinity or NaN among them too: zero times it would reach
+                // the queries that do not see it.  Those that do get their products one by one.
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int j = 0; j < SLOTS; ++j)
+                    if (!(there & 1u << (16 * (j / 4) + j % 4))) x.clear_v(j);
+                if ((w.n > 1) | (a.tree != nullptr)) {
+                    bool wild = false;
 #pragma unroll
-                    for (int j = 0; j < SLOTS; ++j) s_p[(n * SLOTS + j) * 64 + lane] = p[n][j];
-                __builtin_amdgcn_wave_barrier();
+                    for (int j = 0; j < SLOTS; ++j)
+                        if (16 * (j / 4) + j % 4 >= past) wild |= x.tame_v(j);
+                    if (__builtin_expect(__ballot(wild) != 0, 0)) {
+                        float *s_p = reinterpret_cast<float *>(&s_acc[0][0][0]) + wave * (NT * SLOTS * 64);   // (no more than the merge uses)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int j = 0; j < SLOTS; ++j) s_p[(n * SLOTS + j) * 64 + lane] = p[n][j];
+                        __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-                for (int c = 0; c < KEYS; ++c) {
-                    const int t = t0 + c;
-                    if (t < w.start || t >= to || (none >> ((t >> plog) - window) & 1)) continue;
-                    const T *row = rows[0] + (c & 15) * D;
-                    if constexpr (B::NS > 1) row = c < 16 ? row : rows[1] + (c & 15) * D;
+                        for (int c = 0; c < KEYS; ++c) {
+                            const int t = t0 + c;
+                            if (t < w.start || t >= to || (gap >> (c >> 4) & 1)) continue;
+                            const T *row = (NS > 1 && c >= 16 ? rows[NS - 1] : rows[0]) + (c & 15) * D;
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        const float weight = s_p[(n * SLOTS + (c >> 4) * 4 + (c & 3)) * 64 + ((c & 15) >> 2) * 16 + i];
-                        const bool seen = (mask[n] >> (t - w.start)) & 1;
+                            for (int n = 0; n < NT; ++n) {
+                                const float weight = s_p[(n * SLOTS + (c >> 4) * 4 + (c & 3)) * 64 + ((c & 15) >> 2) * 16 + i];
+                                const bool seen = mask[n] >> (t - w.start) & 1;
 #pragma unroll
-                        for (int e = 0; e < 4 * TF; ++e) {
-                            const float f = to_f32(row[4 * g * TF + e]);
-                            acc[n][e % TF][e / TF] += seen && not_finite(f) ? f * weight : 0.f;
+                                for (int e = 0; e < 4 * TF; ++e) {
+                                    const float f = to_f32(row[4 * g * TF + e]);
+                                    acc[n][e % TF][e / TF] += seen && not_finite(f) ? f * weight : 0.f;
+                                }
+                            }
                         }
                     }
                 }
             }
-        }
-        const auto &v = x.operand();
+            const auto &v = x.operand();
 #pragma unroll
-        for (int n = 0; n < NT; ++n) B::accumulate(v, p[n], acc[n]);
-    }
+            for (int n = 0; n < NT; ++n) B::accumulate(v, p[n], z[n], acc[n]);
+        }
 
-    // the sums of a query's four lanes; then wavefronts 2 and 3 into 0 and 1, and 1 into 0
+        // the sums of a query's four lanes; then wavefronts 2 and 3 into 0 and 1, and 1 into 0
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        z[n] += __shfl_xor(z[n], 16);
-        z[n] += __shfl_xor(z[n], 32);
-    }
+        for (int n = 0; n < NT; ++n) {
+            z[n] += __shfl_xor(z[n], 16);
+            z[n] += __shfl_xor(z[n], 32);
+        }
+#pragma unroll 1
+        for (int half = kWaves / 2; half > 0; half >>= 1) {
+            __syncthreads();
+            if (wave >= half && wave < 2 * half) {
 #pragma unroll
-    for (int half = kWaves / 2; half > 0; half >>= 1) {
-        __syncthreads();
-        if (wave >= half && wave < 2 * half) {
+                for (int n = 0; n < NT; ++n) {
+                    s_m[wave - half][n][lane] = m[n];
+                    s_z[wave - half][n][lane] = z[n];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                s_m[wave - half][n][lane] = m[n];
-                s_z[wave - half][n][lane] = z[n];
+                    for (int t = 0; t < TF; ++t) s_acc[wave - half][n * TF + t][lane] = acc[n][t];
+                }
+            }
+            __syncthreads();
+            if (wave < half) {
 #pragma unroll
-                for (int t = 0; t < TF; ++t) s_acc[wave - half][n * TF + t][lane] = acc[n][t];
+                for (int n = 0; n < NT; ++n) {
+                    const float mo = s_m[wave][n][lane], top = fmaxf(m[n], mo), c0 = __builtin_amdgcn_exp2f(m[n] - top), c1 = __builtin_amdgcn_exp2f(mo - top);
+                    m[n] = top;
+                    z[n] = c0 * z[n] + c1 * s_z[wave][n][lane];
+#pragma unroll
+                    for (int t = 0; t < TF; ++t) acc[n][t] = c0 * acc[n][t] + c1 * s_acc[wave][n * TF + t][lane];
+                }
             }
         }
-        __syncthreads();
-        if (wave < half) {
+        if (wave != 0) continue;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const float mo = s_m[wave][n][lane], top = fmaxf(m[n], mo), c0 = exp2f(m[n] - top), c1 = exp2f(mo - top);
-                m[n] = top;
-                z[n] = c0 * z[n] + c1 * s_z[wave][n][lane];
+        for (int n = 0; n < NT; ++n) {
+            const int r = (tile * NT + n) * 16 + i, j = r / a.G;
+            if (j >= w.n) continue;
+            if (take == w.granules) {
+                T *o = static_cast<T *>(a.o) + (static_cast<size_t>(w.cu + j) * a.H + kv * a.G + r % a.G) * D + 4 * g * TF;
+                const float inv = z[n] == 0.f ? 0.f : 1.f / z[n];   // (a query that sees nothing: zeros)
 #pragma unroll
-                for (int t = 0; t < TF; ++t) acc[n][t] = c0 * acc[n][t] + c1 * s_acc[wave][n * TF + t][lane];
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int t = 0; t < TF; ++t) o[e * TF + t] = from_f32<T>(acc[n][t][e] * inv);
+            } else {
+                // a stretch has no more than one unit that began before it (record 0) and one that goes on after it (record 1)
+                const size_t rec = (2 * static_cast<size_t>(blockIdx.x) + (g0 == 0)) * a.tile_rows + n * 16 + i;
+                if (g == 0) a.stats[rec] = make_float2(m[n], z[n]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int t = 0; t < TF; t += 4)
+                        *reinterpret_cast<f32x4 *>(a.sums + rec * D + (4 * g + e) * TF + t) = f32x4{acc[n][t][e], acc[n][t + 1][e], acc[n][t + 2][e], acc[n][t + 3][e]};
             }
-        }
-    }
-    if (wave != 0) return;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int r = (tile * NT + n) * 16 + i, j = r / a.G;
-        if (j >= w.e.n) continue;
-        if (w.parts == 1) {
-            T *o = static_cast<T *>(a.o) + (static_cast<size_t>(w.e.cu + j) * a.H + kv * a.G + r % a.G) * D + 4 * g * TF;
-            const float inv = z[n] == 0.f ? 0.f : 1.f / z[n];   // (a query that sees nothing: zeros)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int t = 0; t < TF; ++t) o[e * TF + t] = from_f32<T>(acc[n][t][e] * inv);
-        } else {
-            float *rec = a.parts + (static_cast<size_t>(unit) * a.max_n * a.G + r) * (2 + D);
-            if (g == 0) {
-                rec[0] = m[n];
-                rec[1] = z[n];
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int t = 0; t < TF; ++t) rec[2 + (4 * g + e) * TF + t] = acc[n][t][e];
         }
     }
 }
 
-// Merges the records of a row's parts.
-template <class T, int D>
-__global__ __launch_bounds__(D) void attention_paged_merge_kernel(PagedArgs a)
+// Merges the records of the units that lie in several workgroups' stretches.  A workgroup takes rows of one entry's head; D / 4
+// lanes hold a row; with SPLIT all of its groups of lanes share the records of one row.
+template <class T, int D, bool SPLIT>
+__global__ __launch_bounds__(256) void attention_paged_merge_kernel(PagedArgs a)
 {
-    const int rows = a.max_n * a.G, r = blockIdx.x % rows, kv = blockIdx.x / rows % a.c.H_kv, b = blockIdx.x / rows / a.c.H_kv, f = threadIdx.x;
-    const Work w = read_work(a, b);
-    const int j = r / a.G;
-    if (!w.live || w.parts == 1 || j >= w.e.n) return;
-    const float *rec = a.parts + ((static_cast<size_t>(b) * a.c.H_kv + kv) * a.P * rows + r) * (2 + D);
-    const size_t pitch = static_cast<size_t>(rows) * (2 + D);
-    float M = -FLT_MAX, Z = 0.f, A = 0.f;
-    constexpr int U = 8;
-    for (int p0 = 0; p0 < w.parts; p0 += U) {   // eight records are requested before the first is used
-        float m[U], z[U], s[U];
+    constexpr int LPR = D / 4, GROUPS = 256 / LPR, U = 4;
+    __shared__ f32x4 s_part[GROUPS][LPR];
+    __shared__ float2 s_stat[GROUPS];
+    const int group = threadIdx.x / LPR, f = threadIdx.x % LPR;
+    const int kv = blockIdx.x % a.c.H_kv, b = blockIdx.x / a.c.H_kv;
+    const int r = SPLIT ? blockIdx.y : blockIdx.y * GROUPS + group, j = r / a.G, tile = r / a.tile_rows;
+    const Line line = read_line(a, 0, b, false);
+    const Work &w = line.w;
+    if (j >= w.n) return;   // (with SPLIT the whole workgroup, here and below)
+    const int first = line.before + (kv * w.tiles + tile) * w.unit() + kAhead;   // the unit's first granule
+    const int w0 = first / line.per, parts = (first + w.granules - 1) / line.per - w0 + 1;
+    if (parts == 1) return;
+    const size_t rec = 2 * static_cast<size_t>(w0) * a.tile_rows + r % a.tile_rows;   // of part p: record 1 of the first workgroup, record 0 of the others
+    float M = -FLT_MAX, Z = 0.f;
+    f32x4 A = {0.f, 0.f, 0.f, 0.f};
+    constexpr int STEP = SPLIT ? GROUPS : 1;
+    for (int p0 = SPLIT ? group : 0; p0 < parts; p0 += STEP * U) {   // U records are requested before the first is used
+        float2 s[U];
+        f32x4 x[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const float *x = rec + (p0 + u < w.parts ? p0 + u : w.parts - 1) * pitch;
-            m[u] = x[0];
-            z[u] = x[1];
-            s[u] = x[2 + f];
+            const int p = p0 + u * STEP < parts ? p0 + u * STEP : p0;
+            const size_t at = rec + static_cast<size_t>(p == 0 ? 1 : 2 * p) * a.tile_rows;
+            s[u] = a.stats[at];
+            x[u] = *reinterpret_cast<const f32x4 *>(a.sums + at * D + 4 * f);
         }
         float top = M;
 #pragma unroll
-        for (int u = 0; u < U; ++u) top = fmaxf(top, m[u]);
-        const float c0 = exp2f(M - top);
+        for (int u = 0; u < U; ++u) top = fmaxf(top, s[u].x);
+        const float c0 = __builtin_amdgcn_exp2f(M - top);
         Z *= c0;
         A *= c0;
         M = top;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const float c = exp2f(m[u] - M);
-            Z = p0 + u < w.parts ? fmaf(c, z[u], Z) : Z;
-            A = p0 + u < w.parts ? fmaf(c, s[u], A) : A;
+        for (int u = 0; u < U; ++u)
+            if (p0 + u * STEP < parts) {
+                const float c = __builtin_amdgcn_exp2f(s[u].x - M);
+                Z = fmaf(c, s[u].y, Z);
+                A += c * x[u];
+            }
+    }
+    if (SPLIT) {
+        s_part[group][f] = A;
+        if (f == 0) s_stat[group] = make_float2(M, Z);
+        __syncthreads();
+        if (group != 0) return;
+        for (int o = 1; o < GROUPS; ++o) {
+            const float top = fmaxf(M, s_stat[o].x), c0 = __builtin_amdgcn_exp2f(M - top), c1 = __builtin_amdgcn_exp2f(s_stat[o].x - top);
+            Z = c0 * Z + c1 * s_stat[o].y;
+            A = c0 * A + c1 * s_part[o][f];
+            M = top;
         }
     }
-    static_cast<T *>(a.o)[(static_cast<size_t>(w.e.cu + j) * a.H + kv * a.G + r % a.G) * D + f] = from_f32<T>(Z == 0.f ? 0.f : A / Z);
+    const float inv = Z == 0.f ? 0.f : 1.f / Z;
+    T *o = static_cast<T *>(a.o) + (static_cast<size_t>(w.cu + j) * a.H + kv * a.G + r % a.G) * D + 4 * f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = from_f32<T>(A[e] * inv);
 }
 
-// How the work is cut: tiles of 16 NT rows, P parts of part_keys keys.
+// Stretches of the line: one workgroup to a compute unit.  256 / 384 / 512 / 768 / 1024 of them (us, 16 bits, one token each): 64
+// requests of 100 to 8192 tokens, 32 heads on 8 of 128, 88 / 101 / 87 / 87 / 93; one of 131072 89 / 107 / 92 / 91 / 97; 16 of 8192
+// 86 / 104 / 90 / 89 / 94; 64 of 300 to 700 33 / 35 / 32 / 32 / 36; 8 of 500 to 2000 17.2 / 19.1 / 19.2 / 16.9 / 17.0.
+constexpr int kStretches = 256;
+
+// How the work is cut: tiles of 16 NT rows, and how many workgroups share the line.
 struct PagedPlan {
-    int NT, tiles, P, part_keys;
-    size_t ws_bytes;
+    int NT, groups;
+    bool split_merge;
+    size_t records;
 };
 PagedPlan plan_of(const dsla_cache &c, const dsla_batch &x, int H, int64_t max_len)
 {
@@ -491,14 +599,12 @@ PagedPlan plan_of(const dsla_cache &c, const dsla_batch &x, int H, int64_t max_l
     const int G = H / c.H_kv;
     const int64_t rows = static_cast<int64_t>(x.max_n) * G, heads = static_cast<int64_t>(x.B) * c.H_kv;
     p.NT = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    p.tiles = static_cast<int>((rows + 16 * p.NT - 1) / (16 * p.NT));
+    const int64_t units = heads * ((rows + 16 * p.NT - 1) / (16 * p.NT));
     const int64_t room = static_cast<int64_t>(c.max_pages) * c.page, longest = max_len < 1 ? 1 : max_len < room ? max_len : room;
-    int64_t P = (1024 + heads * p.tiles - 1) / (heads * p.tiles);
-    const int64_t most = (longest + 255) / 256;
-    if (P > most) P = most;
-    p.part_keys = static_cast<int>(((longest + P - 1) / P + 127) / 128 * 128);
-    p.P = static_cast<int>((longest + p.part_keys - 1) / p.part_keys);
-    p.ws_bytes = p.P > 1 ? static_cast<size_t>(heads) * p.P * rows * (2 + c.d) * sizeof(float) : 0;
+    const int64_t granules = units * ((longest + kGranule - 1) / kGranule);
+    p.groups = static_cast<int>(granules < kStretches ? granules : kStretches);
+    p.split_merge = p.groups > 8 * units;
+    p.records = 2 * static_cast<size_t>(p.groups) * 16 * p.NT;
     return p;
 }
 
@@ -506,19 +612,30 @@ template <class T, int D>
 hipError_t launch_t(const PagedPlan &p, const PagedArgs &a, hipStream_t stream)
 {
     ProfileScope ps(DSLA_KERNEL_ATTENTION_PAGED, stream);
-    if (p.P == 1) ps.e1_first = ps.e1;   // no merge kernel follows: the first launch closes the record too
     auto kernel = p.NT == 1 ? attention_paged_kernel<T, D, 1> : p.NT == 2 ? attention_paged_kernel<T, D, 2> : attention_paged_kernel<T, D, 4>;
-    const int64_t groups = (static_cast<int64_t>(a.units) + 7) / 8 * 8 * p.tiles;
-    DSLA_LAUNCH_FIRST(ps, kernel, dim3(static_cast<unsigned>(groups)), dim3(64 * kWaves), 0, stream, a);
+    DSLA_LAUNCH_FIRST(ps, kernel, dim3(static_cast<unsigned>(p.groups)), dim3(64 * kWaves), 0, stream, a);
     const hipError_t err = hipGetLastError();
-    if (err != hipSuccess || p.P == 1) return err;
-    DSLA_LAUNCH_LAST(ps, (attention_paged_merge_kernel<T, D>), dim3(static_cast<unsigned>(a.x.B) * a.c.H_kv * a.max_n * a.G), dim3(D), 0, stream, a);
+    if (err != hipSuccess) return err;
+    const unsigned units = static_cast<unsigned>(a.x.B) * a.c.H_kv, rows = static_cast<unsigned>(a.max_n) * a.G;
+    constexpr unsigned kGroups = 256 / (D / 4);
+    if (p.split_merge) DSLA_LAUNCH_LAST(ps, (attention_paged_merge_kernel<T, D, true>), dim3(units, rows), dim3(256), 0, stream, a);
+    else DSLA_LAUNCH_LAST(ps, (attention_paged_merge_kernel<T, D, false>), dim3(units, (rows + kGroups - 1) / kGroups), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t attention_paged_workspace_bytes(const dsla_cache &c, const dsla_batch &x, int H, int64_t max_len) { return plan_of(c, x, H, max_len).ws_bytes; }
+bool attention_paged_fits(const dsla_cache &c, const dsla_batch &x, int H)
+{
+    const int64_t rows = static_cast<int64_t>(x.max_n) * (H / c.H_kv), room = static_cast<int64_t>(c.max_pages) * c.page;
+    const int tile_rows = 16 * plan_of(c, x, H, 1).NT;
+    return static_cast<double>(x.B) * c.H_kv * ((rows + tile_rows - 1) / tile_rows) * static_cast<double>(room / kGranule + 1 + kAhead) < 2.0e9;
+}
+
+size_t attention_paged_workspace_bytes(const dsla_cache &c, const dsla_batch &x, int H, int64_t max_len)
+{
+    return plan_of(c, x, H, max_len).records * (2 + c.d) * sizeof(float);
+}
 
 hipError_t launch_attention_paged(const dsla_cache &c, const dsla_batch &x, int H, int64_t max_len, float scale, const void *q, const void *k_pages,
                                   const void *v_pages, const uint64_t *tree, void *o, void *workspace, hipStream_t stream)
@@ -532,14 +649,13 @@ hipError_t launch_attention_paged(const dsla_cache &c, const dsla_batch &x, int 
     a.v = v_pages;
     a.tree = tree;
     a.o = o;
-    a.parts = static_cast<float *>(workspace);
+    a.sums = static_cast<float *>(workspace);
+    a.stats = reinterpret_cast<float2 *>(a.sums + p.records * c.d);
     a.H = H;
     a.G = H / c.H_kv;
     a.max_n = x.max_n;
-    a.tiles = p.tiles;
-    a.P = p.P;
-    a.part_keys = p.part_keys;
-    a.units = x.B * c.H_kv * p.P;
+    a.tile_rows = 16 * p.NT;
+    a.groups = p.groups;
     a.scale_log2e = scale * 1.44269504088896341f;
     if (c.dtype == DSLA_BF16) return c.d == 128 ? launch_t<bf16_t, 128>(p, a, stream) : launch_t<bf16_t, 64>(p, a, stream);
     return c.d == 128 ? launch_t<float, 128>(p, a, stream) : launch_t<float, 64>(p, a, stream);

@@ -150,6 +150,7 @@ hipError_t launch_cache_accept(const dsla_cache &c, const dsla_batch &x, const i
 hipError_t launch_cache_compact(const dsla_cache &c, int32_t *n_live, int n_pools, void *const *pools, void *workspace, hipStream_t stream);
 hipError_t launch_qk_rope(const dsla_rope &r, int64_t rows, const void *q, const void *k, const void *v, void *q_out, void *k_out,
                           const dsla_cache *c, const dsla_batch *x, void *k_pages, void *v_pages, hipStream_t stream);
+bool attention_paged_fits(const dsla_cache &c, const dsla_batch &x, int H);   // places on the line of all granules are 32-bit numbers
 size_t attention_paged_workspace_bytes(const dsla_cache &c, const dsla_batch &x, int H, int64_t max_len);
 hipError_t launch_attention_paged(const dsla_cache &c, const dsla_batch &x, int H, int64_t max_len, float scale, const void *q, const void *k_pages,
                                   const void *v_pages, const uint64_t *tree, void *o, void *workspace, hipStream_t stream);
