@@ -17,7 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdsla.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
 SOURCES = ["api.hip", "decode.hip", "attention.hip", "attention_prefill.hip", "controller.hip", "project.hip", "prefill_short.hip", "prefill.hip",
-           "cache.hip", "qk_rope.hip", "attention_paged.hip"]
+           "cache.hip", "qk_rope.hip", "attention_paged.hip", "attention_paged_rows.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -1,11 +1,7 @@
 // Softmax attention of the last tokens of every sequence over a paged cache (include/dsla.h: dsla_attention_paged).
 //
-// The query heads of a key/value head and the entry's tokens are the rows of one matrix of queries (row = token * G + head of
-// the group), cut into tiles of 16 NT rows.  A tile of an entry's head against all keys of its sequence is a unit of work; units
-// lie one after another on a line of granules of kGranule keys, and every workgroup takes an equal stretch of that line, whatever
-// the lengths are (the host does not know them).  The one or two units that a stretch only has a part of leave a record there, and
-// a second kernel merges the records of a unit.  In a workgroup four wavefronts take blocks of keys in turn, each with a running
-// maximum m, sum z and output tiles of its own, and merge at the end of a unit.
+// A workgroup takes tiles of 16 NT rows; its four wavefronts take blocks of keys in turn, each with a running maximum m, sum z and
+// output tiles of its own, and merge at the end of a unit (attention_paged.h: how the work is laid out).
 //
 // Keys and values go from memory to the matrix instructions' operands without passing through LDS.  Transposed score tiles
 // S^T[key][query] = K Q^T take rows of K as they lie; a result tile has the query in the lane's column and four keys in its
@@ -13,39 +9,10 @@
 // exponentials are its right operand as they are.  The left one, V^T, has a feature per row: a lane loads D/16 adjacent features of
 // the keys whose weights it holds (whole rows of V, 16 lanes to a row), and row i of tile t is feature i * D/16 + t, so that a lane's own
 // loads hold all that it needs: in 32 bits as they are, in 16 bits after exchanging halves between the registers of two keys.
-#include <cfloat>
-
-#include "paged_common.h"
+#include "attention_paged.h"
 
 namespace dsla {
 namespace {
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-constexpr int kWaves = 4;
-// The reference of a query's exponentials is raised only when a score exceeds it by more than this (log2): weights stay below 2^8.
-constexpr float kSlack = 8.f;
-
-constexpr int kGranule = 128;   // keys
-constexpr int kAhead = 1;       // what beginning and ending a unit costs, in granules
-
-struct PagedArgs {
-    CacheArgs c;
-    BatchArgs x;
-    const void *q, *k, *v;
-    const uint64_t *tree;
-    void *o;
-    float *sums;           // [2 groups][tile_rows][D]: sums of the parts that the workgroups leave
-    float2 *stats;         // [2 groups][tile_rows]: their reference and the sum of their weights
-    int H, G, max_n, tile_rows, groups;
-    float scale_log2e;
-};
-
-__device__ __forceinline__ bool not_finite(float f) { return (__float_as_uint(f) & 0x7f800000u) == 0x7f800000u; }
 
 // A block of keys and values as a wavefront holds it.  Lane = 16 g + i.  KEYS keys in NS tiles of 16; slot j of a lane in the second
 // product is key 16 (j / 4) + 4 g + j % 4, whose weight the score tiles leave in that lane.
@@ -220,82 +187,6 @@ struct Block<float, D> {
     }
 };
 
-// What is needed of an entry; units = 0: it takes no part.  A unit's length on the line is its granules and kAhead more, about what it
-// costs to begin and to end one.
-struct Work {
-    int cu, n, row, start, L, tiles, granules, units;
-    __device__ __forceinline__ int unit() const { return granules + kAhead; }
-    __device__ __forceinline__ int size() const { return units * unit(); }   // (fits: the host refuses what could not)
-};
-__device__ __forceinline__ Work work_of(const PagedArgs &a, int cu, int n, int row, int start)
-{
-    Work w{cu, n, row, start, start + n, (n * a.G + a.tile_rows - 1) / a.tile_rows, 0, 0};
-    w.granules = (w.L + kGranule - 1) / kGranule;
-    w.units = w.tiles * a.c.H_kv;
-    return w;
-}
-__device__ __forceinline__ Work read_work(const PagedArgs &a, int b, bool tell)
-{
-    const Entry e = read_entry(a.x, a.c, b);
-    const int start = a.x.start[b];
-    const bool fits = e.ok & (e.n <= a.max_n) & (static_cast<long long>(start) + e.n <= row_room(a.c)), live = fits & (start >= 0);
-    if (tell && !fits && (!e.ok || start >= 0)) report(a.c.status, DSLA_STATUS_CACHE_ENTRY);
-    return work_of(a, e.cu, live ? e.n : 0, e.row, live ? start : 0);
-}
-
-__device__ __forceinline__ int wave_prefix(int x)   // inclusive
-{
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int y = __shfl_up(x, off);
-        x += static_cast<int>(threadIdx.x & 63) >= off ? y : 0;
-    }
-    return x;
-}
-
-// The line as every wavefront finds it for itself: how much there is of it and a workgroup takes, and one entry on it with what lies
-// ahead of it: the one that the stretch of workgroup `group` begins in, or (find >= 0) entry `find`.
-struct Line {
-    int total, per, b, before;
-    Work w;
-};
-__device__ __forceinline__ Line read_line(const PagedArgs &a, int group, int find, bool tell)
-{
-    const int lane = threadIdx.x & 63;
-    Line l;
-    Work w = read_work(a, lane < a.x.B ? lane : 0, tell && lane < a.x.B);
-    int n = lane < a.x.B ? w.size() : 0, sum = wave_prefix(n);
-    l.total = __builtin_amdgcn_readlane(sum, 63);
-    for (int b0 = 64; b0 < a.x.B; b0 += 64) {
-        const Work v = read_work(a, b0 + lane < a.x.B ? b0 + lane : 0, tell && b0 + lane < a.x.B);
-        l.total += __builtin_amdgcn_readlane(wave_prefix(b0 + lane < a.x.B ? v.size() : 0), 63);
-    }
-    l.per = (l.total + a.groups - 1) / a.groups;
-    const long long x = static_cast<long long>(l.per) * group;
-    int ahead = 0;
-    l.b = l.before = 0;
-    for (int b0 = 0;;) {
-        const unsigned long long hit = __ballot(find >= 0 ? b0 + lane == find : (x >= ahead + sum - n) & (x < ahead + sum));
-        if (hit) {
-            const int at = __builtin_ctzll(hit);
-            l.b = b0 + at;
-            l.before = ahead + __builtin_amdgcn_readlane(sum - n, at);
-            l.w = work_of(a, __builtin_amdgcn_readlane(w.cu, at), __builtin_amdgcn_readlane(w.n, at), __builtin_amdgcn_readlane(w.row, at),
-                          __builtin_amdgcn_readlane(w.start, at));
-            return l;
-        }
-        ahead += __builtin_amdgcn_readlane(sum, 63);
-        b0 += 64;
-        if (b0 >= a.x.B) break;
-        w = read_work(a, b0 + lane < a.x.B ? b0 + lane : 0, false);
-        n = b0 + lane < a.x.B ? w.size() : 0;
-        sum = wave_prefix(n);
-    }
-    l.total = 0;   // a stretch past the end
-    l.w = work_of(a, 0, 0, 0, 0);
-    return l;
-}
-
 template <class T, int D, int NT>
 __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void attention_paged_kernel(PagedArgs a)
 {
@@ -307,6 +198,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void attention_paged_
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
     const int plog = a.c.page_log2, page = 1 << plog;
     const Line line = read_line(a, blockIdx.x, -1, blockIdx.x == 0 && wave == 0);
+    if (threadIdx.x == 0) a.open[blockIdx.x].parts = 0;
     if (line.total == 0) return;
     int x0 = line.per * blockIdx.x, before = line.before, b = line.b;   // (no more than the total)
     const int x1 = line.total - x0 < line.per ? line.total : x0 + line.per;
@@ -320,8 +212,13 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void attention_paged_
         // the unit at x0, and the granules of it that are the workgroup's
         const int unit = (x0 - before) / w.unit(), at = x0 - before - unit * w.unit();
         const int len = w.unit() - at < x1 - x0 ? w.unit() - at : x1 - x0;
-        const int g0 = at < kAhead ? 0 : at - kAhead, take = at + len - kAhead - g0;
+        const int g0 = w.granule(at), take = w.granule(at + len) - g0;
         const int tile = unit % w.tiles, kv = unit / w.tiles;
+        if (threadIdx.x == 0 && g0 == 0 && take < w.granules) {
+            const int first = x0 - at + kAhead * w.weight;   // the place of the unit's first granule (the workgroup's)
+            const int rows = w.n * a.G - tile * a.tile_rows;
+            a.open[blockIdx.x] = OpenUnit{take > 0 ? (first + (w.granules - 1) * w.weight) / line.per - static_cast<int>(blockIdx.x) + 1 : 0, w.cu, kv, tile * a.tile_rows, rows < a.tile_rows ? rows : a.tile_rows, {}};
+        }
         x0 += len;
         if (take <= 0) continue;
         __syncthreads();   // (the last unit's merge)
@@ -518,78 +415,78 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void attention_paged_
     }
 }
 
-// Merges the records of the units that lie in several workgroups' stretches.  A workgroup takes rows of one entry's head; D / 4
-// lanes hold a row; with SPLIT all of its groups of lanes share the records of one row.
+// Merges the records of the units that lie in several stretches: workgroup (x, y) takes rows of the one that stretch x begins and does
+// not end.  D / 4 lanes hold a row, kMergeRows rows are a workgroup's; with SPLIT it has one row, whose records its groups of lanes
+// share.
+constexpr int kMergeRows = 8;
 template <class T, int D, bool SPLIT>
 __global__ __launch_bounds__(256) void attention_paged_merge_kernel(PagedArgs a)
 {
-    constexpr int LPR = D / 4, GROUPS = 256 / LPR, U = 4;
+    constexpr int LPR = D / 4, GROUPS = 256 / LPR, U = 4, STEP = SPLIT ? GROUPS : 1;
     __shared__ f32x4 s_part[GROUPS][LPR];
     __shared__ float2 s_stat[GROUPS];
+    const OpenUnit open = a.open[blockIdx.x];
     const int group = threadIdx.x / LPR, f = threadIdx.x % LPR;
-    const int kv = blockIdx.x % a.c.H_kv, b = blockIdx.x / a.c.H_kv;
-    const int r = SPLIT ? blockIdx.y : blockIdx.y * GROUPS + group, j = r / a.G, tile = r / a.tile_rows;
-    const Line line = read_line(a, 0, b, false);
-    const Work &w = line.w;
-    if (j >= w.n) return;   // (with SPLIT the whole workgroup, here and below)
-    const int first = line.before + (kv * w.tiles + tile) * w.unit() + kAhead;   // the unit's first granule
-    const int w0 = first / line.per, parts = (first + w.granules - 1) / line.per - w0 + 1;
-    if (parts == 1) return;
-    const size_t rec = 2 * static_cast<size_t>(w0) * a.tile_rows + r % a.tile_rows;   // of part p: record 1 of the first workgroup, record 0 of the others
-    float M = -FLT_MAX, Z = 0.f;
-    f32x4 A = {0.f, 0.f, 0.f, 0.f};
-    constexpr int STEP = SPLIT ? GROUPS : 1;
-    for (int p0 = SPLIT ? group : 0; p0 < parts; p0 += STEP * U) {   // U records are requested before the first is used
-        float2 s[U];
-        f32x4 x[U];
+    const int row0 = blockIdx.y * (SPLIT ? 1 : kMergeRows), row1 = row0 + (SPLIT ? 1 : kMergeRows);
+    if (open.parts == 0 || row0 >= open.rows) return;
+    for (int row = row0 + (SPLIT ? 0 : group); row < (row1 < open.rows ? row1 : open.rows); row += SPLIT ? 1 : GROUPS) {
+        const size_t rec = 2 * static_cast<size_t>(blockIdx.x) * a.tile_rows + row;   // of part p: record 1 of the first workgroup, record 0 of the others
+        float M = -FLT_MAX, Z = 0.f;
+        f32x4 A = {0.f, 0.f, 0.f, 0.f};
+        for (int p0 = SPLIT ? group : 0; p0 < open.parts; p0 += STEP * U) {   // U records are requested before the first is used
+            float2 s[U];
+            f32x4 x[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int p = p0 + u * STEP < parts ? p0 + u * STEP : p0;
-            const size_t at = rec + static_cast<size_t>(p == 0 ? 1 : 2 * p) * a.tile_rows;
-            s[u] = a.stats[at];
-            x[u] = *reinterpret_cast<const f32x4 *>(a.sums + at * D + 4 * f);
-        }
-        float top = M;
-#pragma unroll
-        for (int u = 0; u < U; ++u) top = fmaxf(top, s[u].x);
-        const float c0 = __builtin_amdgcn_exp2f(M - top);
-        Z *= c0;
-        A *= c0;
-        M = top;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (p0 + u * STEP < parts) {
-                const float c = __builtin_amdgcn_exp2f(s[u].x - M);
-                Z = fmaf(c, s[u].y, Z);
-                A += c * x[u];
+            for (int u = 0; u < U; ++u) {
+                const int p = p0 + u * STEP < open.parts ? p0 + u * STEP : p0;
+                const size_t at = rec + static_cast<size_t>(p == 0 ? 1 : 2 * p) * a.tile_rows;
+                s[u] = a.stats[at];
+                x[u] = *reinterpret_cast<const f32x4 *>(a.sums + at * D + 4 * f);
             }
-    }
-    if (SPLIT) {
-        s_part[group][f] = A;
-        if (f == 0) s_stat[group] = make_float2(M, Z);
-        __syncthreads();
-        if (group != 0) return;
-        for (int o = 1; o < GROUPS; ++o) {
-            const float top = fmaxf(M, s_stat[o].x), c0 = __builtin_amdgcn_exp2f(M - top), c1 = __builtin_amdgcn_exp2f(s_stat[o].x - top);
-            Z = c0 * Z + c1 * s_stat[o].y;
-            A = c0 * A + c1 * s_part[o][f];
-            M = top;
-        }
-    }
-    const float inv = Z == 0.f ? 0.f : 1.f / Z;
-    T *o = static_cast<T *>(a.o) + (static_cast<size_t>(w.cu + j) * a.H + kv * a.G + r % a.G) * D + 4 * f;
+            float top = M;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = from_f32<T>(A[e] * inv);
+            for (int u = 0; u < U; ++u) top = fmaxf(top, s[u].x);
+            const float c0 = __builtin_amdgcn_exp2f(M - top);
+            Z *= c0;
+            A *= c0;
+            M = top;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (p0 + u * STEP < open.parts) {
+                    const float c = __builtin_amdgcn_exp2f(s[u].x - M);
+                    Z = fmaf(c, s[u].y, Z);
+                    A += c * x[u];
+                }
+        }
+        if (SPLIT) {
+            s_part[group][f] = A;
+            if (f == 0) s_stat[group] = make_float2(M, Z);
+            __syncthreads();
+            if (group != 0) return;
+            for (int o = 1; o < GROUPS; ++o) {
+                const float top = fmaxf(M, s_stat[o].x), c0 = __builtin_amdgcn_exp2f(M - top), c1 = __builtin_amdgcn_exp2f(s_stat[o].x - top);
+                Z = c0 * Z + c1 * s_stat[o].y;
+                A = c0 * A + c1 * s_part[o][f];
+                M = top;
+            }
+        }
+        const float inv = Z == 0.f ? 0.f : 1.f / Z;
+        const int r = open.row + row;
+        T *o = static_cast<T *>(a.o) + (static_cast<size_t>(open.cu + r / a.G) * a.H + open.kv * a.G + r % a.G) * D + 4 * f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = from_f32<T>(A[e] * inv);
+    }
 }
 
 // Stretches of the line: one workgroup to a compute unit.  256 / 384 / 512 / 768 / 1024 of them (us, 16 bits, one token each): 64
 // requests of 100 to 8192 tokens, 32 heads on 8 of 128, 88 / 101 / 87 / 87 / 93; one of 131072 89 / 107 / 92 / 91 / 97; 16 of 8192
 // 86 / 104 / 90 / 89 / 94; 64 of 300 to 700 33 / 35 / 32 / 32 / 36; 8 of 500 to 2000 17.2 / 19.1 / 19.2 / 16.9 / 17.0.
-constexpr int kStretches = 256;
+// (The kernel for many rows: two workgroups to a unit.)
+constexpr int kStretches = 256, kRowsStretches = 512;
 
 // How the work is cut: tiles of 16 NT rows, and how many workgroups share the line.
 struct PagedPlan {
-    int NT, groups;
+    int NT, tile_rows, groups;   // NT = 0: attention_paged_rows.hip
     bool split_merge;
     size_t records;
 };
@@ -598,13 +495,15 @@ PagedPlan plan_of(const dsla_cache &c, const dsla_batch &x, int H, int64_t max_l
     PagedPlan p;
     const int G = H / c.H_kv;
     const int64_t rows = static_cast<int64_t>(x.max_n) * G, heads = static_cast<int64_t>(x.B) * c.H_kv;
-    p.NT = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    const int64_t units = heads * ((rows + 16 * p.NT - 1) / (16 * p.NT));
+    p.NT = rows <= 16 ? 1 : rows <= 32 ? 2 : c.dtype == DSLA_BF16 ? 0 : 4;
+    p.tile_rows = p.NT ? 16 * p.NT : kRowsTile;
+    const int64_t units = heads * ((rows + p.tile_rows - 1) / p.tile_rows);
     const int64_t room = static_cast<int64_t>(c.max_pages) * c.page, longest = max_len < 1 ? 1 : max_len < room ? max_len : room;
     const int64_t granules = units * ((longest + kGranule - 1) / kGranule);
-    p.groups = static_cast<int>(granules < kStretches ? granules : kStretches);
+    const int stretches = p.NT ? kStretches : kRowsStretches;
+    p.groups = static_cast<int>(granules < stretches ? granules : stretches);
     p.split_merge = p.groups > 8 * units;
-    p.records = 2 * static_cast<size_t>(p.groups) * 16 * p.NT;
+    p.records = 2 * static_cast<size_t>(p.groups) * p.tile_rows;
     return p;
 }
 
@@ -612,14 +511,20 @@ template <class T, int D>
 hipError_t launch_t(const PagedPlan &p, const PagedArgs &a, hipStream_t stream)
 {
     ProfileScope ps(DSLA_KERNEL_ATTENTION_PAGED, stream);
-    auto kernel = p.NT == 1 ? attention_paged_kernel<T, D, 1> : p.NT == 2 ? attention_paged_kernel<T, D, 2> : attention_paged_kernel<T, D, 4>;
-    DSLA_LAUNCH_FIRST(ps, kernel, dim3(static_cast<unsigned>(p.groups)), dim3(64 * kWaves), 0, stream, a);
-    const hipError_t err = hipGetLastError();
+    hipError_t err = hipSuccess;
+    if constexpr (sizeof(T) == 2)
+        if (p.NT == 0) err = launch_attention_paged_rows(a, ps, stream);
+    if (p.NT) {
+        auto kernel = p.NT == 1 ? attention_paged_kernel<T, D, 1> : attention_paged_kernel<T, D, 2>;
+        if constexpr (sizeof(T) == 4)
+            if (p.NT == 4) kernel = attention_paged_kernel<T, D, 4>;
+        DSLA_LAUNCH_FIRST(ps, kernel, dim3(static_cast<unsigned>(p.groups)), dim3(64 * kWaves), 0, stream, a);
+        err = hipGetLastError();
+    }
     if (err != hipSuccess) return err;
-    const unsigned units = static_cast<unsigned>(a.x.B) * a.c.H_kv, rows = static_cast<unsigned>(a.max_n) * a.G;
-    constexpr unsigned kGroups = 256 / (D / 4);
-    if (p.split_merge) DSLA_LAUNCH_LAST(ps, (attention_paged_merge_kernel<T, D, true>), dim3(units, rows), dim3(256), 0, stream, a);
-    else DSLA_LAUNCH_LAST(ps, (attention_paged_merge_kernel<T, D, false>), dim3(units, (rows + kGroups - 1) / kGroups), dim3(256), 0, stream, a);
+    const unsigned rows = a.max_n * a.G < a.tile_rows ? a.max_n * a.G : a.tile_rows;
+    if (p.split_merge) DSLA_LAUNCH_LAST(ps, (attention_paged_merge_kernel<T, D, true>), dim3(p.groups, rows), dim3(256), 0, stream, a);
+    else DSLA_LAUNCH_LAST(ps, (attention_paged_merge_kernel<T, D, false>), dim3(p.groups, (rows + kMergeRows - 1) / kMergeRows), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -628,13 +533,14 @@ hipError_t launch_t(const PagedPlan &p, const PagedArgs &a, hipStream_t stream)
 bool attention_paged_fits(const dsla_cache &c, const dsla_batch &x, int H)
 {
     const int64_t rows = static_cast<int64_t>(x.max_n) * (H / c.H_kv), room = static_cast<int64_t>(c.max_pages) * c.page;
-    const int tile_rows = 16 * plan_of(c, x, H, 1).NT;
-    return static_cast<double>(x.B) * c.H_kv * ((rows + tile_rows - 1) / tile_rows) * static_cast<double>(room / kGranule + 1 + kAhead) < 2.0e9;
+    const int tile_rows = plan_of(c, x, H, 1).tile_rows;
+    return static_cast<double>(x.B) * c.H_kv * ((rows + tile_rows - 1) / tile_rows) * static_cast<double>(room / kGranule + 1 + kAhead) < 1.0e9;
 }
 
 size_t attention_paged_workspace_bytes(const dsla_cache &c, const dsla_batch &x, int H, int64_t max_len)
 {
-    return plan_of(c, x, H, max_len).records * (2 + c.d) * sizeof(float);
+    const PagedPlan p = plan_of(c, x, H, max_len);
+    return p.records * (2 + c.d) * sizeof(float) + p.groups * sizeof(OpenUnit);
 }
 
 hipError_t launch_attention_paged(const dsla_cache &c, const dsla_batch &x, int H, int64_t max_len, float scale, const void *q, const void *k_pages,
@@ -651,10 +557,11 @@ hipError_t launch_attention_paged(const dsla_cache &c, const dsla_batch &x, int 
     a.o = o;
     a.sums = static_cast<float *>(workspace);
     a.stats = reinterpret_cast<float2 *>(a.sums + p.records * c.d);
+    a.open = reinterpret_cast<OpenUnit *>(a.stats + p.records);
     a.H = H;
     a.G = H / c.H_kv;
     a.max_n = x.max_n;
-    a.tile_rows = 16 * p.NT;
+    a.tile_rows = p.tile_rows;
     a.groups = p.groups;
     a.scale_log2e = scale * 1.44269504088896341f;
     if (c.dtype == DSLA_BF16) return c.d == 128 ? launch_t<bf16_t, 128>(p, a, stream) : launch_t<bf16_t, 64>(p, a, stream);
