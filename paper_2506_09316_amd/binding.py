@@ -21,6 +21,7 @@ _torch = None   # torch._C once the library is loaded
 class _General:
     """In the place of _marshal: leaves every call to the general way."""
     decode = decode_slots = prefill = prefill_varlen = attention_decode = attention_prefill = project = staticmethod(lambda *a: None)
+    cache_extend = cache_fork = cache_truncate = cache_accept = cache_compact = qk_rope = attention_paged = decode
 
 
 _native = _General   # _marshal once the library is loaded, where it can be used
@@ -200,8 +201,9 @@ def _load_native(lib):
                       RuntimeWarning, stacklevel=3)
         return _General
     entries = (lib.dsla_decode, lib.dsla_decode_slots, lib.dsla_prefill, lib.dsla_prefill_varlen, lib.dsla_attention_decode,
-               lib.dsla_attention_prefill, lib.dsla_project)
-    _marshal.bind(*torch_calls, torch.nn.Parameter, DslaDesc, *[ctypes.cast(f, ctypes.c_void_p).value for f in entries])
+               lib.dsla_attention_prefill, lib.dsla_project, lib.dsla_cache_extend, lib.dsla_cache_fork, lib.dsla_cache_truncate, lib.dsla_cache_accept,
+               lib.dsla_cache_compact, lib.dsla_qk_rope, lib.dsla_attention_paged)
+    _marshal.bind(*torch_calls, torch.nn.Parameter, DslaDesc, DslaCache, DslaBatch, DslaRope, *[ctypes.cast(f, ctypes.c_void_p).value for f in entries])
     return _marshal
 
 
@@ -459,12 +461,13 @@ class Pools:
         for t in self.tensors:
             _here(t, t.dtype)
         self.array = (ctypes.c_void_p * max(1, len(self.tensors)))(*[t.data_ptr() for t in self.tensors])
+        self.address, self.sizes = ctypes.addressof(self.array), {(t.numel(), t.dtype) for t in self.tensors}
 
     def of(self, cache: DslaCache):
-        want, dtype = cache.n_pages * cache.H_kv * cache.page * cache.d, _io_dtype(cache.dtype)
-        for t in self.tensors:
-            if t.numel() != want or t.dtype != dtype:
-                raise ValueError(f"a pool of {t.numel()} elements of {t.dtype}, the cache's have {want} of {dtype}")
+        """Number and array, for a cache that they are pools of."""
+        want = {(cache.n_pages * cache.H_kv * cache.page * cache.d, _io_dtype(cache.dtype))}
+        if not self.sizes <= want:
+            raise ValueError(f"pools of {self.sizes}, the cache's are of {want}")
         return len(self.tensors), self.array
 
 
@@ -489,32 +492,52 @@ def dsla_cache_init(cache: DslaCache):
 
 def dsla_cache_extend(cache: DslaCache, batch: DslaBatch, pools: Pools, workspace):
     """Room for the tokens of every entry at the end of its sequence (include/dsla.h: dsla_cache_extend)."""
-    _check(load_library().dsla_cache_extend(ctypes.byref(cache), ctypes.byref(batch), *pools.of(cache), *_scratch(workspace), _stream()))
+    lib, (n, array) = _lib or load_library(), pools.of(cache)
+    status = _native.cache_extend(cache, batch, n, pools.address, workspace)
+    if status is not None:
+        return _check(status)
+    _check(lib.dsla_cache_extend(ctypes.byref(cache), ctypes.byref(batch), n, array, *_scratch(workspace), _stream()))
 
 
 def dsla_cache_fork(cache: DslaCache, parent):
     """Sequences that share the pages of others (include/dsla.h: dsla_cache_fork).  parent: int32 GPU tensor [n_seqs]."""
+    lib = _lib or load_library()
+    status = _native.cache_fork(cache, parent)
+    if status is not None:
+        return _check(status)
     import torch
-    _check(load_library().dsla_cache_fork(ctypes.byref(cache), _here(parent, torch.int32, cache.n_seqs), _stream()))
+    _check(lib.dsla_cache_fork(ctypes.byref(cache), _here(parent, torch.int32, cache.n_seqs), _stream()))
 
 
 def dsla_cache_truncate(cache: DslaCache, new_lens):
     """Sequences cut to their first tokens, or ended (include/dsla.h: dsla_cache_truncate).  new_lens: int32 GPU tensor [n_seqs]."""
+    lib = _lib or load_library()
+    status = _native.cache_truncate(cache, new_lens)
+    if status is not None:
+        return _check(status)
     import torch
-    _check(load_library().dsla_cache_truncate(ctypes.byref(cache), _here(new_lens, torch.int32, cache.n_seqs), _stream()))
+    _check(lib.dsla_cache_truncate(ctypes.byref(cache), _here(new_lens, torch.int32, cache.n_seqs), _stream()))
 
 
 def dsla_cache_accept(cache: DslaCache, batch: DslaBatch, path, n_accepted, pools: Pools, workspace):
     """Keeps the accepted tokens of every entry (include/dsla.h: dsla_cache_accept).  path: int32 GPU tensor [total], n_accepted [B]."""
+    lib, (n, array) = _lib or load_library(), pools.of(cache)
+    status = _native.cache_accept(cache, batch, path, n_accepted, n, pools.address, workspace)
+    if status is not None:
+        return _check(status)
     import torch
-    _check(load_library().dsla_cache_accept(ctypes.byref(cache), ctypes.byref(batch), _here(path, torch.int32, batch.total),
-                                            _here(n_accepted, torch.int32, batch.B), *pools.of(cache), *_scratch(workspace), _stream()))
+    _check(lib.dsla_cache_accept(ctypes.byref(cache), ctypes.byref(batch), _here(path, torch.int32, batch.total), _here(n_accepted, torch.int32, batch.B),
+                                 n, array, *_scratch(workspace), _stream()))
 
 
 def dsla_cache_compact(cache: DslaCache, n_live, pools: Pools, workspace):
     """Pages in use to the front of the pools (include/dsla.h: dsla_cache_compact).  n_live: int32 GPU tensor [1], written."""
+    lib, (n, array) = _lib or load_library(), pools.of(cache)
+    status = _native.cache_compact(cache, n_live, n, pools.address, workspace)
+    if status is not None:
+        return _check(status)
     import torch
-    _check(load_library().dsla_cache_compact(ctypes.byref(cache), _here(n_live, torch.int32, 1), *pools.of(cache), *_scratch(workspace), _stream()))
+    _check(lib.dsla_cache_compact(ctypes.byref(cache), _here(n_live, torch.int32, 1), n, array, *_scratch(workspace), _stream()))
 
 
 def make_rope(H, H_kv, d, *, io_dtype, inv_freq=None, interleaved=False, q_weight=None, k_weight=None, eps=1e-6, offsets=None) -> DslaRope:
@@ -532,16 +555,18 @@ def make_rope(H, H_kv, d, *, io_dtype, inv_freq=None, interleaved=False, q_weigh
 def dsla_qk_rope(rope: DslaRope, q, k, v, q_out, k_out=None, cache: DslaCache = None, batch: DslaBatch = None, k_pages=None, v_pages=None):
     """Norm and rotation of q and k, keys and values into their pages (include/dsla.h: dsla_qk_rope).  q, q_out [total, H, d];
     k, v, k_out [total, H_kv, d]; k_pages, v_pages [n_pages, H_kv, page, d]."""
-    import torch
-    dtype, total = _io_dtype(rope.io_dtype), q.shape[0]
-    nq, nk = total * rope.H * rope.d, total * rope.H_kv * rope.d
+    lib, total = _lib or load_library(), q.shape[0]
     if rope.offsets and rope._keep[3].numel() != total:
         raise ValueError(f"{rope._keep[3].numel()} offsets for {total} tokens")
+    status = _native.qk_rope(rope, total, q, k, v, q_out, k_out, cache, batch, k_pages, v_pages)
+    if status is not None:
+        return _check(status)
+    dtype, nq, nk = _io_dtype(rope.io_dtype), total * rope.H * rope.d, total * rope.H_kv * rope.d
     pool = None if cache is None else cache.n_pages * cache.H_kv * cache.page * cache.d
-    _check(load_library().dsla_qk_rope(ctypes.byref(rope), int(total), _here(q, dtype, nq), _here(k, dtype, nk), _here(v, dtype, nk, optional=True),
-                                       _here(q_out, dtype, nq), _here(k_out, dtype, nk, optional=True),
-                                       None if cache is None else ctypes.byref(cache), None if batch is None else ctypes.byref(batch),
-                                       _here(k_pages, dtype, pool, optional=True), _here(v_pages, dtype, pool, optional=True), _stream()))
+    _check(lib.dsla_qk_rope(ctypes.byref(rope), int(total), _here(q, dtype, nq), _here(k, dtype, nk), _here(v, dtype, nk, optional=True),
+                            _here(q_out, dtype, nq), _here(k_out, dtype, nk, optional=True),
+                            None if cache is None else ctypes.byref(cache), None if batch is None else ctypes.byref(batch),
+                            _here(k_pages, dtype, pool, optional=True), _here(v_pages, dtype, pool, optional=True), _stream()))
 
 
 def dsla_attention_paged_workspace_bytes(cache: DslaCache, batch: DslaBatch, H: int, max_len: int) -> int:
@@ -551,10 +576,14 @@ def dsla_attention_paged_workspace_bytes(cache: DslaCache, batch: DslaBatch, H: 
 def dsla_attention_paged(cache: DslaCache, batch: DslaBatch, q, k_pages, v_pages, o, scale: float, max_len: int, tree=None, workspace=None):
     """Attention of the last tokens of every sequence over a paged cache (include/dsla.h: dsla_attention_paged).  q, o [total, H, d];
     k_pages, v_pages [n_pages, H_kv, page, d]; tree: int64 GPU tensor [total] (its bits) or None."""
+    lib = _lib or load_library()
+    status = _native.attention_paged(cache, batch, q, k_pages, v_pages, o, scale, max_len, tree, workspace)
+    if status is not None:
+        return _check(status)
     import torch
     dtype, pool = _io_dtype(cache.dtype), cache.n_pages * cache.H_kv * cache.page * cache.d
     H, n = q.shape[1], batch.total * q.shape[1] * cache.d
-    _check(load_library().dsla_attention_paged(ctypes.byref(cache), ctypes.byref(batch), int(H), int(max_len), float(scale), _here(q, dtype, n),
+    _check(lib.dsla_attention_paged(ctypes.byref(cache), ctypes.byref(batch), int(H), int(max_len), float(scale), _here(q, dtype, n),
                                                _here(k_pages, dtype, pool), _here(v_pages, dtype, pool),
                                                _here(tree, torch.int64, batch.total, optional=True), _here(o, dtype, n), *_scratch(workspace), _stream()))
 

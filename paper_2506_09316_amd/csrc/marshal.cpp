@@ -14,7 +14,8 @@
 
 namespace {
 
-PyObject *g_device, *g_raw_stream, *g_parameter, *g_desc;   // torch._C._cuda_getDevice, _cuda_getCurrentRawStream; torch.nn.Parameter, binding.DslaDesc
+// torch._C._cuda_getDevice, _cuda_getCurrentRawStream; torch.nn.Parameter, binding.DslaDesc, DslaCache, DslaBatch, DslaRope
+PyObject *g_device, *g_raw_stream, *g_parameter, *g_desc, *g_cache, *g_batch, *g_rope;
 struct Entries {
     decltype(&dsla_decode) decode;
     decltype(&dsla_decode_slots) decode_slots;
@@ -23,6 +24,13 @@ struct Entries {
     decltype(&dsla_attention_decode) attention_decode;
     decltype(&dsla_attention_prefill) attention_prefill;
     decltype(&dsla_project) project;
+    decltype(&dsla_cache_extend) cache_extend;
+    decltype(&dsla_cache_fork) cache_fork;
+    decltype(&dsla_cache_truncate) cache_truncate;
+    decltype(&dsla_cache_accept) cache_accept;
+    decltype(&dsla_cache_compact) cache_compact;
+    decltype(&dsla_qk_rope) qk_rope;
+    decltype(&dsla_attention_paged) attention_paged;
 } g_entry;
 
 // A tensor whose memory can be handed over; other subclasses answer for themselves in Python.
@@ -56,12 +64,14 @@ struct Args {
         *bytes = static_cast<size_t>(t->numel()) * t->element_size();
         return t->data_ptr();
     }
-    dsla_desc desc(int i)   // (a copy: the caller's structure may change while the call runs without the interpreter's lock)
+    // a structure of binding.py  (a copy: the caller's may change while the call runs without the interpreter's lock)
+    template <class S>
+    S structure(int i, PyObject *type)
     {
-        dsla_desc d;
+        S d;
         std::memset(&d, 0, sizeof(d));
         Py_buffer view;
-        if (reinterpret_cast<PyObject *>(Py_TYPE(o[i])) != g_desc) {   // (bytes of that size have a buffer too)
+        if (reinterpret_cast<PyObject *>(Py_TYPE(o[i])) != type) {   // (bytes of that size have a buffer too)
             ok = false;
             return d;
         }
@@ -73,6 +83,25 @@ struct Args {
         else ok = false;
         PyBuffer_Release(&view);
         return d;
+    }
+    dsla_desc desc(int i) { return structure<dsla_desc>(i, g_desc); }
+    // a tensor on the current device, of that type and number of elements (n < 0: any)
+    void *here(int i, at::ScalarType type, int64_t n, bool optional = false)
+    {
+        if (optional && o[i] == Py_None) return nullptr;
+        const at::Tensor *t = gpu_tensor(o[i]);
+        if (!t || t->scalar_type() != type || (n >= 0 && t->numel() != n) || t->get_device() != device()) {
+            ok = false;
+            return nullptr;
+        }
+        return t->data_ptr();
+    }
+    int32_t *ints(int i, int64_t n) { return static_cast<int32_t *>(here(i, at::kInt, n)); }
+    void *scratch(int i, size_t *bytes)
+    {
+        void *p = buffer(i, bytes);
+        if (p && gpu_tensor(o[i])->get_device() != device()) ok = false;
+        return p;
     }
     int64_t integer(int i)
     {
@@ -89,10 +118,21 @@ struct Args {
         if (!PyFloat_CheckExact(o[i])) ok = false;
         return ok ? static_cast<float>(PyFloat_AS_DOUBLE(o[i])) : 0.f;
     }
+    int64_t current = -1;   // torch's current device, once asked for
+    int64_t device()
+    {
+        if (current < 0) {
+            PyObject *d = PyObject_CallNoArgs(g_device);
+            current = d ? PyLong_AsLongLong(d) : -1;
+            Py_XDECREF(d);
+            if (PyErr_Occurred()) ok = false;
+        }
+        return current;
+    }
     void *stream()
     {
         if (!ok) return nullptr;
-        PyObject *device = PyObject_CallNoArgs(g_device), *s = device ? PyObject_CallOneArg(g_raw_stream, device) : nullptr;
+        PyObject *device = current >= 0 ? PyLong_FromLongLong(current) : PyObject_CallNoArgs(g_device), *s = device ? PyObject_CallOneArg(g_raw_stream, device) : nullptr;
         Py_XDECREF(device);
         void *p = s ? PyLong_AsVoidPtr(s) : nullptr;
         Py_XDECREF(s);
@@ -264,11 +304,139 @@ PyObject *project(PyObject *, PyObject *const *args, Py_ssize_t n)   // x, W, ou
     });
 }
 
-// device, raw_stream, parameter type, descriptor type, addresses of the entry points in the order of Entries
+at::ScalarType type_of(int32_t dtype) { return dtype == DSLA_BF16 ? at::kBFloat16 : at::kFloat; }
+int64_t pool_size(const dsla_cache &c) { return static_cast<int64_t>(c.n_pages) * c.H_kv * c.page * c.d; }
+// the array of a binding.Pools: its length and address
+void *const *pools(Args &a, int i, int32_t *n)
+{
+    *n = static_cast<int32_t>(a.integer(i));
+    return reinterpret_cast<void *const *>(a.integer(i + 1));
+}
+
+PyObject *cache_extend(PyObject *, PyObject *const *args, Py_ssize_t n)   // cache, batch, n_pools, pools, workspace
+{
+    return guarded(args, n, 5, [](Args &a) -> int {
+        const dsla_cache c = a.structure<dsla_cache>(0, g_cache);
+        const dsla_batch x = a.structure<dsla_batch>(1, g_batch);
+        int32_t np;
+        void *const *p = pools(a, 2, &np);
+        size_t bytes;
+        void *ws = a.scratch(4, &bytes), *s = a.stream();
+        int status = 0;
+        CALL(status, a, g_entry.cache_extend(&c, &x, np, p, ws, bytes, s));
+        return status;
+    });
+}
+
+PyObject *cache_fork(PyObject *, PyObject *const *args, Py_ssize_t n)   // cache, parent
+{
+    return guarded(args, n, 2, [](Args &a) -> int {
+        const dsla_cache c = a.structure<dsla_cache>(0, g_cache);
+        const int32_t *parent = a.ints(1, c.n_seqs);
+        void *s = a.stream();
+        int status = 0;
+        CALL(status, a, g_entry.cache_fork(&c, parent, s));
+        return status;
+    });
+}
+
+PyObject *cache_truncate(PyObject *, PyObject *const *args, Py_ssize_t n)   // cache, new_lens
+{
+    return guarded(args, n, 2, [](Args &a) -> int {
+        const dsla_cache c = a.structure<dsla_cache>(0, g_cache);
+        const int32_t *lens = a.ints(1, c.n_seqs);
+        void *s = a.stream();
+        int status = 0;
+        CALL(status, a, g_entry.cache_truncate(&c, lens, s));
+        return status;
+    });
+}
+
+PyObject *cache_accept(PyObject *, PyObject *const *args, Py_ssize_t n)   // cache, batch, path, n_accepted, n_pools, pools, workspace
+{
+    return guarded(args, n, 7, [](Args &a) -> int {
+        const dsla_cache c = a.structure<dsla_cache>(0, g_cache);
+        const dsla_batch x = a.structure<dsla_batch>(1, g_batch);
+        const int32_t *path = a.ints(2, x.total), *accepted = a.ints(3, x.B);
+        int32_t np;
+        void *const *p = pools(a, 4, &np);
+        size_t bytes;
+        void *ws = a.scratch(6, &bytes), *s = a.stream();
+        int status = 0;
+        CALL(status, a, g_entry.cache_accept(&c, &x, path, accepted, np, p, ws, bytes, s));
+        return status;
+    });
+}
+
+PyObject *cache_compact(PyObject *, PyObject *const *args, Py_ssize_t n)   // cache, n_live, n_pools, pools, workspace
+{
+    return guarded(args, n, 5, [](Args &a) -> int {
+        const dsla_cache c = a.structure<dsla_cache>(0, g_cache);
+        int32_t *live = a.ints(1, 1), np;
+        void *const *p = pools(a, 2, &np);
+        size_t bytes;
+        void *ws = a.scratch(4, &bytes), *s = a.stream();
+        int status = 0;
+        CALL(status, a, g_entry.cache_compact(&c, live, np, p, ws, bytes, s));
+        return status;
+    });
+}
+
+PyObject *qk_rope(PyObject *, PyObject *const *args, Py_ssize_t n)   // rope, total, q, k, v, q_out, k_out, cache, batch, k_pages, v_pages
+{
+    return guarded(args, n, 11, [](Args &a) -> int {
+        const dsla_rope r = a.structure<dsla_rope>(0, g_rope);
+        const int64_t total = a.integer(1), nq = total * r.H * r.d, nk = total * r.H_kv * r.d;
+        const at::ScalarType type = type_of(r.io_dtype);
+        void *q = a.here(2, type, nq), *k = a.here(3, type, nk), *v = a.here(4, type, nk, true), *q_out = a.here(5, type, nq), *k_out = a.here(6, type, nk, true);
+        const bool cached = a.o[7] != Py_None && a.o[8] != Py_None;
+        if (!cached && (a.o[7] != Py_None || a.o[8] != Py_None || a.o[9] != Py_None || a.o[10] != Py_None)) a.ok = false;
+        dsla_cache c;
+        dsla_batch x;
+        void *kp = nullptr, *vp = nullptr;
+        if (cached) {
+            c = a.structure<dsla_cache>(7, g_cache);
+            x = a.structure<dsla_batch>(8, g_batch);
+            kp = a.here(9, type, pool_size(c));
+            vp = a.here(10, type, pool_size(c));
+        }
+        void *s = a.stream();
+        int status = 0;
+        CALL(status, a, g_entry.qk_rope(&r, total, q, k, v, q_out, k_out, cached ? &c : nullptr, cached ? &x : nullptr, kp, vp, s));
+        return status;
+    });
+}
+
+PyObject *attention_paged(PyObject *, PyObject *const *args, Py_ssize_t n)   // cache, batch, q, k_pages, v_pages, o, scale, max_len, tree, workspace
+{
+    return guarded(args, n, 10, [](Args &a) -> int {
+        const dsla_cache c = a.structure<dsla_cache>(0, g_cache);
+        const dsla_batch x = a.structure<dsla_batch>(1, g_batch);
+        const at::Tensor *t = gpu_tensor(a.o[2]);
+        if (!t || t->dim() != 3 || t->size(1) > 0x7fffffff) {
+            a.ok = false;
+            return 0;
+        }
+        const int32_t H = static_cast<int32_t>(t->size(1));
+        const at::ScalarType type = type_of(c.dtype);
+        const int64_t nq = x.total * H * c.d;
+        void *q = a.here(2, type, nq), *kp = a.here(3, type, pool_size(c)), *vp = a.here(4, type, pool_size(c)), *o = a.here(5, type, nq);
+        const float scale = a.real(6);
+        const int64_t max_len = a.integer(7);
+        const uint64_t *tree = static_cast<uint64_t *>(a.here(8, at::kLong, x.total, true));
+        size_t bytes;
+        void *ws = a.scratch(9, &bytes), *s = a.stream();
+        int status = 0;
+        CALL(status, a, g_entry.attention_paged(&c, &x, H, max_len, scale, q, kp, vp, tree, o, ws, bytes, s));
+        return status;
+    });
+}
+
+// device, raw_stream, parameter type, the structures' types, addresses of the entry points in the order of Entries
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     constexpr int kEntries = sizeof(Entries) / sizeof(void *);
-    constexpr int kObjects = 4;
+    constexpr int kObjects = 7;
     if (n != kObjects + kEntries) {
         PyErr_SetString(PyExc_TypeError, "bind: number of arguments");
         return nullptr;
@@ -279,7 +447,7 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
         if (PyErr_Occurred()) return nullptr;
     }
     std::memcpy(&g_entry, p, sizeof(p));
-    PyObject **to[kObjects] = {&g_device, &g_raw_stream, &g_parameter, &g_desc};
+    PyObject **to[kObjects] = {&g_device, &g_raw_stream, &g_parameter, &g_desc, &g_cache, &g_batch, &g_rope};
     for (int i = 0; i < kObjects; ++i) {
         Py_INCREF(args[i]);
         Py_XDECREF(*to[i]);
@@ -290,7 +458,8 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {METHOD(bind), METHOD(decode), METHOD(decode_slots), METHOD(prefill), METHOD(prefill_varlen), METHOD(attention_decode),
-                           METHOD(attention_prefill), METHOD(project), {nullptr, nullptr, 0, nullptr}};
+                           METHOD(attention_prefill), METHOD(project), METHOD(cache_extend), METHOD(cache_fork), METHOD(cache_truncate), METHOD(cache_accept),
+                           METHOD(cache_compact), METHOD(qk_rope), METHOD(attention_paged), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
