@@ -54,19 +54,83 @@ __device__ __forceinline__ long long block_prefix(long long x, long long *s_wave
     return before + sum - x;
 }
 
-// Where a wavefront of the planning workgroup looks for pages: a run of whole wavefronts' worth.
-__device__ __forceinline__ void wave_pages(int n_pages, int *from, int *to)
+// Where a wavefront of the planning workgroup looks for pages: a run of whole wavefronts' worth; the first `idle` look for none.
+__device__ __forceinline__ void wave_pages(int n_pages, int idle, int *from, int *to)
 {
-    const long long per = ((static_cast<long long>(n_pages) + kPlanThreads - 1) / kPlanThreads) * 64;
-    const int wave = threadIdx.x >> 6;
-    const long long a = per * wave, b = a + per;
-    *from = static_cast<int>(a < n_pages ? a : n_pages);
-    *to = static_cast<int>(b < n_pages ? b : n_pages);
+    const int rows = (n_pages + 63) / 64, waves = kPlanWaves - idle, wave = static_cast<int>(threadIdx.x >> 6) - idle;
+    const long long per = (rows + waves - 1) / waves * 64ll, a = per * wave, b = a + per;
+    *from = wave < 0 ? 0 : static_cast<int>(a < n_pages ? a : n_pages);
+    *to = wave < 0 ? 0 : static_cast<int>(b < n_pages ? b : n_pages);
+}
+// f(first page, the reference count of page first + lane or -1 past the end) for 64 pages after 64, kBatch loads at a time; until f
+// returns false.  (One at a time: 20000 pages 4 us.)
+constexpr int kBatch = 4;
+template <class F>
+__device__ __forceinline__ void each_page(const int32_t *refs, int from, int to, F &&f)
+{
+    const int lane = threadIdx.x & 63;
+    for (int p = from; p < to; p += 64 * kBatch) {
+        int r[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) r[u] = p + 64 * u + lane < to ? refs[p + 64 * u + lane] : -1;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+            if (p + 64 * u < to && !f(p + 64 * u, r[u])) return;
+    }
 }
 
-// Room for the entries' tokens.  Workspace: claim[n_seqs], which entry a row belongs to; before[B], pages that the entries
-// ahead of one need; first[B], the first column that gets a new page (-1: the entry is left out); fresh[n_pages], the free
-// pages in ascending order; moves[B] and their number.
+// What an entry asks for: its row's length, the first column that gets a new page, and how many.  at = -1: it is left out.
+struct Need {
+    int len, at;
+    long long pages;
+};
+__device__ __forceinline__ Need need_of(const CacheArgs &c, const Entry &e, bool again, int *bits)
+{
+    Need w{e.ok ? c.lens[e.row] : -1, -1, 0};
+    if (!e.ok || again || w.len < 0 || w.len > row_room(c)) {
+        *bits |= DSLA_STATUS_CACHE_ENTRY;
+    } else if (static_cast<long long>(w.len) + e.n > row_room(c)) {
+        *bits |= DSLA_STATUS_CACHE_FULL;
+    } else {
+        const bool partial = (w.len & ((1 << c.page_log2) - 1)) != 0 && e.n > 0;
+        const int last = partial ? page_of(c, e.row, w.len - 1) : 0;
+        if (last < 0) {
+            *bits |= DSLA_STATUS_CACHE_ENTRY;
+        } else {
+            w.at = pages_of(w.len, c.page_log2) - (partial && c.refs[last] > 1);
+            w.pages = pages_of(static_cast<long long>(w.len) + e.n, c.page_log2) - w.at;
+        }
+    }
+    return w;
+}
+// An entry that is served, with `before` pages ahead of it: its length, and its shared page that is not full onto the list.
+__device__ __forceinline__ void serve(const CacheArgs &c, const Entry &e, const Need &w, int before, const int32_t *fresh, Move *moves, int *s_moves)
+{
+    if (w.pages > 0 && w.at < pages_of(w.len, c.page_log2)) {
+        const int old = page_of(c, e.row, w.len - 1);
+        moves[atomicAdd(s_moves, 1)] = Move{old, fresh[before], w.len & ((1 << c.page_log2) - 1), 0};
+        atomicSub(&c.refs[old], 1);
+    }
+    c.lens[e.row] = w.len + e.n;
+}
+// The new pages into the table: page number r of all belongs to the last entry that has at most r pages ahead of it.
+__device__ __forceinline__ void place(const CacheArgs &c, const BatchArgs &x, const int32_t *before, const int32_t *first, const int32_t *fresh, int granted)
+{
+    for (int r = threadIdx.x; r < granted; r += kPlanThreads) {
+        int lo = 0, hi = x.B;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (before[mid] <= r) lo = mid;
+            else hi = mid;
+        }
+        const int row = x.row ? x.row[lo] : lo;
+        c.table[static_cast<size_t>(row) * c.max_pages + first[lo] + (r - before[lo])] = fresh[r];
+        c.refs[fresh[r]] = 1;
+    }
+}
+
+// Room for the entries' tokens.  Workspace: claim[n_seqs], the first entry that names a row; before[B], the pages that the entries ahead
+// need; first[B], the first column that gets a new page; fresh[n_pages], the free pages in ascending order; moves[B] and their number.
 __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(CacheArgs c, BatchArgs x, int32_t *claim, int32_t *before, int32_t *first,
                                                                     int32_t *fresh, Move *moves, int32_t *n_moves)
 {
@@ -74,8 +138,6 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(CacheArgs c,
     __shared__ int s_found[kPlanWaves], s_granted, s_moves;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if (tid == 0) s_granted = s_moves = 0;
-
-    // of entries that name one row the first takes part
     for (int b = tid; b < x.B; b += kPlanThreads) {
         const Entry e = read_entry(x, c, b);
         if (e.ok) claim[e.row] = 0x7fffffff;
@@ -87,47 +149,32 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(CacheArgs c,
     }
     __syncthreads();
 
-    // how many pages every entry needs
-    long long ahead = 0;
+    long long wanted = 0;
     int bits = 0;
     for (int b0 = 0; b0 < x.B; b0 += kPlanThreads) {
         const int b = b0 + tid;
-        long long need = 0;
-        int at = -1;
+        Need w{0, -1, 0};
         if (b < x.B) {
             const Entry e = read_entry(x, c, b);
-            const int len = e.ok ? c.lens[e.row] : -1;
-            if (!e.ok || claim[e.row] != b || len < 0 || len > row_room(c)) {
-                bits |= DSLA_STATUS_CACHE_ENTRY;
-            } else if (static_cast<long long>(len) + e.n > row_room(c)) {
-                bits |= DSLA_STATUS_CACHE_FULL;
-            } else {
-                const int have = pages_of(len, c.page_log2);
-                const bool partial = (len & ((1 << c.page_log2) - 1)) != 0 && e.n > 0;
-                const int last = partial ? page_of(c, e.row, len - 1) : 0;
-                if (last < 0) {
-                    bits |= DSLA_STATUS_CACHE_ENTRY;
-                } else {
-                    at = have - (partial && c.refs[last] > 1);
-                    need = pages_of(static_cast<long long>(len) + e.n, c.page_log2) - at;
-                }
-            }
+            w = need_of(c, e, e.ok && claim[e.row] != b, &bits);
         }
         long long sum;
-        const long long mine = ahead + block_prefix(need, s_wave, &sum);
+        const long long mine = wanted + block_prefix(w.pages, s_wave, &sum);
         if (b < x.B) {
             before[b] = static_cast<int32_t>(mine < 0x7fffffff ? mine : 0x7fffffff);
-            first[b] = at;
+            first[b] = w.at;
         }
-        ahead += sum;
+        wanted += sum;
     }
-    const long long wanted = ahead;
 
     // the lowest free pages, as many as are wanted
     int from, to, found = 0;
-    wave_pages(c.n_pages, &from, &to);
+    wave_pages(c.n_pages, 0, &from, &to);
     if (wanted > 0)
-        for (int p = from; p < to; p += 64) found += __popcll(__ballot(p + lane < to && c.refs[p + lane] == 0));
+        each_page(c.refs, from, to, [&](int, int r) {
+            found += __popcll(__ballot(r == 0));
+            return true;
+        });
     if (lane == 0) s_found[wave] = found;
     __syncthreads();
     int rank = 0, all = 0;
@@ -135,55 +182,119 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(CacheArgs c,
         if (w < wave) rank += s_found[w];
         all += s_found[w];
     }
-    if (wanted > 0)
-        for (int p = from; p < to && rank < wanted; p += 64) {
-            const bool is_free = p + lane < to && c.refs[p + lane] == 0;
-            const unsigned long long m = __ballot(is_free);
-            if (is_free) fresh[rank + __popcll(m & ((1ull << lane) - 1))] = p + lane;
+    if (found > 0 && rank < wanted)
+        each_page(c.refs, from, to, [&](int p, int r) {
+            const unsigned long long m = __ballot(r == 0);
+            if (r == 0) fresh[rank + __popcll(m & ((1ull << lane) - 1))] = p + lane;
             rank += __popcll(m);
-        }
+            return rank < wanted;
+        });
     __syncthreads();
 
-    // who is served, what is copied
     for (int b = tid; b < x.B; b += kPlanThreads) {
         int start = -1;
         if (first[b] >= 0) {
             const Entry e = read_entry(x, c, b);
-            const int len = c.lens[e.row];
-            const long long need = pages_of(static_cast<long long>(len) + e.n, c.page_log2) - first[b];
-            if (need > 0 && before[b] + need > all) {
+            Need w{c.lens[e.row], first[b], 0};
+            w.pages = pages_of(static_cast<long long>(w.len) + e.n, c.page_log2) - w.at;
+            if (w.pages > 0 && before[b] + w.pages > all) {
                 bits |= DSLA_STATUS_CACHE_FULL;
-                first[b] = -1;
             } else {
-                start = len;
-                if (need > 0) {
-                    atomicMax(&s_granted, static_cast<int>(before[b] + need));
-                    if (first[b] < pages_of(len, c.page_log2)) {   // a shared page that is not full
-                        const int old = page_of(c, e.row, len - 1);
-                        moves[atomicAdd(&s_moves, 1)] = Move{old, fresh[before[b]], len & ((1 << c.page_log2) - 1), 0};
-                        atomicSub(&c.refs[old], 1);
-                    }
-                }
-                c.lens[e.row] = len + e.n;
+                start = w.len;
+                if (w.pages > 0) atomicMax(&s_granted, static_cast<int>(before[b] + w.pages));
+                serve(c, e, w, before[b], fresh, moves, &s_moves);
             }
         }
         x.start[b] = start;
     }
     if (bits) report(c.status, bits);
     __syncthreads();
+    place(c, x, before, first, fresh, s_granted);
+    if (tid == 0) *n_moves = s_moves;
+}
 
-    // the new pages into the table: page number r of all belongs to the last entry that has at most r pages ahead of it
-    for (int r = tid; r < s_granted; r += kPlanThreads) {
-        int lo = 0, hi = x.B;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (before[mid] <= r) lo = mid;
-            else hi = mid;
-        }
-        const int row = x.row ? x.row[lo] : lo;
-        c.table[static_cast<size_t>(row) * c.max_pages + first[lo] + (r - before[lo])] = fresh[r];
-        c.refs[fresh[r]] = 1;
+// The same for up to kFew entries and kFewPages pages, as decoding has them: bound by the chain of dependent reads, which is cut short.  The
+// first wavefronts look at the entries while the others look for free pages (once: which are free stays in LDS as bits), an
+// entry's thread keeps what it read, and one that names a row again finds out by looking at the rows of those ahead.  The kernel above
+// and this one (us): 64 requests of which some need one of 20000 pages 9.2 / 8.7, 56 branches that all copy 10.4 / 8.2, 16 requests of up
+// to 15 new pages 7.8 / 5.1.
+constexpr int kFew = 256, kFewWaves = kFew / 64, kFewPages = 131072;
+__global__ __launch_bounds__(kPlanThreads) void cache_extend_few_kernel(CacheArgs c, BatchArgs x, int32_t *fresh, Move *moves, int32_t *n_moves)
+{
+    __shared__ unsigned long long s_free[kFewPages / 64];
+    __shared__ __align__(16) int32_t s_row[kFew];
+    __shared__ int32_t s_before[kFew], s_first[kFew];
+    __shared__ __align__(16) int s_need[kFewWaves];
+    __shared__ int s_found[kPlanWaves], s_granted, s_moves;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (tid == 0) s_granted = s_moves = 0;
+    Entry e{0, 0, 0, false};
+    Need w{0, -1, 0};
+    int bits = 0, from = 0, to = 0, found = 0;
+    if (wave < kFewWaves) {
+        if (tid < x.B) e = read_entry(x, c, tid);
+        s_row[tid] = e.ok ? e.row : -1;
+    } else {
+        wave_pages(c.n_pages, kFewWaves, &from, &to);
+        each_page(c.refs, from, to, [&](int p, int r) {
+            const unsigned long long m = __ballot(r == 0);
+            if (lane == 0) s_free[p / 64] = m;
+            found += __popcll(m);
+            return true;
+        });
     }
+    if (lane == 0) s_found[wave] = found;
+    __syncthreads();
+    if (tid < x.B) {
+        int same = 0;
+        if (x.row)
+#pragma unroll 2
+            for (int o = 0; o < x.B; o += 4) {   // (rows behind the last entry are -1)
+                const int4 r = *reinterpret_cast<const int4 *>(s_row + o);
+                same |= ((r.x == e.row) & (o < tid)) | ((r.y == e.row) & (o + 1 < tid)) | ((r.z == e.row) & (o + 2 < tid)) | ((r.w == e.row) & (o + 3 < tid));
+            }
+        w = need_of(c, e, same != 0, &bits);
+    }
+    // sums in 32 bits: what no pool has counts as a page more than there are
+    const int pages = w.pages <= c.n_pages ? static_cast<int>(w.pages) : c.n_pages + 1;
+    int sum = pages;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int y = __shfl_up(sum, off);
+        sum += lane >= off ? y : 0;
+    }
+    if (lane == 63 && wave < kFewWaves) s_need[wave] = sum;
+    __syncthreads();
+    const int4 need = *reinterpret_cast<const int4 *>(s_need);
+    const int before = sum - pages + (wave > 0 ? need.x : 0) + (wave > 1 ? need.y : 0) + (wave > 2 ? need.z : 0), wanted = need.x + need.y + need.z + need.w;
+    if (tid < x.B) {
+        s_before[tid] = before;
+        s_first[tid] = w.at;
+    }
+    int rank = lane < kPlanWaves ? s_found[lane] : 0;
+#pragma unroll
+    for (int off = 1; off < kPlanWaves; off <<= 1) {
+        const int y = __shfl_up(rank, off);
+        rank += lane >= off ? y : 0;
+    }
+    const int all = __builtin_amdgcn_readlane(rank, kPlanWaves - 1);
+    rank = __builtin_amdgcn_readlane(rank, __builtin_amdgcn_readfirstlane(wave)) - found;
+    for (int p = from; p < to && rank < wanted; p += 64) {
+        const unsigned long long m = s_free[p / 64];
+        if (m >> lane & 1) fresh[rank + __popcll(m & ((1ull << lane) - 1))] = p + lane;
+        rank += __popcll(m);
+    }
+    __syncthreads();
+    if (tid < x.B) {
+        const bool served = w.at >= 0 && (pages == 0 || before + pages <= all);
+        if (w.at >= 0 && !served) bits |= DSLA_STATUS_CACHE_FULL;
+        if (served && pages > 0) atomicMax(&s_granted, before + pages);
+        if (served) serve(c, e, w, before, fresh, moves, &s_moves);
+        x.start[tid] = served ? w.len : -1;
+    }
+    if (bits) report(c.status, bits);
+    __syncthreads();
+    place(c, x, s_before, s_first, fresh, s_granted);
     if (tid == 0) *n_moves = s_moves;
 }
 
@@ -251,12 +362,11 @@ __global__ __launch_bounds__(64) void cache_fork_kernel(CacheArgs c, const int32
     if (threadIdx.x == 0) c.lens[s] = len;
 }
 
-// Accepted tokens of an entry to the front.  verdict[b]: the new length, or -1.  One wavefront per entry.
-__global__ __launch_bounds__(64) void cache_accept_kernel(CacheArgs c, BatchArgs x, const int32_t *path, const int32_t *n_accepted, int32_t *verdict)
+// The length that entry b is cut to once its accepted tokens are at the front, or -1: it stays as it is.  By a wavefront; nothing that it
+// reads is changed before cache_accept_cut_kernel.
+__device__ __forceinline__ int accepted_length(const CacheArgs &c, const BatchArgs &x, const Entry &e, int b, const int32_t *path, const int32_t *n_accepted, bool tell)
 {
-    const int b = blockIdx.x, lane = threadIdx.x;
-    const Entry e = read_entry(x, c, b);
-    const int start = x.start[b], n = n_accepted[b];
+    const int start = x.start[b], n = n_accepted[b], lane = threadIdx.x & 63;
     const bool asked = n >= 0 && !(e.ok && start < 0);
     bool good = asked && e.ok && n <= e.n && static_cast<long long>(start) + e.n <= row_room(c) && c.lens[e.row] == start + e.n;
     if (good) {
@@ -271,34 +381,33 @@ __global__ __launch_bounds__(64) void cache_accept_kernel(CacheArgs c, BatchArgs
         }
         good = __ballot(!good) == 0;
     }
-    if (lane == 0) {
-        verdict[b] = good ? start + n : -1;
-        if (asked && !good) report(c.status, DSLA_STATUS_CACHE_ENTRY);
-    }
+    if (tell && lane == 0 && asked && !good) report(c.status, DSLA_STATUS_CACHE_ENTRY);
+    return good ? start + n : -1;
 }
 
-// A wavefront takes one head of one entry in one pool.  path[i] >= i and ascending, so no row is written that a later one of
-// the path still has to be read from: groups of rows go in order, and within a group all are read before any is written.
-__global__ __launch_bounds__(256) void cache_accept_rows_kernel(CacheArgs c, BatchArgs x, const int32_t *path, const int32_t *verdict, int n_pools,
-                                                                int row_bytes, Pools pools)
+// Accepted tokens to the front.  A wavefront takes one head of one entry in one pool; the first of an entry's leaves the verdict.
+// path[i] >= i and ascending, so no row is written that a later one of the path still has to be read from: groups of rows go in order,
+// and within a group all are read before any is written.
+__global__ __launch_bounds__(256) void cache_accept_rows_kernel(CacheArgs c, BatchArgs x, const int32_t *path, const int32_t *n_accepted, int32_t *verdict,
+                                                                int n_pools, int row_bytes, Pools pools)
 {
+    const int lane = threadIdx.x & 63, heads = n_pools > 0 ? n_pools * c.H_kv : 1;   // wavefronts of an entry
     const long long item = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (item >= static_cast<long long>(x.B) * n_pools * c.H_kv) return;
-    const int h = static_cast<int>(item % c.H_kv), b = static_cast<int>(item / c.H_kv / n_pools);
-    char *pool = pools.p[item / c.H_kv % n_pools];
-    if (verdict[b] < 0) return;
+    if (item >= static_cast<long long>(x.B) * heads) return;
+    const int b = static_cast<int>(item / heads), which = static_cast<int>(item % heads);
     const Entry e = read_entry(x, c, b);
-    const int start = x.start[b], n = verdict[b] - start, page = 1 << c.page_log2;
+    const int length = accepted_length(c, x, e, b, path, n_accepted, which == 0);
+    if (which == 0 && lane == 0) verdict[b] = length;
+    if (length < 0 || n_pools == 0) return;
+    const int h = which % c.H_kv, start = x.start[b], n = length - start, page = 1 << c.page_log2;
+    char *pool = pools.p[which / c.H_kv];
     const int lanes = row_bytes / 16, rows = 64 / lanes;   // lanes of a row; rows of a group
     for (int i0 = 0; i0 < n; i0 += rows) {
         const int i = i0 + lane / lanes;
         const int p = i < n ? path[e.cu + i] : i;
-        uint4 row;
         if (p != i) {
-            const int t = start + p;
-            row = reinterpret_cast<const uint4 *>(pool + ((static_cast<size_t>(page_of(c, e.row, t)) * c.H_kv + h) * page + (t & (page - 1))) * row_bytes)[lane % lanes];
-            const int u = start + i;
+            const int t = start + p, u = start + i;
+            const uint4 row = reinterpret_cast<const uint4 *>(pool + ((static_cast<size_t>(page_of(c, e.row, t)) * c.H_kv + h) * page + (t & (page - 1))) * row_bytes)[lane % lanes];
             reinterpret_cast<uint4 *>(pool + ((static_cast<size_t>(page_of(c, e.row, u)) * c.H_kv + h) * page + (u & (page - 1))) * row_bytes)[lane % lanes] = row;
         }
     }
@@ -318,18 +427,23 @@ __global__ __launch_bounds__(kPlanThreads) void cache_compact_kernel(CacheArgs c
     __shared__ int s_live[kPlanWaves], s_src[kPlanWaves], s_dst[kPlanWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int from, to, live = 0;
-    wave_pages(c.n_pages, &from, &to);
-    for (int p = from; p < to; p += 64) live += __popcll(__ballot(p + lane < to && c.refs[p + lane] > 0));
+    wave_pages(c.n_pages, 0, &from, &to);
+    each_page(c.refs, from, to, [&](int, int r) {
+        live += __popcll(__ballot(r > 0));
+        return true;
+    });
     if (lane == 0) s_live[wave] = live;
     __syncthreads();
     int L = 0;
     for (int w = 0; w < kPlanWaves; ++w) L += s_live[w];
+    // in use from page L on, and free below it: as many of the ones as of the others
     int src = 0, dst = 0;
-    for (int p = from; p < to; p += 64) {
-        const bool in = p + lane < to, used = in && c.refs[p + lane] > 0;
+    each_page(c.refs, from, to, [&](int p, int r) {
+        const bool in = p + lane < to, used = r > 0;
         src += __popcll(__ballot(used && p + lane >= L));
         dst += __popcll(__ballot(in && !used && p + lane < L));
-    }
+        return true;
+    });
     if (lane == 0) {
         s_src[wave] = src;
         s_dst[wave] = dst;
@@ -344,8 +458,8 @@ __global__ __launch_bounds__(kPlanThreads) void cache_compact_kernel(CacheArgs c
         }
         n += s_src[w];
     }
-    for (int p = from; p < to; p += 64) {
-        const bool in = p + lane < to, used = in && c.refs[p + lane] > 0;
+    each_page(c.refs, from, to, [&](int p, int r) {
+        const bool in = p + lane < to, used = r > 0;
         const bool moves_away = used && p + lane >= L, hole = in && !used && p + lane < L;
         const unsigned long long ms = __ballot(moves_away), md = __ballot(hole), low = (1ull << lane) - 1;
         if (in && !used && p + lane >= L) to_page[p + lane] = p + lane;   // (a table that names a page no one counts keeps its number)
@@ -357,7 +471,8 @@ __global__ __launch_bounds__(kPlanThreads) void cache_compact_kernel(CacheArgs c
         }
         src += __popcll(ms);
         dst += __popcll(md);
-    }
+        return true;
+    });
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += kPlanThreads) {
         const Move m = moves[i];
@@ -447,8 +562,11 @@ hipError_t launch_cache_extend(const dsla_cache &c, const dsla_batch &x, int n_p
     const Scratch s = scratch_of(c, x.B, workspace);
     {
         ProfileScope ps(DSLA_KERNEL_CACHE, stream);
-        DSLA_LAUNCH(ps, cache_extend_kernel, dim3(1), dim3(kPlanThreads), 0, stream, args_of(c), args_of(x), s.claim, s.before, s.first, s.fresh,
-                    s.moves, s.n_moves);
+        if (x.B <= kFew && c.n_pages <= kFewPages)
+            DSLA_LAUNCH(ps, cache_extend_few_kernel, dim3(1), dim3(kPlanThreads), 0, stream, args_of(c), args_of(x), s.fresh, s.moves, s.n_moves);
+        else
+            DSLA_LAUNCH(ps, cache_extend_kernel, dim3(1), dim3(kPlanThreads), 0, stream, args_of(c), args_of(x), s.claim, s.before, s.first, s.fresh,
+                        s.moves, s.n_moves);
     }
     const hipError_t e = hipGetLastError();
     return e != hipSuccess ? e : launch_moves(c, s, n_pools, pools, stream);
@@ -471,22 +589,15 @@ hipError_t launch_cache_truncate(const dsla_cache &c, const int32_t *new_lens, h
 hipError_t launch_cache_accept(const dsla_cache &c, const dsla_batch &x, const int32_t *path, const int32_t *n_accepted, int n_pools,
                                void *const *pools, void *workspace, hipStream_t stream)
 {
-    const Scratch s = scratch_of(c, x.B, workspace);
-    int32_t *verdict = s.before;
+    int32_t *verdict = scratch_of(c, x.B, workspace).before;
+    const size_t items = static_cast<size_t>(x.B) * (n_pools > 0 ? n_pools * c.H_kv : 1);
     {
         ProfileScope ps(DSLA_KERNEL_CACHE, stream);
-        DSLA_LAUNCH(ps, cache_accept_kernel, dim3(x.B), dim3(64), 0, stream, args_of(c), args_of(x), path, n_accepted, verdict);
+        DSLA_LAUNCH(ps, cache_accept_rows_kernel, dim3(static_cast<unsigned>((items + 3) / 4)), dim3(256), 0, stream, args_of(c), args_of(x), path, n_accepted,
+                    verdict, n_pools, row_bytes(c), pools_of(n_pools, pools));
     }
-    hipError_t e = hipGetLastError();
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (n_pools > 0) {
-        const size_t items = static_cast<size_t>(x.B) * n_pools * c.H_kv;
-        ProfileScope ps(DSLA_KERNEL_CACHE, stream);
-        DSLA_LAUNCH(ps, cache_accept_rows_kernel, dim3(static_cast<unsigned>((items + 3) / 4)), dim3(256), 0, stream, args_of(c), args_of(x), path,
-                    static_cast<const int32_t *>(verdict), n_pools, row_bytes(c), pools_of(n_pools, pools));
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
     ProfileScope ps(DSLA_KERNEL_CACHE, stream);
     DSLA_LAUNCH(ps, cache_accept_cut_kernel, dim3(x.B), dim3(64), 0, stream, args_of(c), args_of(x), static_cast<const int32_t *>(verdict));
     return hipGetLastError();

@@ -148,7 +148,7 @@ for dtype in (0, 1):
         each_launch("init", 1, lambda: lib.dsla_cache_init(c, None))
         for k in (0, 2):
             each_launch("extend", 1 + (k > 0), lambda: lib.dsla_cache_extend(c, x, k, pools, fake, n, None))
-            each_launch("accept", 2 + (k > 0), lambda: lib.dsla_cache_accept(c, x, fake, fake, k, pools, fake, n, None))
+            each_launch("accept", 2, lambda: lib.dsla_cache_accept(c, x, fake, fake, k, pools, fake, n, None))
             each_launch("compact", 2 + (k > 0), lambda: lib.dsla_cache_compact(c, fake, k, pools, fake, n, None))
         each_launch("fork", 1, lambda: lib.dsla_cache_fork(c, fake, None))
         each_launch("truncate", 1, lambda: lib.dsla_cache_truncate(c, fake, None))
