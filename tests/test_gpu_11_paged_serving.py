@@ -1,0 +1,204 @@
+"""The calls on a paged cache together, as a serving loop makes them: prompts, decode steps, forks, turns of drafting, moves; eager and
+replayed from a graph, beside a dense cache and the layer's other kernels."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2506_09316_amd as dsla
+from oracle import paged as orc
+from tests.paged_common import GpuCache, U, W, assert_within, attention_bound, bits, f64, gpu, values
+from tests.util import code
+
+pytestmark = pytest.mark.gpu
+
+FREQ = [10000.0 ** (-i / 32) for i in range(32)]
+
+
+class Loop:
+    """One softmax layer of a serving loop over a cache, checked step by step against the oracle."""
+
+    def __init__(self, dtype, H=8, H_kv=2, d=64, page=16, n_seqs=6, n_pages=120, max_pages=30):
+        self.dtype, self.H, self.H_kv, self.d = dtype, H, H_kv, d
+        self.c = GpuCache(n_pages, page, n_seqs, max_pages, H_kv=H_kv, d=d, dtype=dtype, fill=float("nan"))
+        self.freq = torch.tensor(FREQ, dtype=torch.float32, device="cuda")
+        self.w = [1 + 0.2 * values((d,), "f32", 50 + i) for i in range(2)]
+        self.seed = 0
+
+    def step(self, rows, counts, tree=None, depth=None):
+        """Room, rotation and writing, attention; returns what the oracle says of the entries' starts."""
+        c, total = self.c, sum(counts)
+        x = c.batch(rows, list(counts))
+        start = c.extend(x)
+        self.seed += 1
+        q, k, v = (values((total, n, self.d), self.dtype, 10 * self.seed + i, 1.3) for i, n in enumerate((self.H, self.H_kv, self.H_kv)))
+        rope = dsla.make_rope(self.H, self.H_kv, self.d, io_dtype=code(self.dtype), inv_freq=self.freq, q_weight=self.w[0], k_weight=self.w[1], offsets=gpu(depth))
+        q_out, k_out, o = torch.empty_like(q), torch.empty_like(k), torch.full_like(q, 7.0)
+        dsla.dsla_qk_rope(rope, q, k, v, q_out, k_out, c.desc, x, c.pools[0], c.pools[1])
+        where = [(b, j) for b, n in enumerate(counts) for j in range(n)]
+        position = np.array([max(0, start[b]) + (j if depth is None else depth[m]) for m, (b, j) in enumerate(where)])
+        served = np.array([start[b] >= 0 for b, _ in where])
+        for name, got, was, weight in (("q", q_out, q, self.w[0]), ("k", k_out, k, self.w[1])):
+            want, size = orc.rotate(f64(was), f64(weight), 1e-6, position, f64(self.freq), False)
+            assert_within(name, f64(got)[served], want[served], (32 * U * size + (W if self.dtype == "bf16" else U) * np.abs(want))[served])
+        kb, vb = bits(k_out), bits(v)
+        for m, (b, j) in enumerate(where):
+            if served[m]:
+                t = int(start[b]) + j
+                p = c.oracle.table[rows[b], t // c.oracle.page]
+                c.oracle.pools[0][p, :, t % c.oracle.page], c.oracle.pools[1][p, :, t % c.oracle.page] = kb[m], vb[m]
+        c.same()
+        n = dsla.dsla_attention_paged_workspace_bytes(c.desc, x, self.H, 500)
+        ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+        dsla.dsla_attention_paged(c.desc, x, q_out, c.pools[0], c.pools[1], o, 0.125, 500, tree=None if tree is None else gpu(tree, torch.int64), workspace=ws)
+        cu = np.concatenate([[0], np.cumsum(counts)])
+        want, size, reach = orc.attention(c.oracle, f64(c.pools[0]), f64(c.pools[1]), cu, rows, start, f64(q_out), 0.125, tree)
+        assert (f64(o)[~served] == 7).all()
+        assert_within("o", f64(o)[served], want[served], attention_bound(want, size, reach, 500, self.d, self.dtype)[served])
+        return x
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_serving_loop(dtype):
+    loop = Loop(dtype)
+    c = loop.c
+    loop.step([0, 3, 5], [40, 1, 64])                         # prompts
+    loop.step([5, 0, 3], [1, 1, 1])                           # a decode step
+    c.fork([-1, 0, 0, -1, 5, -1])                             # sampled several ways
+    loop.step([0, 1, 2, 3, 4, 5], [1] * 6)
+    loop.step([0, 1, 2, 3, 4, 5], [1, 2, 1, 30, 1, 5])
+    tree, depth = [1, 3, 5, 11, 19, 37] + [1, 3, 5], [0, 1, 1, 2, 2, 2, 0, 1, 1]
+    x = loop.step([2, 4], [6, 3], tree, depth)                # a turn of drafting
+    c.accept(x, [0, 1, 4, 0, 0, 0, 0, 2, 0], [3, 2])
+    loop.step([2, 4, 1], [1, 1, 1])
+    c.truncate([0, -1, -1, 20, -1, 64])                       # one ends, two go back
+    c.compact()
+    loop.step([0, 3, 4, 5], [50, 3, 1, 1])                    # another comes
+    loop.step([0, 1, 2, 3, 4, 5], [1] * 6)
+    assert c.status.item() == 0
+    c.truncate([0] * 6)
+    assert c.compact() == 0 and c.refs.sum().item() == 0
+
+
+def test_short_of_pages():
+    """Entries that got no room are left out by every call of the step, and take part again once there is some."""
+    loop = Loop("bf16", n_pages=8, n_seqs=4)
+    loop.step([0, 1, 2], [60, 60, 20])
+    assert loop.c.status.item() == 2
+    loop.step([0, 1, 2], [1, 1, 30])
+    loop.c.truncate([0, -1, -1, -1])
+    loop.step([2, 1], [40, 1])
+
+
+@pytest.mark.parametrize("H, H_kv", [(4, 4), (8, 2)])
+def test_beside_a_dense_cache(H, H_kv):
+    """The same keys and values in pages and in a dense cache: dsla_attention_decode says the same within both bounds (its weights are not
+    rounded, so its bound is the one of 32 bits and a rounding)."""
+    lens, d, page, T = [700, 33, 1], 128, 64, 700
+    k, v = (values((3, T, H_kv, d), "bf16", i) for i in (1, 2))
+    q = values((3, H, d), "bf16", 3)
+    c = GpuCache(30, page, 3, 12, H_kv=H_kv, d=d, fill=float("nan"))
+    c.extend(c.batch([2, 0, 1], lens))
+    for b, row in enumerate([2, 0, 1]):
+        for t in range(lens[b]):
+            p = int(c.oracle.table[row, t // page])
+            c.pools[0][p, :, t % page], c.pools[1][p, :, t % page] = k[b, t], v[b, t]
+    x = c.batch([2, 0, 1], start=[n - 1 for n in lens])
+    o, dense = torch.empty_like(q), torch.empty_like(q)
+    ws = torch.empty(dsla.dsla_attention_paged_workspace_bytes(c.desc, x, H, T), dtype=torch.uint8, device="cuda")
+    dsla.dsla_attention_paged(c.desc, x, q, c.pools[0], c.pools[1], o, d ** -0.5, T, workspace=ws)
+    kk, vv = (t.repeat_interleave(H // H_kv, 2).contiguous() for t in (k, v))
+    dws = torch.empty(max(16, dsla.dsla_attention_decode_workspace_bytes(3, H, d, T)), dtype=torch.uint8, device="cuda")
+    dsla.dsla_attention_decode(q, kk, vv, dense, d ** -0.5, dws, seq_lens=gpu(lens))
+    want, size, reach = orc.attention(c.oracle, f64(c.pools[0]), f64(c.pools[1]), None, [2, 0, 1], c.start(x).tolist(), f64(q), d ** -0.5)
+    assert_within("paged", f64(o), want, attention_bound(want, size, reach, T, d, "bf16"))
+    assert_within("dense", f64(dense), want, attention_bound(want, size, reach, T, d, "f32") + W * np.abs(want))
+
+
+def test_a_step_replayed_from_a_graph():
+    """Room, rotation, attention and the acceptance of a path in one graph, replayed over inputs that change, two graphs with workspaces of
+    their own in turn, with eager work and waits between: every replay as the eager calls."""
+    H, H_kv, d, page, n_seqs, layers = 8, 2, 64, 16, 4, 2
+    c = GpuCache(200, page, n_seqs, 40, H_kv=H_kv, d=d, n_pools=2 * layers)
+    c.extend(c.batch([0, 1, 2, 3], [100, 3, 47, 200]))
+    c.fork([-1, -1, -1, -1])
+    freq, scale = torch.tensor(FREQ, dtype=torch.float32, device="cuda"), 0.125
+    counts = [5, 1, 7, 3]
+    tree, depth = [1, 3, 5, 11, 19] + [1] + [1, 3, 5, 9, 17, 33, 65] + [1, 3, 7], [0, 1, 1, 2, 2, 0, 0, 1, 1, 1, 1, 1, 1, 0, 1, 2]
+    path, accepted = gpu([0, 1, 3, 0, 0] + [0] + [0, 4, 0, 0, 0, 0, 0] + [0, 1, 2]), gpu([3, 1, 2, 3])
+    x = dsla.make_batch(gpu([0] * 4), 16, cu=gpu(np.concatenate([[0], np.cumsum(counts)])), row=gpu([3, 0, 1, 2]), max_n=7)
+    rope = dsla.make_rope(H, H_kv, d, io_dtype=1, inv_freq=freq, offsets=gpu(depth))
+    inputs = [[torch.empty(16, n, d, dtype=torch.bfloat16, device="cuda") for n in (H, H_kv, H_kv)] for _ in range(layers)]
+    rotated, o = ([torch.empty(16, H, d, dtype=torch.bfloat16, device="cuda") for _ in range(layers)] for _ in range(2))
+    tree_t = gpu(tree, torch.int64)
+
+    def turn(ws):
+        dsla.dsla_cache_extend(c.desc, x, c.handles, ws)
+        for l in range(layers):
+            dsla.dsla_qk_rope(rope, *inputs[l], rotated[l], None, c.desc, x, c.pools[2 * l], c.pools[2 * l + 1])
+            dsla.dsla_attention_paged(c.desc, x, rotated[l], c.pools[2 * l], c.pools[2 * l + 1], o[l], scale, 640, tree=tree_t, workspace=ws)
+        dsla.dsla_cache_accept(c.desc, x, path, accepted, c.handles, ws)
+
+    nbytes = max(dsla.dsla_cache_workspace_bytes(c.desc, 4), dsla.dsla_attention_paged_workspace_bytes(c.desc, x, H, 640))
+    state = [c.table, c.lens, c.refs, *c.pools]
+    saved = [t.clone() for t in state]
+
+    def restore():
+        for t, s in zip(state, saved):
+            t.copy_(s)
+
+    def fill(i):
+        for l in range(layers):
+            for j, t in enumerate(inputs[l]):
+                t.copy_(values(tuple(t.shape), "bf16", 1000 + 100 * i + 10 * l + j))
+
+    eager = []
+    ws = torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda")
+    for i in range(6):
+        fill(i)
+        turn(ws)
+        eager.append([t.clone() for t in state + o])
+    restore()
+    graphs = []
+    for _ in range(2):
+        own = torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda")
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            turn(own)
+        torch.cuda.current_stream().wait_stream(s)
+        restore()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            turn(own)
+        graphs.append((g, own))
+    restore()
+    for i in range(6):
+        fill(i)
+        graphs[i % 2][0].replay()
+        if i % 3 == 0:
+            torch.cuda.synchronize()
+        for n, (got, want) in enumerate(zip(state + o, eager[i])):
+            assert torch.equal(got.view(torch.int16) if got.dtype == torch.bfloat16 else got, want.view(torch.int16) if want.dtype == torch.bfloat16 else want), (i, n)
+    assert c.status.item() == 0
+
+
+def test_the_general_way_says_the_same(monkeypatch):
+    """Without the native calls every call goes through ctypes: the same results, and the same refusals."""
+    def run():
+        loop = Loop("bf16")
+        x = loop.step([0, 3], [40, 6], [(2 << j) - 1 for j in range(40)] + [1, 3, 5, 11, 19, 37], list(range(40)) + [0, 1, 1, 2, 2, 2])
+        loop.c.accept(x, list(range(40)) + [0, 1, 3, 0, 0, 0], [40, 3])
+        loop.c.fork([-1, 0, -1, -1, 3, -1])
+        loop.step([0, 1, 4], [1, 1, 1])
+        loop.c.truncate([0, -1, -1, -1, -1, -1])
+        loop.c.compact()
+        for call in (lambda: dsla.dsla_cache_truncate(loop.c.desc, gpu([0])), lambda: dsla.dsla_cache_fork(loop.c.desc, None),
+                     lambda: dsla.dsla_qk_rope(dsla.make_rope(1, 1, 64, io_dtype=1), loop.c.pools[0][0], loop.c.pools[0][0], None, loop.c.pools[0][0]),
+                     lambda: dsla.dsla_cache_accept(loop.c.desc, x, gpu([0]), gpu([0, 0]), loop.c.handles, loop.c.ws)):
+            with pytest.raises(ValueError):
+                call()
+        return [bits(p) for p in loop.c.pools]
+    a = run()
+    monkeypatch.setattr(dsla.binding, "_native", dsla.binding._General)
+    b = run()
+    assert all(np.array_equal(s, t) for s, t in zip(a, b))
