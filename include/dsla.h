@@ -380,12 +380,12 @@ DSLA_API dsla_status dsla_attention_prefill(int32_t B, int32_t H, int32_t d, int
  * n_pages before it uses them.  Calls that change the cache go on one stream, or are ordered by the caller.
  */
 typedef struct {
-    int32_t n_pages;    /* pages of a pool                                                      */
+    int32_t n_pages;    /* pages of a pool, up to 2^30                                          */
     int32_t page;       /* tokens of a page: 16, 32, 64 or 128                                  */
-    int32_t H_kv;       /* key/value heads                                                      */
+    int32_t H_kv;       /* key/value heads, up to 2^16                                          */
     int32_t d;          /* head size, 64 or 128                                                 */
     int32_t dtype;      /* dsla_dtype of the pools                                              */
-    int32_t n_seqs;     /* rows of the table                                                    */
+    int32_t n_seqs;     /* rows of the table, up to 2^23                                        */
     int32_t max_pages;  /* columns of the table; max_pages * page <= 2^31 - 256                 */
     int32_t *table;     /* DEVICE [n_seqs][max_pages]                                           */
     int32_t *lens;      /* DEVICE [n_seqs]                                                      */
@@ -449,7 +449,7 @@ DSLA_API dsla_status dsla_cache_truncate(const dsla_cache *cache, const int32_t 
  * path[cu[b]], path[cu[b] + 1], ... (ascending), such as the accepted path of a tree of drafted tokens: their rows move to
  * start[b], start[b] + 1, ... in every pool, and the sequence is cut behind them.
  *   path       : DEVICE [total]      n_accepted : DEVICE [B], 0 .. tokens of b; negative: entry b stays as it is
- * An entry whose path is not ascending or out of range, whose tokens are not the last, or that would change a page which other
+ * B * n_pools * H_kv is limited to 2^25 (else DSLA_ERR_SHAPE).  An entry whose path is not ascending or out of range, whose tokens are not the last, or that would change a page which other
  * sequences name, stays as it is and is reported.
  */
 DSLA_API dsla_status dsla_cache_accept(const dsla_cache *cache, const dsla_batch *batch, const int32_t *path, const int32_t *n_accepted,

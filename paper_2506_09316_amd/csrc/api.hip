@@ -447,7 +447,7 @@ bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0
 dsla_status check_cache(const dsla_cache *c)
 {
     if (!c) return DSLA_ERR_NULL;
-    if (c->n_pages <= 0 || c->n_pages > (1 << 30) || c->H_kv <= 0 || c->n_seqs <= 0 || c->max_pages <= 0) return DSLA_ERR_SHAPE;
+    if (c->n_pages <= 0 || c->n_pages > (1 << 30) || c->H_kv <= 0 || c->n_seqs <= 0 || c->n_seqs > (1 << 23) || c->max_pages <= 0) return DSLA_ERR_SHAPE;
     if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return DSLA_ERR_UNSUPPORTED;
     if (c->d != 64 && c->d != 128) return DSLA_ERR_UNSUPPORTED;
     if (c->dtype != DSLA_F32 && c->dtype != DSLA_BF16) return DSLA_ERR_UNSUPPORTED;
@@ -471,7 +471,7 @@ dsla_status check_pools(const dsla_cache &c, int32_t n_pools, void *const *pools
 {
     if (n_pools < 0) return DSLA_ERR_SHAPE;
     if (n_pools > DSLA_MAX_POOLS) return DSLA_ERR_UNSUPPORTED;
-    if (entries * n_pools * c.H_kv > 0x7fffffffLL) return DSLA_ERR_SHAPE;   // one wavefront each
+    if (entries * n_pools * c.H_kv > (1 << 25)) return DSLA_ERR_SHAPE;   // a wavefront each
     if (n_pools > 0 && !pools) return DSLA_ERR_NULL;
     for (int i = 0; i < n_pools; ++i) {
         if (!pools[i]) return DSLA_ERR_NULL;

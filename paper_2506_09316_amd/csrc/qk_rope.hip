@@ -12,17 +12,21 @@ struct RopeArgs {
     void *q_out, *k_out, *k_pages, *v_pages;
     const float *inv_freq, *q_weight, *k_weight;
     const int32_t *offsets;
-    int H, H_kv, rot, rows;
+    int H, H_kv, rot, first;
     float eps;
     bool cached, interleaved;
     CacheArgs c;
     BatchArgs x;
 };
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Everything is read once and written once, whole rows at a time: with the non-temporal hint on both 16000 tokens take 74 us (5.3 TB/s, what a
+// copy reaches), on the stores only 77, on the loads only 81, without 80.
 __device__ __forceinline__ void load8(const bf16_t *p, float (&f)[8])
 {
-    const uint4 u = *reinterpret_cast<const uint4 *>(p);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         f[2 * i] = __uint_as_float(w[i] << 16);
@@ -31,21 +35,24 @@ __device__ __forceinline__ void load8(const bf16_t *p, float (&f)[8])
 }
 __device__ __forceinline__ void load8(const float *p, float (&f)[8])
 {
-    const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    const f32x4 a = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p)), b = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p + 4));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[i] = a[i];
+        f[4 + i] = b[i];
+    }
 }
 __device__ __forceinline__ void store8(bf16_t *p, const float (&f)[8])
 {
-    uint32_t w[4];
+    u32x4 w;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = f32_to_bf16_bits(f[2 * i]) | static_cast<uint32_t>(f32_to_bf16_bits(f[2 * i + 1])) << 16;
-    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(p));
 }
 __device__ __forceinline__ void store8(float *p, const float (&f)[8])
 {
-    *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
-    *reinterpret_cast<float4 *>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
+    __builtin_nontemporal_store(f32x4{f[0], f[1], f[2], f[3]}, reinterpret_cast<f32x4 *>(p));
+    __builtin_nontemporal_store(f32x4{f[4], f[5], f[6], f[7]}, reinterpret_cast<f32x4 *>(p + 4));
 }
 
 // Cosine and sine of position * freq: the turns and their fraction in 64 bits (a far position in 32 bits has no fraction left).
@@ -60,7 +67,7 @@ __global__ __launch_bounds__(256) void qk_rope_kernel(RopeArgs a)
 {
     constexpr int LPR = D / 16, ROWS = 256 / LPR;   // lanes of a head; heads at a time
     __shared__ float s_cos[D / 2], s_sin[D / 2];
-    const int m = blockIdx.x;
+    const int m = a.first + blockIdx.x;
     // the token's entry, its place in the sequence and its page
     long long place = 0, position = a.offsets ? a.offsets[m] : m;
     int page = -1;
@@ -78,14 +85,14 @@ __global__ __launch_bounds__(256) void qk_rope_kernel(RopeArgs a)
         const Entry e = read_entry(a.x, a.c, b);
         const int start = a.x.start[b], j = m - e.cu;
         if (!e.ok) {
-            if (threadIdx.x == 0) report(a.c.status, DSLA_STATUS_CACHE_ENTRY);
+            if (threadIdx.x == 0 && blockIdx.y == 0) report(a.c.status, DSLA_STATUS_CACHE_ENTRY);
             return;
         }
         if (start < 0 || j < 0 || j >= e.n) return;
         place = static_cast<long long>(start) + j;
         position = static_cast<long long>(start) + (a.offsets ? a.offsets[m] : j);
         page = place < row_room(a.c) ? page_of(a.c, e.row, static_cast<int>(place)) : -1;
-        if (page < 0 && threadIdx.x == 0) report(a.c.status, DSLA_STATUS_CACHE_ENTRY);
+        if (page < 0 && threadIdx.x == 0 && blockIdx.y == 0) report(a.c.status, DSLA_STATUS_CACHE_ENTRY);
     }
     for (int i = threadIdx.x; i < a.rot / 2; i += 256) angle_of(position, a.inv_freq[i], &s_cos[i], &s_sin[i]);
     __syncthreads();
@@ -96,7 +103,7 @@ __global__ __launch_bounds__(256) void qk_rope_kernel(RopeArgs a)
     const bool turns = c < rotated;
     const int p0 = a.interleaved || !turns ? 2 * c : c, p1 = a.interleaved || !turns ? 2 * c + 1 : c + rotated;
     const int heads = a.H + a.H_kv + (a.cached ? a.H_kv : 0);
-    for (int r = threadIdx.x / LPR; r < heads; r += ROWS) {   // (the lanes of a head stay together)
+    for (int r = blockIdx.y * ROWS + threadIdx.x / LPR; r < heads; r += gridDim.y * ROWS) {   // (the lanes of a head stay together)
         const bool is_q = r < a.H, is_v = r >= a.H + a.H_kv;
         const int h = is_q ? r : is_v ? r - a.H - a.H_kv : r - a.H;
         const TIO *src = static_cast<const TIO *>(is_q ? a.q : is_v ? a.v : a.k) + (static_cast<size_t>(m) * (is_q ? a.H : a.H_kv) + h) * D;
@@ -179,7 +186,6 @@ hipError_t launch_qk_rope(const dsla_rope &r, int64_t rows, const void *q, const
     a.H = r.H;
     a.H_kv = r.H_kv;
     a.rot = r.rot_dim;
-    a.rows = static_cast<int>(rows);
     a.eps = r.eps;
     a.cached = c != nullptr;
     a.interleaved = r.interleaved != 0;
@@ -190,9 +196,20 @@ hipError_t launch_qk_rope(const dsla_rope &r, int64_t rows, const void *q, const
     const bool bf16 = r.io_dtype == DSLA_BF16;
     auto kernel = bf16 ? (r.d == 128 ? qk_rope_kernel<128, bf16_t> : qk_rope_kernel<64, bf16_t>)
                        : (r.d == 128 ? qk_rope_kernel<128, float> : qk_rope_kernel<64, float>);
-    ProfileScope ps(DSLA_KERNEL_QK_ROPE, stream);
-    DSLA_LAUNCH(ps, kernel, dim3(static_cast<unsigned>(rows)), dim3(256), 0, stream, a);
-    return hipGetLastError();
+    // A workgroup to a token: what it reads of the token is uniform and read before anything is written, by scalar loads (in a loop over
+    // tokens these are vector loads: 16000 tokens 94 us instead of 78).  Where there are few, one to every chunk of a token's heads.
+    const int heads = r.H + r.H_kv + (c ? r.H_kv : 0), at_a_time = 256 / (r.d / 16);
+    const unsigned chunks = rows < 256 ? (heads + at_a_time - 1) / at_a_time : 1;
+    constexpr int64_t kMost = 1 << 23;   // threads of a launch are a 32-bit number
+    for (int64_t first = 0; first < rows; first += kMost) {
+        a.first = static_cast<int>(first);
+        const int64_t n = rows - first < kMost ? rows - first : kMost;
+        ProfileScope ps(DSLA_KERNEL_QK_ROPE, stream);
+        DSLA_LAUNCH(ps, kernel, dim3(static_cast<unsigned>(n), chunks), dim3(256), 0, stream, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace dsla

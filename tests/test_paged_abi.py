@@ -35,7 +35,7 @@ def rope(**change):
                                 offsets=None), **change))
 
 
-BAD_CACHES = [(dict(n_pages=0), SHAPE), (dict(n_pages=(1 << 30) + 1), SHAPE), (dict(H_kv=0), SHAPE), (dict(H_kv=70000), SHAPE), (dict(n_seqs=0), SHAPE),
+BAD_CACHES = [(dict(n_pages=0), SHAPE), (dict(n_pages=(1 << 30) + 1), SHAPE), (dict(H_kv=0), SHAPE), (dict(H_kv=70000), SHAPE), (dict(n_seqs=0), SHAPE), (dict(n_seqs=(1 << 23) + 1), SHAPE),
               (dict(max_pages=0), SHAPE), (dict(max_pages=1 << 25), SHAPE), (dict(page=48), UNSUPPORTED), (dict(page=0), UNSUPPORTED), (dict(page=256), UNSUPPORTED),
               (dict(d=96), UNSUPPORTED), (dict(dtype=2), UNSUPPORTED), (dict(table=None), NULL), (dict(lens=None), NULL), (dict(refs=None), NULL),
               (dict(table=4098), SHAPE), (dict(status=4097), SHAPE)]
@@ -90,8 +90,8 @@ def test_pools_and_workspaces(lib):
     assert lib.dsla_cache_fork(c, None, None) == lib.dsla_cache_truncate(c, None, None) == lib.dsla_cache_compact(c, None, 0, None, P, 1 << 30, None) == NULL
     assert lib.dsla_cache_accept(c, ctypes.byref(batch()), None, P, 0, None, P, 1 << 30, None) == NULL
     assert lib.dsla_cache_accept(c, ctypes.byref(batch()), P, ctypes.c_void_p(4098), 0, None, P, 1 << 30, None) == SHAPE
-    big = cache(n_seqs=1 << 30, H_kv=1 << 16)
-    assert lib.dsla_cache_accept(ctypes.byref(big), ctypes.byref(batch(B=1 << 20)), P, P, 1, (ctypes.c_void_p * 1)(4096), P, 1 << 62, None) == SHAPE
+    big = cache(n_seqs=1 << 20, H_kv=1 << 6)
+    assert lib.dsla_cache_accept(ctypes.byref(big), ctypes.byref(batch(B=(1 << 19) + 1)), P, P, 1, (ctypes.c_void_p * 1)(4096), P, 1 << 62, None) == SHAPE
 
 
 def test_rope_arguments(lib):
