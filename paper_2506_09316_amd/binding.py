@@ -424,6 +424,14 @@ def _here(t, dtype, numel=None, optional=False):
     return p
 
 
+def _same_device(*structures):
+    """Structures are for the device that their tensors are on."""
+    here = _torch._cuda_getDevice()
+    for x in structures:
+        if getattr(x, "device", here) != here:
+            raise ValueError(f"a structure for device {x.device}, and the current one is {here}")
+
+
 def _io_dtype(code):
     import torch
     return torch.bfloat16 if code == DSLA_BF16 else torch.float32
@@ -437,7 +445,7 @@ def make_cache(table, lens, refs, *, page, H_kv, d, dtype, status=None) -> DslaC
     n_seqs, max_pages = table.shape
     c = DslaCache(int(refs.numel()), int(page), int(H_kv), int(d), int(dtype), int(n_seqs), int(max_pages), _here(table, torch.int32),
                   _here(lens, torch.int32, n_seqs), _here(refs, torch.int32), _here(status, torch.int32, 1, optional=True))
-    c._keep = (table, lens, refs, status)
+    c._keep, c.device = (table, lens, refs, status), table.get_device()
     return c
 
 
@@ -449,7 +457,7 @@ def make_batch(start, total, *, cu=None, row=None, max_n=1) -> DslaBatch:
     B = start.numel()
     x = DslaBatch(int(B), int(max_n), int(total), _here(cu, torch.int32, B + 1, optional=True), _here(row, torch.int32, B, optional=True),
                   _here(start, torch.int32))
-    x._keep = (start, cu, row)
+    x._keep, x.device = (start, cu, row), start.get_device()
     return x
 
 
@@ -461,6 +469,8 @@ class Pools:
         for t in self.tensors:
             _here(t, t.dtype)
         self.array = (ctypes.c_void_p * max(1, len(self.tensors)))(*[t.data_ptr() for t in self.tensors])
+        if self.tensors:
+            self.device = _torch._cuda_getDevice()
         self.address, self.sizes = ctypes.addressof(self.array), {(t.numel(), t.dtype) for t in self.tensors}
 
     def of(self, cache: DslaCache):
@@ -487,12 +497,15 @@ def dsla_cache_workspace_bytes(cache: DslaCache, B: int) -> int:
 
 def dsla_cache_init(cache: DslaCache):
     """All pages free, all sequences empty (include/dsla.h: dsla_cache_init)."""
-    _check(load_library().dsla_cache_init(ctypes.byref(cache), _stream()))
+    lib = _lib or load_library()
+    _same_device(cache)
+    _check(lib.dsla_cache_init(ctypes.byref(cache), _stream()))
 
 
 def dsla_cache_extend(cache: DslaCache, batch: DslaBatch, pools: Pools, workspace):
     """Room for the tokens of every entry at the end of its sequence (include/dsla.h: dsla_cache_extend)."""
     lib, (n, array) = _lib or load_library(), pools.of(cache)
+    _same_device(cache, batch, pools)
     status = _native.cache_extend(cache, batch, n, pools.address, workspace)
     if status is not None:
         return _check(status)
@@ -502,6 +515,7 @@ def dsla_cache_extend(cache: DslaCache, batch: DslaBatch, pools: Pools, workspac
 def dsla_cache_fork(cache: DslaCache, parent):
     """Sequences that share the pages of others (include/dsla.h: dsla_cache_fork).  parent: int32 GPU tensor [n_seqs]."""
     lib = _lib or load_library()
+    _same_device(cache)
     status = _native.cache_fork(cache, parent)
     if status is not None:
         return _check(status)
@@ -512,6 +526,7 @@ def dsla_cache_fork(cache: DslaCache, parent):
 def dsla_cache_truncate(cache: DslaCache, new_lens):
     """Sequences cut to their first tokens, or ended (include/dsla.h: dsla_cache_truncate).  new_lens: int32 GPU tensor [n_seqs]."""
     lib = _lib or load_library()
+    _same_device(cache)
     status = _native.cache_truncate(cache, new_lens)
     if status is not None:
         return _check(status)
@@ -522,6 +537,7 @@ def dsla_cache_truncate(cache: DslaCache, new_lens):
 def dsla_cache_accept(cache: DslaCache, batch: DslaBatch, path, n_accepted, pools: Pools, workspace):
     """Keeps the accepted tokens of every entry (include/dsla.h: dsla_cache_accept).  path: int32 GPU tensor [total], n_accepted [B]."""
     lib, (n, array) = _lib or load_library(), pools.of(cache)
+    _same_device(cache, batch, pools)
     status = _native.cache_accept(cache, batch, path, n_accepted, n, pools.address, workspace)
     if status is not None:
         return _check(status)
@@ -533,6 +549,7 @@ def dsla_cache_accept(cache: DslaCache, batch: DslaBatch, path, n_accepted, pool
 def dsla_cache_compact(cache: DslaCache, n_live, pools: Pools, workspace):
     """Pages in use to the front of the pools (include/dsla.h: dsla_cache_compact).  n_live: int32 GPU tensor [1], written."""
     lib, (n, array) = _lib or load_library(), pools.of(cache)
+    _same_device(cache, pools)
     status = _native.cache_compact(cache, n_live, n, pools.address, workspace)
     if status is not None:
         return _check(status)
@@ -549,6 +566,8 @@ def make_rope(H, H_kv, d, *, io_dtype, inv_freq=None, interleaved=False, q_weigh
                  _here(inv_freq, torch.float32, optional=True), _here(q_weight, torch.float32, d, optional=True),
                  _here(k_weight, torch.float32, d, optional=True), _here(offsets, torch.int32, optional=True))
     r._keep = (inv_freq, q_weight, k_weight, offsets)
+    if any(t is not None for t in r._keep):
+        r.device = _torch._cuda_getDevice()
     return r
 
 
@@ -558,6 +577,7 @@ def dsla_qk_rope(rope: DslaRope, q, k, v, q_out, k_out=None, cache: DslaCache = 
     lib, total = _lib or load_library(), q.shape[0]
     if rope.offsets and rope._keep[3].numel() != total:
         raise ValueError(f"{rope._keep[3].numel()} offsets for {total} tokens")
+    _same_device(rope, cache, batch)
     status = _native.qk_rope(rope, total, q, k, v, q_out, k_out, cache, batch, k_pages, v_pages)
     if status is not None:
         return _check(status)
@@ -577,6 +597,7 @@ def dsla_attention_paged(cache: DslaCache, batch: DslaBatch, q, k_pages, v_pages
     """Attention of the last tokens of every sequence over a paged cache (include/dsla.h: dsla_attention_paged).  q, o [total, H, d];
     k_pages, v_pages [n_pages, H_kv, page, d]; tree: int64 GPU tensor [total] (its bits) or None."""
     lib = _lib or load_library()
+    _same_device(cache, batch)
     status = _native.attention_paged(cache, batch, q, k_pages, v_pages, o, scale, max_len, tree, workspace)
     if status is not None:
         return _check(status)

@@ -478,8 +478,8 @@ __global__ __launch_bounds__(256) void attention_paged_merge_kernel(PagedArgs a)
     }
 }
 
-// Stretches of the line: one workgroup to a compute unit.  256 / 384 / 512 / 768 / 1024 of them (us, 16 bits, one token each): 64
-// requests of 100 to 8192 tokens, 32 heads on 8 of 128, 88 / 101 / 87 / 87 / 93; one of 131072 89 / 107 / 92 / 91 / 97; 16 of 8192
+// Stretches of the line: one workgroup to a compute unit.  256 / 384 / 512 / 768 / 1024 of them (us, with kAhead = 1; 16 bits, one token
+// each): 64 requests of 100 to 8192 tokens, 32 heads on 8 of 128, 88 / 101 / 87 / 87 / 93; one of 131072 89 / 107 / 92 / 91 / 97; 16 of 8192
 // 86 / 104 / 90 / 89 / 94; 64 of 300 to 700 33 / 35 / 32 / 32 / 36; 8 of 500 to 2000 17.2 / 19.1 / 19.2 / 16.9 / 17.0.
 // (The kernel for many rows: two workgroups to a unit.)
 constexpr int kStretches = 256, kRowsStretches = 512;

@@ -202,3 +202,30 @@ def test_the_general_way_says_the_same(monkeypatch):
     monkeypatch.setattr(dsla.binding, "_native", dsla.binding._General)
     b = run()
     assert all(np.array_equal(s, t) for s, t in zip(a, b))
+
+
+def test_another_device_is_refused(monkeypatch):
+    """Structures and tensors of a device that is not the current one (there is one here: the current one is said to be another)."""
+    loop = Loop("f32")
+    c, x = loop.c, loop.c.batch([0, 1])
+    c.extend(x)
+    q = torch.zeros(2, 8, 64, device="cuda")
+    kv = torch.zeros(2, 2, 64, device="cuda")
+    ints, rope = gpu([0] * 6), dsla.make_rope(8, 2, 64, io_dtype=0)
+    calls = [lambda: dsla.dsla_cache_init(c.desc), lambda: dsla.dsla_cache_extend(c.desc, x, c.handles, c.ws), lambda: dsla.dsla_cache_truncate(c.desc, ints),
+             lambda: dsla.dsla_cache_fork(c.desc, ints), lambda: dsla.dsla_cache_compact(c.desc, gpu([0]), c.handles, c.ws),
+             lambda: dsla.dsla_cache_accept(c.desc, x, gpu([0, 0]), gpu([1, 1]), c.handles, c.ws), lambda: dsla.dsla_qk_rope(rope, q, kv, kv, q),
+             lambda: dsla.dsla_qk_rope(rope, q, kv, kv, q, None, c.desc, x, *c.pools), lambda: dsla.dsla_attention_paged(c.desc, x, q, *c.pools, q, 1.0, 10)]
+
+    class Elsewhere:
+        _cuda_getDevice = staticmethod(lambda: 1)
+        _cuda_getCurrentRawStream = staticmethod(lambda d: 0)
+
+    real = dsla.binding._torch
+    monkeypatch.setattr(dsla.binding, "_torch", Elsewhere)
+    monkeypatch.setattr(dsla.binding, "_native", dsla.binding._General)
+    for call in calls:
+        with pytest.raises(ValueError):
+            call()
+    monkeypatch.setattr(dsla.binding, "_torch", real)
+    c.same()
