@@ -156,13 +156,22 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attention_paged_rows_kerne
             for (int t = 0; t < NH; ++t)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) sc[t][e] = 0.f;
+            // The fragments of keys are asked for kReads products ahead, in an order that is kept: with one ahead, as the compiler has it, every
+            // product waits for its own.
+            constexpr int kReads = 6;
+            bf16x8 kf[kReads];
+            const auto read_k = [&](int i) {   // product i: tile i % NH, features 16 (i / NH) and on
+                kf[i % kReads] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(kb_ + 32 * (half + i % NH) * L::RB + kf_off + 32 * (i / NH ^ kf_s1)));
+            };
 #pragma unroll
-            for (int kb = 0; kb < NKB; ++kb)
+            for (int i = 0; i < kReads; ++i) read_k(i);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int t = 0; t < NH; ++t) {
-                    const bf16x8 kf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(kb_ + 32 * (half + t) * L::RB + kf_off + 32 * (kb ^ kf_s1)));
-                    sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[kb], sc[t], 0, 0, 0);
-                }
+            for (int i = 0; i < NH * NKB; ++i) {
+                sc[i % NH] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % kReads], qf[i / NH], sc[i % NH], 0, 0, 0);
+                if (i + kReads < NH * NKB) read_k(i + kReads);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             float factor = scale;
             if (edge) {   // bits counted from key first: a lane's keys are first + 8 (e / 4) + e % 4
 #pragma unroll
