@@ -450,7 +450,7 @@ DSLA_API dsla_status dsla_cache_truncate(const dsla_cache *cache, const int32_t 
  * start[b], start[b] + 1, ... in every pool, and the sequence is cut behind them.
  *   path       : DEVICE [total]      n_accepted : DEVICE [B], 0 .. tokens of b; negative: entry b stays as it is
  * B * n_pools * H_kv is limited to 2^25 (else DSLA_ERR_SHAPE).  An entry whose path is not ascending or out of range, whose tokens are not the last, or that would change a page which other
- * sequences name, stays as it is and is reported.
+ * sequences name, stays as it is and is reported; of two entries that name one row the first takes part.
  */
 DSLA_API dsla_status dsla_cache_accept(const dsla_cache *cache, const dsla_batch *batch, const int32_t *path, const int32_t *n_accepted,
                                        int32_t n_pools, void *const *pools, void *workspace, size_t workspace_bytes, void *stream);

@@ -116,7 +116,7 @@ class Cache:
             k = int(n_accepted[b])
             if k < 0 or (e is not None and start[b] < 0):
                 continue
-            if e is None or k > e[1] or self.lens[e[2]] != start[b] + e[1]:
+            if e is None or e[2] in [int(r) for r in row[:b]] or k > e[1] or self.lens[e[2]] != start[b] + e[1]:
                 self.status |= ENTRY
                 continue
             a, n, s = e

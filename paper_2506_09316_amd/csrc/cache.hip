@@ -379,7 +379,11 @@ __device__ __forceinline__ int accepted_length(const CacheArgs &c, const BatchAr
 {
     const int start = x.start[b], n = n_accepted[b], lane = threadIdx.x & 63;
     const bool asked = n >= 0 && !(e.ok && start < 0);
-    bool good = asked && e.ok && n <= e.n && static_cast<long long>(start) + e.n <= row_room(c) && c.lens[e.row] == start + e.n;
+    bool again = false;
+    if (x.row)
+        for (int o = lane; o < b; o += 64) again |= x.row[o] == e.row;
+    again = __ballot(again) != 0;
+    bool good = asked && e.ok && !again && n <= e.n && static_cast<long long>(start) + e.n <= row_room(c) && c.lens[e.row] == start + e.n;
     if (good) {
         for (int i = lane; i < n; i += 64) {
             const int p = path[e.cu + i];

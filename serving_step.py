@@ -8,6 +8,7 @@
     python serving_step.py --entropy [--B 8 --T 8192]
     python serving_step.py --attention-decode [--B 8 --T 8192]
     python serving_step.py --attention-prefill [--B 8 --T 8192]
+    python serving_step.py --paged-attention [--layers 16 --B 8 --T 8192 --Hkv 8 --drafted 1 --decode 64]
 
 L layer instances (each with its own blend coefficient and its own pair of states per sequence) prefill a
 prompt of T tokens for B sequences and then decode token by token.  The decode step of all layers is captured
@@ -186,6 +187,87 @@ def attention_decode(B: int, T: int, H: int, d: int):
                       "softmax_attention_frac_of_8TBps": round(cache_bytes / us_attn / 1e3 / 8000, 4),
                       "dsla_decode_us": round(us_dsla, 2), "dsla_state_bytes": B * H * 2 * d * d * 4,
                       "ratio": round(us_attn / us_dsla, 2)}))
+
+
+def paged_attention(L: int, B: int, T: int, H: int, Hkv: int, d: int, drafted: int, steps: int):
+    """The softmax layers of a serving step over a paged cache: room for the tokens of every request, then in every layer norm, rotation,
+    writing and attention; with `drafted` > 1 a tree of that many drafted tokens a request, of which a path is accepted.  B requests of T / 2 to
+    T tokens; eager, and replayed from a graph.  One JSON line."""
+    import time
+    import torch
+    import paper_2506_09316_amd as dsla
+    from paper_2506_09316_amd.binding import DSLA_BF16
+
+    dev = torch.device("cuda:0")
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(20250609)
+    page, n = 64, drafted
+    lens = [T - b * T // (2 * B) for b in range(B)]
+    columns = -(-(T + (steps + 20) * n) // page)
+    n_pages = sum(-(-x // page) for x in lens) + B * (1 + -(-(steps + 20) * n // page))
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device=dev)
+    table, held, refs = (torch.empty(*s, dtype=torch.int32, device=dev) for s in ((B, columns), (B,), (n_pages,)))
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    cache = dsla.make_cache(table, held, refs, page=page, H_kv=Hkv, d=d, dtype=DSLA_BF16, status=status)
+    layers = [[torch.randn(n_pages, Hkv, page, d, device=dev, generator=gen, dtype=torch.bfloat16) for _ in range(2)] for _ in range(L)]
+    pools = dsla.make_pools([t for pair in layers for t in pair])
+    nbytes = dsla.dsla_cache_workspace_bytes(cache, B)
+    prompt = dsla.make_batch(torch.empty(B, dtype=torch.int32, device=dev), sum(lens), cu=ints([0] + [sum(lens[:b + 1]) for b in range(B)]))
+    batch = dsla.make_batch(torch.empty(B, dtype=torch.int32, device=dev), B * n, cu=ints([n * b for b in range(B + 1)]) if n > 1 else None, max_n=n)
+    ws = torch.empty(max(nbytes, dsla.dsla_attention_paged_workspace_bytes(cache, batch, H, T + steps * n)), dtype=torch.uint8, device=dev)
+    dsla.dsla_cache_init(cache)
+    dsla.dsla_cache_extend(cache, prompt, pools, ws)
+    # a tree: node j hangs on node (j - 1) / 2; accepted are the nodes on the way to the last one
+    parent = [-1] + [(j - 1) // 2 for j in range(1, n)]
+    mask, depth = [1], [0]
+    for j in range(1, n):
+        mask.append(mask[parent[j]] | 1 << j)
+        depth.append(depth[parent[j]] + 1)
+    way, j = [], n - 1
+    while j >= 0:
+        way.insert(0, j)
+        j = parent[j]
+    tree = torch.tensor([m - (1 << 64) if m >> 63 else m for m in mask] * B, device=dev) if n > 1 else None
+    path, accepted = ints((way + [0] * (n - len(way))) * B), ints([len(way)] * B)
+    freq = torch.tensor([10000.0 ** (-2 * i / d) for i in range(d // 2)], device=dev)
+    one = torch.ones(d, device=dev)
+    rope = dsla.make_rope(H, Hkv, d, io_dtype=DSLA_BF16, inv_freq=freq, q_weight=one, k_weight=one, offsets=ints(depth * B))
+    q = torch.randn(B * n, H, d, device=dev, generator=gen, dtype=torch.bfloat16)
+    k, v = (torch.randn(B * n, Hkv, d, device=dev, generator=gen, dtype=torch.bfloat16) for _ in range(2))
+    rotated, o = torch.empty_like(q), torch.empty_like(q)
+
+    def step():
+        dsla.dsla_cache_extend(cache, batch, pools, ws)
+        for k_pages, v_pages in layers:
+            dsla.dsla_qk_rope(rope, q, k, v, rotated, None, cache, batch, k_pages, v_pages)
+            dsla.dsla_attention_paged(cache, batch, rotated, k_pages, v_pages, o, d ** -0.5, T + steps * n, tree=tree, workspace=ws)
+        if n > 1:
+            dsla.dsla_cache_accept(cache, batch, path, accepted, pools, ws)
+
+    def timed(run, reps):
+        torch.cuda.synchronize()
+        t = time.perf_counter()
+        for _ in range(reps):
+            run()
+        torch.cuda.synchronize()
+        return (time.perf_counter() - t) / reps * 1e6
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    timed(step, 3)
+    eager = timed(step, steps // 2)
+    timed(graph.replay, 3)
+    replayed = timed(graph.replay, steps - steps // 2)
+    keys = 2 * sum(lens) * Hkv * d * 2 * L
+    print(json.dumps({"workload": f"{L} softmax layers over a paged cache, {B} requests of {T // 2} to {T} tokens, {H} heads on {Hkv} of {d}, {n} tokens each, bf16",
+                      "eager_us": round(eager, 1), "graph_us": round(replayed, 1), "keys_and_values_GBps": round(keys / replayed / 1e3, 1),
+                      "tokens_kept_per_step": len(way) * B, "status": int(status.item())}))
 
 
 def hybrid(n_layers: int, B: int, T: int, H: int, d: int, decode: int):
@@ -414,6 +496,8 @@ def main():
                     help="time the decode step of an unconverted softmax layer against the DSLA decode step instead")
     ap.add_argument("--attention-prefill", action="store_true",
                     help="time the causal softmax prefill of one unconverted layer instead")
+    ap.add_argument("--paged-attention", action="store_true", help="the softmax layers of a step over a paged cache instead")
+    ap.add_argument("--drafted", type=int, default=1, help="--paged-attention: tokens of a request in a step, up to 64 (a tree of drafted ones)")
     ap.add_argument("--entropy", action="store_true", help="time the attention-entropy kernel on one layer's keys instead")
     ap.add_argument("--packed", choices=sorted(MIXES), help="time one packed mixed-length prefill batch instead")
     ap.add_argument("--hybrid", action="store_true",
@@ -422,7 +506,7 @@ def main():
     ap.add_argument("--project", action="store_true", help="time the projection GEMM of one layer and the prefill behind it")
     ap.add_argument("--K", type=int, default=4096, help="--project: model width")
     ap.add_argument("--multi", type=int, default=0, metavar="N", help="time the N-state decode and prefill calls")
-    ap.add_argument("--Hkv", type=int, default=0, help="--multi: key/value heads (default: H)")
+    ap.add_argument("--Hkv", type=int, default=0, help="--multi, --paged-attention: key/value heads (default: H)")
     ap.add_argument("--layers", type=int, default=None)
     ap.add_argument("--B", type=int, default=8)
     ap.add_argument("--T", type=int, default=8192)
@@ -446,6 +530,8 @@ def main():
         return attention_decode(a.B, a.T, a.H, a.d)
     if a.attention_prefill:
         return attention_prefill(a.B, a.T, a.H, a.d)
+    if a.paged_attention:
+        return paged_attention(a.layers, a.B, a.T, a.H, a.Hkv or a.H, a.d, a.drafted, 64 if a.decode == 128 else a.decode)
 
     import torch
     import paper_2506_09316_amd as dsla

@@ -126,6 +126,32 @@ def test_accepted_paths():
     assert c.lens.tolist() == before
 
 
+def test_one_row_named_twice():
+    c = GpuCache(60, 16, 5, 12)   # (a batch has no more entries than the cache has rows)
+    c.extend(c.batch([0, 1, 2], [20, 40, 5]))
+    x = c.batch([1, 0, 1, 1, 2], [4, 4, 4, 9, 2])
+    assert c.extend(x).tolist() == [40, 20, -1, -1, 5] and c.status.item() == 4
+    y = c.batch([1, 0, 1, 1, 2], [4, 4, 4, 4, 2], start=[40, 20, 40, 40, 5])
+    c.accept(y, [1, 3, 0, 0, 0, 0, 0, 0, 2, 0, 0, 0, 0, 0, 0, 0, 1, 0], [2, 0, 1, 0, 1])
+    assert c.lens.tolist() == [20, 42, 6, 0, 0]
+
+
+def test_many_entries():
+    """More entries than a wavefront, than the kernel for few, and than the planning workgroup have lanes; more pages than that kernel takes."""
+    for B, n_pages in ((257, 900), (1030, 4200), (65, 131200)):
+        c = GpuCache(n_pages, 16, B + 3, 4, H_kv=1, n_pools=1)
+        rows = [int(r) for r in np.random.default_rng(B).permutation(B + 3)[:B]]
+        c.extend(c.batch(rows, [(11 * i) % 40 for i in range(B)]))
+        c.fork([rows[0] if s not in rows else -1 for s in range(B + 3)])
+        x = c.batch(rows, [1 + i % 5 for i in range(B)])
+        c.extend(x)
+        path = [j for i in range(B) for j in ([0] if i % 5 == 0 else [1] + [0] * (i % 5))]
+        c.accept(x, path, [1 if i % 3 else 0 for i in range(B)])
+        c.truncate([0 if s % 2 else -1 for s in range(B + 3)])
+        c.compact()
+        c.extend(c.batch(rows))
+
+
 def test_to_the_front():
     c = GpuCache(600, 16, 9, 80, n_pools=3)
     c.extend(c.batch(list(range(9)), [16 * 7 * (i + 1) for i in range(9)]))

@@ -160,6 +160,41 @@ def test_what_takes_no_part():
     assert c.status.item() == 4
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B, n_hi, H, H_kv, d", [(70, 1, 4, 2, 64), (131, 3, 2, 1, 128), (66, 20, 8, 2, 64), (300, 1, 1, 1, 64)])
+def test_many_entries(B, n_hi, H, H_kv, d, dtype):
+    """More entries than a wavefront has lanes, some of no tokens, some that take no part, of short and long sequences."""
+    r = np.random.default_rng(B)
+    counts = [int(r.integers(0, n_hi + 1)) if n_hi > 1 else 1 for _ in range(B)]
+    lens = [n + int(r.integers(0, [5, 60, 900][i % 3])) for i, n in enumerate(counts)]
+    c, x = held(lens, counts, H_kv=H_kv, d=d, page=32, dtype=dtype, seed=B)
+    start = [a - k if i % 7 else -1 for i, (a, k) in enumerate(zip(lens, counts))]
+    c.start(x).copy_(gpu(start))
+    q = values((sum(counts), H, d), dtype, 31)
+    got = f64(attend(c, x, q, 0.1, max(lens)))
+    cu, rows, total = x.plain
+    want, size, reach = orc.attention(c.oracle, f64(c.pools[0]), f64(c.pools[1]), cu, rows, start, f64(q), float(np.float32(0.1)))
+    part = ~np.isnan(want[:, 0, 0])
+    assert (got[~part] == 9).all() and c.status.item() == 0
+    assert_within("o", got[part], want[part], attention_bound(want, size, reach, max(lens), d, dtype)[part])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H, H_kv, n, page", [(8, 1, 24, 16), (4, 1, 64, 32), (2, 2, 3, 16), (16, 1, 1, 64)])
+def test_pages_that_are_none(H, H_kv, n, page, dtype):
+    """The first, the last and pages between: their tokens are not seen, whatever number the table has there."""
+    c, x = held([400, n, 150], [n] * 3, H_kv=H_kv, d=128, page=page, dtype=dtype, seed=40)
+    rows = x.plain[1]
+    t = c.oracle.table
+    t[rows[0], [0, 3, 399 // page]] = [-1, c.oracle.n_pages, 2 ** 31 - 1]
+    t[rows[1], 0] = -2 ** 31                                   # all that it has, where one page holds it
+    c.table.copy_(gpu(t))
+    q = values((3 * n, H, 128), dtype, 41)
+    tree = tree_of([n] * 3, np.random.default_rng(1)) if n > 1 else None
+    got, _ = check(c, x, q, 0.1, 400, tree, dtype)
+    assert c.status.item() == 4 and (page < n or (got[n:2 * n] == 0).all())
+
+
 def test_the_same_again_and_on_another_stream():
     c, x = held([3000, 100, 700], [3, 9, 30], H_kv=2, d=128, page=16, dtype="bf16", seed=15)
     q = values((42, 8, 128), "bf16", 16)

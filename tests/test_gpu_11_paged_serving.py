@@ -229,3 +229,11 @@ def test_another_device_is_refused(monkeypatch):
             call()
     monkeypatch.setattr(dsla.binding, "_torch", real)
     c.same()
+
+
+@pytest.mark.parametrize("drafted", [1, 7])
+def test_the_serving_example_runs(drafted, capsys):
+    import json
+    import serving_step
+    serving_step.paged_attention(2, 3, 200, 4, 2, 64, drafted, 6)
+    assert json.loads(capsys.readouterr().out.splitlines()[-1])["status"] == 0
