@@ -500,7 +500,7 @@ DSLA_API dsla_status dsla_qk_rope(const dsla_rope *rope, int64_t total_rows, con
  *     tree == NULL : i <= j
  *     o_j = sum_{i seen} softmax_i(scale * q_j . k_i) v_i
  * A query that sees nothing gets zeros; a token that a query does not see has no part in its result, whatever it holds.
- *   H       : query heads, a multiple of H_kv; head h reads key/value head h / (H / H_kv)
+ *   H       : query heads, a multiple of H_kv, up to 4096 H_kv; head h reads key/value head h / (H / H_kv)
  *   max_len : an upper bound of the lengths start[b] + n, used for planning only
  *   q, o    : [total][H][d] of the cache's type      tree : DEVICE [total] or NULL
  *   batch->max_n : 1 .. 64; an entry with more tokens is left out and reported.  B * H * max_n * max_pages * page is limited to about

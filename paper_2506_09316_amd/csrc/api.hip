@@ -588,6 +588,7 @@ dsla_status check_attention_paged(const dsla_cache *cache, const dsla_batch *bat
     DSLA_TRY(check_cache(cache));
     DSLA_TRY(check_batch(*cache, batch));
     if (H <= 0 || H % cache->H_kv != 0 || max_len < 0) return DSLA_ERR_SHAPE;
+    if (H / cache->H_kv > 4096) return DSLA_ERR_UNSUPPORTED;
     if (batch->max_n < 1) return DSLA_ERR_SHAPE;
     if (batch->max_n > 64) return DSLA_ERR_UNSUPPORTED;
     if (static_cast<int64_t>(batch->B) * H * batch->max_n > 0x7fffffffLL / 1024 || !attention_paged_fits(*cache, *batch, H)) return DSLA_ERR_SHAPE;

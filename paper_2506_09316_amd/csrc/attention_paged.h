@@ -28,8 +28,10 @@ struct PagedArgs {
     float *sums;           // [2 groups][tile_rows][D]: sums of the parts that the workgroups leave
     float2 *stats;         // [2 groups][tile_rows]: their reference and the sum of their weights
     OpenUnit *open;        // [groups]
-    int H, G, max_n, tile_rows, groups;
+    int H, G, max_n, tile_rows, log2_tile, groups;
+    uint32_t G_inverse;    // 2^32 / G, rounded up
     float scale_log2e;
+    __device__ __forceinline__ int token(int row) const { return G == 1 ? row : static_cast<int>(__umulhi(row, G_inverse)); }   // row / G (G <= 4096, row < 64 G)
 };
 
 // Tiles of kRowsTile rows (attention_paged_rows.hip), 16 bits.
@@ -49,18 +51,23 @@ constexpr int kAhead = 2;
 
 __device__ __forceinline__ bool not_finite(float f) { return (__float_as_uint(f) & 0x7f800000u) == 0x7f800000u; }
 
-// What is needed of an entry; units = 0: it takes no part.  On the line a granule has `weight` places and lies at the first of them; a unit is
+// What is needed of an entry; units = 0: it takes no part.  On the line a granule has 1 << log2_weight places and lies at the first of them; a unit is
 // its granules and kAhead granules' places ahead of them, about what it costs to begin and to end one.
 struct Work {
-    int cu, n, row, start, L, tiles, granules, units, weight;
-    __device__ __forceinline__ int unit() const { return (granules + kAhead) * weight; }
+    int cu, n, row, start, L, tiles, granules, units, log2_weight;
+    __device__ __forceinline__ int unit() const { return (granules + kAhead) << log2_weight; }
     __device__ __forceinline__ int size() const { return units * unit(); }   // (fits: the host refuses what could not)
     // Of the places at .. at + len - 1 of a unit: its first granule there (or the first one behind), and how many.
-    __device__ __forceinline__ int granule(int at) const { return at <= kAhead * weight ? 0 : (at - kAhead * weight + weight - 1) / weight; }
+    __device__ __forceinline__ int granule(int at) const
+    {
+        const int place = at - (kAhead << log2_weight);
+        return place <= 0 ? 0 : (place + (1 << log2_weight) - 1) >> log2_weight;
+    }
+    __device__ __forceinline__ int first() const { return kAhead << log2_weight; }   // the first granule's place in a unit
 };
 __device__ __forceinline__ Work work_of(const PagedArgs &a, int cu, int n, int row, int start)
 {
-    Work w{cu, n, row, start, start + n, (n * a.G + a.tile_rows - 1) / a.tile_rows, 0, 0, a.tile_rows == kRowsTile && n * a.G > kRowsTile / 2 ? 2 : 1};
+    Work w{cu, n, row, start, start + n, (n * a.G + a.tile_rows - 1) >> a.log2_tile, 0, 0, a.tile_rows == kRowsTile && n * a.G > kRowsTile / 2};
     w.granules = (w.L + kGranule - 1) / kGranule;
     w.units = w.tiles * a.c.H_kv;
     return w;
@@ -74,13 +81,23 @@ __device__ __forceinline__ Work read_work(const PagedArgs &a, int b, bool tell)
     return work_of(a, e.cu, live ? e.n : 0, e.row, live ? start : 0);
 }
 
-__device__ __forceinline__ int wave_prefix(int x)   // inclusive
+// The same of an entry that is the whole wavefront's, in scalar registers.
+__device__ __forceinline__ Work read_work_scalar(const PagedArgs &a, int b)
 {
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int y = __shfl_up(x, off);
-        x += static_cast<int>(threadIdx.x & 63) >= off ? y : 0;
-    }
+    const Work w = read_work(a, b, false);
+    return work_of(a, __builtin_amdgcn_readfirstlane(w.cu), __builtin_amdgcn_readfirstlane(w.n), __builtin_amdgcn_readfirstlane(w.row), __builtin_amdgcn_readfirstlane(w.start));
+}
+
+// Inclusive sum over the wavefront: within rows of 16 lanes, then the rows' last lanes handed on.  (Through LDS instead, like the divisions that
+// are multiplications here, it is part of about 1 us in front of the first keys, most of a short call being what happens once.)
+__device__ __forceinline__ int wave_prefix(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // from 1, 2, 4, 8 lanes below
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // lane 15 of a row to the next one
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // lane 31 to the upper half
     return x;
 }
 

@@ -207,17 +207,17 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void attention_paged_
     while (x0 < x1) {
         while (x0 - before >= w.size()) {   // (also over entries that take no part)
             before += w.size();
-            w = read_work(a, ++b, false);
+            w = read_work_scalar(a, ++b);
         }
         // the unit at x0, and the granules of it that are the workgroup's
         const int unit = (x0 - before) / w.unit(), at = x0 - before - unit * w.unit();
         const int len = w.unit() - at < x1 - x0 ? w.unit() - at : x1 - x0;
         const int g0 = w.granule(at), take = w.granule(at + len) - g0;
-        const int tile = unit % w.tiles, kv = unit / w.tiles;
+        const int kv = w.tiles == 1 ? unit : unit / w.tiles, tile = unit - kv * w.tiles;
         if (threadIdx.x == 0 && g0 == 0 && take < w.granules) {
-            const int first = x0 - at + kAhead * w.weight;   // the place of the unit's first granule (the workgroup's)
+            const int first = x0 - at + w.first();   // the place of the unit's first granule (the workgroup's)
             const int rows = w.n * a.G - tile * a.tile_rows;
-            a.open[blockIdx.x] = OpenUnit{take > 0 ? (first + (w.granules - 1) * w.weight) / line.per - static_cast<int>(blockIdx.x) + 1 : 0, w.cu, kv, tile * a.tile_rows, rows < a.tile_rows ? rows : a.tile_rows, {}};
+            a.open[blockIdx.x] = OpenUnit{take > 0 ? (first + ((w.granules - 1) << w.log2_weight)) / line.per - static_cast<int>(blockIdx.x) + 1 : 0, w.cu, kv, tile * a.tile_rows, rows < a.tile_rows ? rows : a.tile_rows, {}};
         }
         x0 += len;
         if (take <= 0) continue;
@@ -227,10 +227,10 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void attention_paged_
         uint64_t mask[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int r = (tile * NT + n) * 16 + i, j = r / a.G;
+            const int r = (tile * NT + n) * 16 + i, j = a.token(r);
             const bool is = j < w.n;
             mask[n] = a.tree ? a.tree[w.cu + (is ? j : 0)] : ~0ull >> (63 - (is ? j : 0));
-            q[n].load(static_cast<const T *>(a.q) + (static_cast<size_t>(w.cu + (is ? j : 0)) * a.H + kv * a.G + r % a.G) * D, lane);
+            q[n].load(static_cast<const T *>(a.q) + (static_cast<size_t>(w.cu + (is ? j : 0)) * a.H + kv * a.G + r - j * a.G) * D, lane);
             if (!is) q[n].zero();
         }
 
@@ -392,10 +392,10 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void attention_paged_
         if (wave != 0) continue;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int r = (tile * NT + n) * 16 + i, j = r / a.G;
+            const int r = (tile * NT + n) * 16 + i, j = a.token(r);
             if (j >= w.n) continue;
             if (take == w.granules) {
-                T *o = static_cast<T *>(a.o) + (static_cast<size_t>(w.cu + j) * a.H + kv * a.G + r % a.G) * D + 4 * g * TF;
+                T *o = static_cast<T *>(a.o) + (static_cast<size_t>(w.cu + j) * a.H + kv * a.G + r - j * a.G) * D + 4 * g * TF;
                 const float inv = z[n] == 0.f ? 0.f : 1.f / z[n];   // (a query that sees nothing: zeros)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
@@ -471,8 +471,8 @@ __global__ __launch_bounds__(256) void attention_paged_merge_kernel(PagedArgs a)
             }
         }
         const float inv = Z == 0.f ? 0.f : 1.f / Z;
-        const int r = open.row + row;
-        T *o = static_cast<T *>(a.o) + (static_cast<size_t>(open.cu + r / a.G) * a.H + open.kv * a.G + r % a.G) * D + 4 * f;
+        const int r = open.row + row, j = a.token(r);
+        T *o = static_cast<T *>(a.o) + (static_cast<size_t>(open.cu + j) * a.H + open.kv * a.G + r - j * a.G) * D + 4 * f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] = from_f32<T>(A[e] * inv);
     }
@@ -562,6 +562,8 @@ hipError_t launch_attention_paged(const dsla_cache &c, const dsla_batch &x, int 
     a.G = H / c.H_kv;
     a.max_n = x.max_n;
     a.tile_rows = p.tile_rows;
+    a.log2_tile = __builtin_ctz(p.tile_rows);
+    a.G_inverse = static_cast<uint32_t>(((1ull << 32) + a.G - 1) / a.G);
     a.groups = p.groups;
     a.scale_log2e = scale * 1.44269504088896341f;
     if (c.dtype == DSLA_BF16) return c.d == 128 ? launch_t<bf16_t, 128>(p, a, stream) : launch_t<bf16_t, 64>(p, a, stream);

@@ -42,9 +42,18 @@ __device__ __forceinline__ void block_landed_barrier(int ahead)
     else loads_landed_barrier();
 }
 
-template <int D>
-__global__ __launch_bounds__(64 * kRowsWaves, 2) void attention_paged_rows_kernel(PagedArgs a)
+// The arguments, to be read anew: kept over a unit's blocks they would take the registers from what the blocks need.
+__device__ __forceinline__ const PagedArgs &arguments()
 {
+    auto at = __builtin_amdgcn_kernarg_segment_ptr();
+    asm("" : "+s"(at));
+    return *(const PagedArgs *)at;
+}
+
+template <int D>
+__global__ __launch_bounds__(64 * kRowsWaves, 2) void attention_paged_rows_kernel(PagedArgs)
+{
+    const PagedArgs &a = arguments();
     using L = AttnTiles<D>;
     constexpr int NKB = D / 16, CT = D / 32;           // contraction blocks over the features; output tiles of 32 features
     constexpr int RPI = 1024 / L::RB;                  // rows that one load of a wavefront fills
@@ -73,6 +82,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attention_paged_rows_kerne
     const uint32_t flip = a.scale_log2e < 0.f ? 0x80008000u : 0u;
 
     while (x0 < x1) {
+        const PagedArgs &a = arguments();
         while (x0 - before >= w.size()) {   // (also over entries that take no part)
             before += w.size();
             w = read_work(a, ++b, false);
@@ -83,9 +93,9 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attention_paged_rows_kerne
         const int g0 = w.granule(at), take = w.granule(at + len) - g0;
         const int tile = unit % w.tiles, kv = unit / w.tiles;
         if (threadIdx.x == 0 && g0 == 0 && take < w.granules) {
-            const int first = x0 - at + kAhead * w.weight;   // the place of the unit's first granule (the workgroup's)
+            const int first = x0 - at + w.first();   // the place of the unit's first granule (the workgroup's)
             const int rows = w.n * a.G - tile * a.tile_rows;
-            a.open[blockIdx.x] = OpenUnit{take > 0 ? (first + (w.granules - 1) * w.weight) / line.per - static_cast<int>(blockIdx.x) + 1 : 0, w.cu, kv, tile * a.tile_rows, rows < a.tile_rows ? rows : a.tile_rows, {}};
+            a.open[blockIdx.x] = OpenUnit{take > 0 ? (first + ((w.granules - 1) << w.log2_weight)) / line.per - static_cast<int>(blockIdx.x) + 1 : 0, w.cu, kv, tile * a.tile_rows, rows < a.tile_rows ? rows : a.tile_rows, {}};
         }
         x0 += len;
         if (take <= 0) continue;
@@ -93,12 +103,12 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attention_paged_rows_kerne
 
         const int live = w.n * a.G - tile * kRowsTile;              // rows
         const bool halves = live <= kRowsTile / 2;                  // (uniform) the first wavefronts the first half of a block's keys, the others the second
-        const int my = halves ? wave & (kRowsWaves / 2 - 1) : wave, r = tile * kRowsTile + 32 * my + ln, j = r / a.G;
+        const int my = halves ? wave & (kRowsWaves / 2 - 1) : wave, r = tile * kRowsTile + 32 * my + ln, j = a.token(r);
         const bool works = 32 * my < live, is = j < w.n;
         const uint64_t mask = a.tree ? a.tree[w.cu + (is ? j : 0)] : ~0ull >> (63 - (is ? j : 0));
         bf16x8 qf[NKB];
         {
-            const bf16_t *q = static_cast<const bf16_t *>(a.q) + (static_cast<size_t>(w.cu + (is ? j : 0)) * a.H + kv * a.G + r % a.G) * D + 8 * g;
+            const bf16_t *q = static_cast<const bf16_t *>(a.q) + (static_cast<size_t>(w.cu + (is ? j : 0)) * a.H + kv * a.G + r - j * a.G) * D + 8 * g;
 #pragma unroll
             for (int kb = 0; kb < NKB; ++kb) {
                 u32x4 u = *reinterpret_cast<const u32x4 *>(q + 16 * kb);
@@ -344,8 +354,13 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attention_paged_rows_kerne
                 for (int e = 0; e < 16; ++e) oacc[ct][e] = c0 * oacc[ct][e] + c1 * s[(2 + 16 * ct + e) * 64];
         }
         if (!is) continue;
+        const PagedArgs &out = arguments();
+        int at_row = lane & 31;
+        asm("" : "+v"(at_row));
+        at_row += tile * kRowsTile + 32 * my;
+        const int at_token = out.token(at_row);
         if (take == w.granules) {
-            uint32_t *o = reinterpret_cast<uint32_t *>(static_cast<bf16_t *>(a.o) + (static_cast<size_t>(w.cu + j) * a.H + kv * a.G + r % a.G) * D + 4 * g);
+            uint32_t *o = reinterpret_cast<uint32_t *>(static_cast<bf16_t *>(out.o) + (static_cast<size_t>(w.cu + at_token) * out.H + kv * out.G + at_row - at_token * out.G) * D + 4 * g);
             const float inv = z == 0.f ? 0.f : 1.f / z;   // (a query that sees nothing: zeros)
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
@@ -355,12 +370,12 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attention_paged_rows_kerne
         } else {
             // a stretch has no more than one unit that began before it (record 0) and one that goes on after it (record 1)
             const size_t rec = (2 * static_cast<size_t>(blockIdx.x) + (g0 == 0)) * kRowsTile + 32 * my + ln;
-            if (g == 0) a.stats[rec] = make_float2(m, z);
+            if (g == 0) out.stats[rec] = make_float2(m, z);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    *reinterpret_cast<f32x4 *>(a.sums + rec * D + 32 * ct + 8 * e + 4 * g) = f32x4{oacc[ct][4 * e], oacc[ct][4 * e + 1], oacc[ct][4 * e + 2], oacc[ct][4 * e + 3]};
+                    *reinterpret_cast<f32x4 *>(out.sums + rec * D + 32 * ct + 8 * e + 4 * g) = f32x4{oacc[ct][4 * e], oacc[ct][4 * e + 1], oacc[ct][4 * e + 2], oacc[ct][4 * e + 3]};
         }
     }
 }

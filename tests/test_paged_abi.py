@@ -124,7 +124,8 @@ def test_attention_arguments(lib):
     assert call(q=None) == call(kp=None) == call(vp=None) == call(o=None) == NULL
     assert call(q=odd) == call(kp=odd) == call(vp=odd) == call(o=odd) == call(tree=ctypes.c_void_p(4100)) == SHAPE
     assert call(total=0, q=None) == OK
-    assert call(c=cache(n_seqs=1 << 20), H=1 << 16, B=1 << 16) == SHAPE
+    assert call(c=cache(n_seqs=1 << 20), H=1 << 15, B=1 << 16) == SHAPE and call(H=8 * 4097) == UNSUPPORTED
+    assert call(c=cache(max_pages=(1 << 24) + 3), B=8, max_n=64) == SHAPE      # places of 64 x 32 rows of up to 2^30 tokens on 8 heads
 
 
 LAUNCHES = r"""
