@@ -41,6 +41,15 @@ hipError_t launch_attention_paged_rows(const PagedArgs &a, ProfileScope &ps, hip
 namespace {
 
 constexpr int kWaves = 4;       // of a workgroup
+
+// The stretch of a workgroup, one of `count` (of one that merges: whose open unit is its): those of one XCD (workgroups go round the 8 of them) lie
+// next to each other, so that the tiles of one head's rows find each other's keys in its L2, and the merge the records.  8 requests of 8192
+// tokens, 64 drafted, 32 heads on 8 of 128: 115 -> 106 us; with one token each neither gains nor loses.
+__device__ __forceinline__ int stretch_of(int count)
+{
+    const int xcd = blockIdx.x % 8, more = count % 8;
+    return xcd * (count / 8) + (xcd < more ? xcd : more) + blockIdx.x / 8;
+}
 // The reference of a query's exponentials is raised only when a score exceeds it by more than this (log2): weights stay below 2^8.
 constexpr float kSlack = 8.f;
 

@@ -197,10 +197,11 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void attention_paged_
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
     const int plog = a.c.page_log2, page = 1 << plog;
-    const Line line = read_line(a, blockIdx.x, -1, blockIdx.x == 0 && wave == 0);
-    if (threadIdx.x == 0) a.open[blockIdx.x].parts = 0;
+    const int stretch = stretch_of(a.groups);
+    const Line line = read_line(a, stretch, -1, blockIdx.x == 0 && wave == 0);
+    if (threadIdx.x == 0) a.open[stretch].parts = 0;
     if (line.total == 0) return;
-    int x0 = line.per * blockIdx.x, before = line.before, b = line.b;   // (no more than the total)
+    int x0 = line.per * stretch, before = line.before, b = line.b;   // (no more than the total)
     const int x1 = line.total - x0 < line.per ? line.total : x0 + line.per;
     Work w = line.w;
 
@@ -217,7 +218,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void attention_paged_
         if (threadIdx.x == 0 && g0 == 0 && take < w.granules) {
             const int first = x0 - at + w.first();   // the place of the unit's first granule (the workgroup's)
             const int rows = w.n * a.G - tile * a.tile_rows;
-            a.open[blockIdx.x] = OpenUnit{take > 0 ? (first + ((w.granules - 1) << w.log2_weight)) / line.per - static_cast<int>(blockIdx.x) + 1 : 0, w.cu, kv, tile * a.tile_rows, rows < a.tile_rows ? rows : a.tile_rows, {}};
+            a.open[stretch] = OpenUnit{take > 0 ? (first + ((w.granules - 1) << w.log2_weight)) / line.per - stretch + 1 : 0, w.cu, kv, tile * a.tile_rows, rows < a.tile_rows ? rows : a.tile_rows, {}};
         }
         x0 += len;
         if (take <= 0) continue;
@@ -403,7 +404,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void attention_paged_
                     for (int t = 0; t < TF; ++t) o[e * TF + t] = from_f32<T>(acc[n][t][e] * inv);
             } else {
                 // a stretch has no more than one unit that began before it (record 0) and one that goes on after it (record 1)
-                const size_t rec = (2 * static_cast<size_t>(blockIdx.x) + (g0 == 0)) * a.tile_rows + n * 16 + i;
+                const size_t rec = (2 * static_cast<size_t>(stretch) + (g0 == 0)) * a.tile_rows + n * 16 + i;
                 if (g == 0) a.stats[rec] = make_float2(m[n], z[n]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
@@ -425,12 +426,13 @@ __global__ __launch_bounds__(256) void attention_paged_merge_kernel(PagedArgs a)
     constexpr int LPR = D / 4, GROUPS = 256 / LPR, U = 4, STEP = SPLIT ? GROUPS : 1;
     __shared__ f32x4 s_part[GROUPS][LPR];
     __shared__ float2 s_stat[GROUPS];
-    const OpenUnit open = a.open[blockIdx.x];
+    const int stretch = stretch_of(a.groups);
+    const OpenUnit open = a.open[stretch];
     const int group = threadIdx.x / LPR, f = threadIdx.x % LPR;
     const int row0 = blockIdx.y * (SPLIT ? 1 : kMergeRows), row1 = row0 + (SPLIT ? 1 : kMergeRows);
     if (open.parts == 0 || row0 >= open.rows) return;
     for (int row = row0 + (SPLIT ? 0 : group); row < (row1 < open.rows ? row1 : open.rows); row += SPLIT ? 1 : GROUPS) {
-        const size_t rec = 2 * static_cast<size_t>(blockIdx.x) * a.tile_rows + row;   // of part p: record 1 of the first workgroup, record 0 of the others
+        const size_t rec = 2 * static_cast<size_t>(stretch) * a.tile_rows + row;   // of part p: record 1 of the first workgroup, record 0 of the others
         float M = -FLT_MAX, Z = 0.f;
         f32x4 A = {0.f, 0.f, 0.f, 0.f};
         for (int p0 = SPLIT ? group : 0; p0 < open.parts; p0 += STEP * U) {   // U records are requested before the first is used

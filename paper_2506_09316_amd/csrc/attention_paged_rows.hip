@@ -63,10 +63,11 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attention_paged_rows_kerne
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, g = lane >> 5;
     const int plog = a.c.page_log2, page = 1 << plog;
-    const Line line = read_line(a, blockIdx.x, -1, blockIdx.x == 0 && wave == 0);
-    if (threadIdx.x == 0) a.open[blockIdx.x].parts = 0;
+    const int stretch = stretch_of(a.groups);
+    const Line line = read_line(a, stretch, -1, blockIdx.x == 0 && wave == 0);
+    if (threadIdx.x == 0) a.open[stretch].parts = 0;
     if (line.total == 0) return;
-    int x0 = line.per * blockIdx.x, before = line.before, b = line.b;   // (no more than the total)
+    int x0 = line.per * stretch, before = line.before, b = line.b;   // (no more than the total)
     const int x1 = line.total - x0 < line.per ? line.total : x0 + line.per;
     Work w = line.w;
 
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attention_paged_rows_kerne
         if (threadIdx.x == 0 && g0 == 0 && take < w.granules) {
             const int first = x0 - at + w.first();   // the place of the unit's first granule (the workgroup's)
             const int rows = w.n * a.G - tile * a.tile_rows;
-            a.open[blockIdx.x] = OpenUnit{take > 0 ? (first + ((w.granules - 1) << w.log2_weight)) / line.per - static_cast<int>(blockIdx.x) + 1 : 0, w.cu, kv, tile * a.tile_rows, rows < a.tile_rows ? rows : a.tile_rows, {}};
+            a.open[stretch] = OpenUnit{take > 0 ? (first + ((w.granules - 1) << w.log2_weight)) / line.per - stretch + 1 : 0, w.cu, kv, tile * a.tile_rows, rows < a.tile_rows ? rows : a.tile_rows, {}};
         }
         x0 += len;
         if (take <= 0) continue;
@@ -369,7 +370,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attention_paged_rows_kerne
                     *reinterpret_cast<u32x2 *>(o + 16 * ct + 4 * e) = u32x2{pack2(oacc[ct][4 * e] * inv, oacc[ct][4 * e + 1] * inv), pack2(oacc[ct][4 * e + 2] * inv, oacc[ct][4 * e + 3] * inv)};
         } else {
             // a stretch has no more than one unit that began before it (record 0) and one that goes on after it (record 1)
-            const size_t rec = (2 * static_cast<size_t>(blockIdx.x) + (g0 == 0)) * kRowsTile + 32 * my + ln;
+            const size_t rec = (2 * static_cast<size_t>(stretch) + (g0 == 0)) * kRowsTile + 32 * my + ln;
             if (g == 0) out.stats[rec] = make_float2(m, z);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
