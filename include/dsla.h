@@ -424,8 +424,8 @@ DSLA_API dsla_status dsla_cache_init(const dsla_cache *cache, void *stream);
 
 /*
  * dsla_cache_extend - makes room for the tokens of every entry at the end of its sequence: start[b] = lens[row], lens[row] +=
- * the tokens of b, and pages for them.  A last page that is not full and that other sequences name too is first replaced by a
- * page of its own, to which the rows that the sequence has in it are copied in every pool.  Entries are served in order; those
+ * the tokens of b, and pages for them.  A last page that is not full and that, as the call finds it, other sequences name too is
+ * first replaced by a page of its own, to which the rows that the sequence has in it are copied in every pool.  Entries are served in order; those
  * that the free pages do not reach, and all later ones that need pages, stay as they are: start[b] = -1, reported as
  * DSLA_STATUS_CACHE_FULL.  Of two entries that name one row the first takes part.
  */
@@ -499,7 +499,8 @@ DSLA_API dsla_status dsla_qk_rope(const dsla_rope *rope, int64_t total_rows, con
  *     tree != NULL : those with bit i of tree[cu[b] + j] set (a tree of drafted tokens: a node's ancestors and itself)
  *     tree == NULL : i <= j
  *     o_j = sum_{i seen} softmax_i(scale * q_j . k_i) v_i
- * A query that sees nothing gets zeros; a token that a query does not see has no part in its result, whatever it holds.
+ * A query that sees nothing gets zeros; a token that a query does not see has no part in its result, whatever it holds.  A score
+ * of -inf weighs nothing (all of them: zeros); +inf and NaN among what a query sees reach its result as the formula has it.
  *   H       : query heads, a multiple of H_kv, up to 4096 H_kv; head h reads key/value head h / (H / H_kv)
  *   max_len : an upper bound of the lengths start[b] + n, used for planning only
  *   q, o    : [total][H][d] of the cache's type      tree : DEVICE [total] or NULL
@@ -507,6 +508,7 @@ DSLA_API dsla_status dsla_qk_rope(const dsla_rope *rope, int64_t total_rows, con
  *             10^12 (else DSLA_ERR_SHAPE)
  * Tokens of a page that the table gives no valid number for are not seen (reported).
  * io bf16: bf16 operands on MFMA, fp32 accumulation and softmax statistics; io f32: fp32 throughout.
+ * workspace: 16-byte aligned; calls that may overlap, also replayed ones, need buffers of their own.
  */
 DSLA_API size_t dsla_attention_paged_workspace_bytes(const dsla_cache *cache, const dsla_batch *batch, int32_t H, int64_t max_len);
 DSLA_API dsla_status dsla_attention_paged(const dsla_cache *cache, const dsla_batch *batch, int32_t H, int64_t max_len, float scale,
