@@ -20,7 +20,7 @@ namespace dsla {
 namespace {
 
 // 16 bytes a lane from `base` (uniform) + `voff` (per lane) into LDS at `lds` (uniform) + 16 * lane.  The compiler does not know these
-// loads: whoever reads the bytes waits with block_landed_barrier() first.  (The five states in front are what a vector memory
+// loads: whoever reads the bytes waits with loads_landed_barrier() first.  (The five states in front are what a vector memory
 // instruction needs behind a vector instruction that wrote its scalar address.)
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
@@ -34,17 +34,6 @@ __device__ __forceinline__ void page_to_lds16(const char *lds, uint32_t voff, co
 #pragma clang diagnostic pop
 
 constexpr int kRowsWaves = kRowsTile / 32;
-constexpr int kBuffers = 2, kAheadBlocks = kBuffers - 1;
-
-// Waits until no more than `ahead` blocks' loads of this wavefront are on their way (`loads` each), then for the others.
-template <int LOADS>
-__device__ __forceinline__ void block_landed_barrier(int ahead)
-{
-    static_assert(kAheadBlocks == 3 || kAheadBlocks == 1);
-    if (kAheadBlocks > 2 && ahead >= 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS) : "memory");
-    else if (kAheadBlocks > 1 && ahead == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
-    else loads_landed_barrier();
-}
 
 // The arguments, to be read anew: kept over a unit's blocks they would take the registers from what the blocks need.
 __device__ __forceinline__ const PagedArgs &arguments()
@@ -62,7 +51,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attention_paged_rows_kerne
     constexpr int NKB = D / 16, CT = D / 32;           // contraction blocks over the features; output tiles of 32 features
     constexpr int RPI = 1024 / L::RB;                  // rows that one load of a wavefront fills
     constexpr int NI = kKeys / RPI / kRowsWaves;          // loads of a wavefront for a block's keys
-    __shared__ __attribute__((aligned(1024))) char buf[kBuffers * L::BUF_BYTES];
+    __shared__ __attribute__((aligned(1024))) char buf[2 * L::BUF_BYTES];
     __shared__ int s_wild;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, g = lane >> 5;
@@ -324,15 +313,14 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attention_paged_rows_kerne
             else products(std::integral_constant<int, 2>(), kb_, vb_, t0, gap, edge, wild, 0);
         };
 
-        // Block n lives in buffer n % kBuffers; its loads are issued kAheadBlocks blocks ahead, right after the barrier that frees the buffer.
+        // Block n lives in buffer n % 2; its loads are issued one block ahead, right after the barrier that frees the buffer.  (Its lines asked for
+        // yet a block earlier, so that the loads find them in the L2: 106 -> 118 us; what bounds the loop is not their latency.)
         const int blocks = (to - from + kKeys - 1) / kKeys;
-        int gaps = 0;   // four bits of each block that is staged
-        for (int n = 0; n < (blocks < kAheadBlocks ? blocks : kAheadBlocks); ++n) gaps |= stage(buf + n * L::BUF_BYTES, from + n * kKeys) << 4 * n;
+        int gaps = stage(buf, from);   // four bits of each block that is staged
         for (int n = 0; n < blocks; ++n) {
-            const int ahead = blocks - 1 - n;
-            block_landed_barrier<2 * NI>(ahead);   // the block is there; every wavefront is done with the one before
-            if (ahead >= kAheadBlocks) gaps |= stage(buf + (n + kAheadBlocks) % kBuffers * L::BUF_BYTES, from + (n + kAheadBlocks) * kKeys) << 4 * kAheadBlocks;
-            compute(buf + n % kBuffers * L::BUF_BYTES, from + n * kKeys, gaps & 15);
+            loads_landed_barrier();   // the block is there; every wavefront is done with the one before
+            if (n + 1 < blocks) gaps |= stage(buf + (n + 1) % 2 * L::BUF_BYTES, from + (n + 1) * kKeys) << 4;
+            compute(buf + n % 2 * L::BUF_BYTES, from + n * kKeys, gaps & 15);
             gaps >>= 4;
         }
 
