@@ -197,8 +197,8 @@ hipError_t launch_qk_rope(const dsla_rope &r, int64_t rows, const void *q, const
     auto kernel = bf16 ? (r.d == 128 ? qk_rope_kernel<128, bf16_t> : qk_rope_kernel<64, bf16_t>)
                        : (r.d == 128 ? qk_rope_kernel<128, float> : qk_rope_kernel<64, float>);
     // A workgroup to a token: what it reads of the token is uniform and read before anything is written, by scalar loads (in a loop over
-    // tokens these are vector loads: 16000 tokens 94 us instead of 78).  Where there are few, one to every chunk of a token's heads (48 heads of 128, with chunks /
-    // without: 1 token 3.5 / 4.0 us, 64 4.3 / 5.1, 512 5.4 / 5.8, 1024 9.1 / 8.2).
+    // tokens these are vector loads: 16000 tokens 94 us instead of 78).  Where there are few, one to every chunk of a token's heads (48 heads of
+    // 128, with chunks / without: 1 token 3.5 / 4.0 us, 64 4.3 / 5.1, 512 5.4 / 5.8, 1024 9.1 / 8.2).
     const int heads = r.H + r.H_kv + (c ? r.H_kv : 0), at_a_time = 256 / (r.d / 16);
     const unsigned chunks = rows <= 512 ? (heads + at_a_time - 1) / at_a_time : 1;
     constexpr int64_t kMost = 1 << 23;   // threads of a launch are a 32-bit number
