@@ -112,13 +112,13 @@ __device__ __forceinline__ int wave_prefix(int x)
     return x;
 }
 
-// The line as every wavefront finds it for itself: how much there is of it and a workgroup takes, and one entry on it with what lies
-// ahead of it: the one that the stretch of workgroup `group` begins in, or (find >= 0) entry `find`.
+// The line as every wavefront finds it for itself: how much there is of it and a workgroup takes, and the entry that a stretch begins in, with what
+// lies ahead of it.
 struct Line {
     int total, per, b, before;
     Work w;
 };
-__device__ __forceinline__ Line read_line(const PagedArgs &a, int group, int find, bool tell)
+__device__ __forceinline__ Line read_line(const PagedArgs &a, int stretch, bool tell)
 {
     const int lane = threadIdx.x & 63;
     Line l;
@@ -131,11 +131,11 @@ __device__ __forceinline__ Line read_line(const PagedArgs &a, int group, int fin
     }
     l.per = (l.total + a.groups - 1) / a.groups;
     if (l.per < (a.tile_rows == kRowsTile ? 2 : 1)) l.per = a.tile_rows == kRowsTile ? 2 : 1;   // (a granule's places: no stretch inside a unit without one)
-    const long long x = static_cast<long long>(l.per) * group;
+    const long long x = static_cast<long long>(l.per) * stretch;
     int ahead = 0;
     l.b = l.before = 0;
     for (int b0 = 0;;) {
-        const unsigned long long hit = __ballot(find >= 0 ? b0 + lane == find : (x >= ahead + sum - n) & (x < ahead + sum));
+        const unsigned long long hit = __ballot((x >= ahead + sum - n) & (x < ahead + sum));
         if (hit) {
             const int at = __builtin_ctzll(hit);
             l.b = b0 + at;

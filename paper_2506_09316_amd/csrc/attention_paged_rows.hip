@@ -57,7 +57,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attention_paged_rows_kerne
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, g = lane >> 5;
     const int plog = a.c.page_log2, page = 1 << plog;
     const int stretch = stretch_of(a.groups);
-    const Line line = read_line(a, stretch, -1, blockIdx.x == 0 && wave == 0);
+    const Line line = read_line(a, stretch, blockIdx.x == 0 && wave == 0);
     if (threadIdx.x == 0) a.open[stretch].parts = 0;
     if (line.total == 0) return;
     int x0 = line.per * stretch, before = line.before, b = line.b;   // (no more than the total)
