@@ -504,8 +504,9 @@ DSLA_API dsla_status dsla_qk_rope(const dsla_rope *rope, int64_t total_rows, con
  *   H       : query heads, a multiple of H_kv, up to 4096 H_kv; head h reads key/value head h / (H / H_kv)
  *   max_len : an upper bound of the lengths start[b] + n, used for planning only
  *   q, o    : [total][H][d] of the cache's type      tree : DEVICE [total] or NULL
- *   batch->max_n : 1 .. 64; an entry with more tokens is left out and reported.  B * H * max_n * max_pages * page is limited to about
- *             10^12 (else DSLA_ERR_SHAPE)
+ *   batch->max_n : 1 .. 64; an entry with more tokens is left out and reported
+ * The work of a call is numbered in 32 bits: B * H_kv * ceil(r / t) * (max_pages * page / 128 + 3) has to be below 10^9 (else DSLA_ERR_SHAPE),
+ * r = max_n * H / H_kv rows in tiles of t = 16 for r <= 16, 32 for r <= 32, beyond that 128 (io bf16) or 64 (io f32).
  * Tokens of a page that the table gives no valid number for are not seen (reported).
  * io bf16: bf16 operands on MFMA, fp32 accumulation and softmax statistics; io f32: fp32 throughout.
  * workspace: 16-byte aligned; calls that may overlap, also replayed ones, need buffers of their own.

@@ -591,8 +591,7 @@ dsla_status check_attention_paged(const dsla_cache *cache, const dsla_batch *bat
     if (H / cache->H_kv > 4096) return DSLA_ERR_UNSUPPORTED;
     if (batch->max_n < 1) return DSLA_ERR_SHAPE;
     if (batch->max_n > 64) return DSLA_ERR_UNSUPPORTED;
-    if (static_cast<int64_t>(batch->B) * H * batch->max_n > 0x7fffffffLL / 1024 || !attention_paged_fits(*cache, *batch, H)) return DSLA_ERR_SHAPE;
-    return DSLA_OK;
+    return attention_paged_fits(*cache, *batch, H) ? DSLA_OK : DSLA_ERR_SHAPE;
 }
 }  // namespace
 

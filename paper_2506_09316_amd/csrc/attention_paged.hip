@@ -542,6 +542,7 @@ hipError_t launch_t(const PagedPlan &p, const PagedArgs &a, hipStream_t stream)
 
 }  // namespace
 
+// The line's places, two to a granule in the kernel for many rows, are 32-bit numbers.
 bool attention_paged_fits(const dsla_cache &c, const dsla_batch &x, int H)
 {
     const int64_t rows = static_cast<int64_t>(x.max_n) * (H / c.H_kv), room = static_cast<int64_t>(c.max_pages) * c.page;
