@@ -427,7 +427,7 @@ DSLA_API dsla_status dsla_cache_init(const dsla_cache *cache, void *stream);
  * the tokens of b, and pages for them.  A last page that is not full and that, as the call finds it, other sequences name too is
  * first replaced by a page of its own, to which the rows that the sequence has in it are copied in every pool.  Entries are served in order; those
  * that the free pages do not reach, and all later ones that need pages, stay as they are: start[b] = -1, reported as
- * DSLA_STATUS_CACHE_FULL.  Of two entries that name one row the first takes part.
+ * DSLA_STATUS_CACHE_FULL.  Of two entries that name one row the first takes part (one that is out of range does not count).
  */
 DSLA_API dsla_status dsla_cache_extend(const dsla_cache *cache, const dsla_batch *batch, int32_t n_pools, void *const *pools,
                                        void *workspace, size_t workspace_bytes, void *stream);
@@ -450,7 +450,8 @@ DSLA_API dsla_status dsla_cache_truncate(const dsla_cache *cache, const int32_t 
  * start[b], start[b] + 1, ... in every pool, and the sequence is cut behind them.
  *   path       : DEVICE [total]      n_accepted : DEVICE [B], 0 .. tokens of b; negative: entry b stays as it is
  * B * n_pools * H_kv is limited to 2^25 (else DSLA_ERR_SHAPE).  An entry whose path is not ascending or out of range, whose tokens are not the last, or that would change a page which other
- * sequences name, stays as it is and is reported; of two entries that name one row the first takes part.
+ * sequences name, stays as it is and is reported; of two entries that name one row the first takes part (one that is out of range, or that
+ * start[b] < 0 keeps out, does not count).
  */
 DSLA_API dsla_status dsla_cache_accept(const dsla_cache *cache, const dsla_batch *batch, const int32_t *path, const int32_t *n_accepted,
                                        int32_t n_pools, void *const *pools, void *workspace, size_t workspace_bytes, void *stream);

@@ -111,12 +111,13 @@ class Cache:
             self.lens[s] = self.lens[f]
 
     def accept(self, cu, row, total, start, path, n_accepted):
-        todo = []
-        for b, e in enumerate(self.entries(cu, row, total)):
+        todo, entries = [], self.entries(cu, row, total)
+        takes_part = [e is not None and start[b] >= 0 for b, e in enumerate(entries)]
+        for b, e in enumerate(entries):
             k = int(n_accepted[b])
             if k < 0 or (e is not None and start[b] < 0):
                 continue
-            if e is None or e[2] in [int(r) for r in row[:b]] or k > e[1] or self.lens[e[2]] != start[b] + e[1]:
+            if e is None or e[2] in [int(r) for r, part in zip(row[:b], takes_part) if part] or k > e[1] or self.lens[e[2]] != start[b] + e[1]:
                 self.status |= ENTRY
                 continue
             a, n, s = e

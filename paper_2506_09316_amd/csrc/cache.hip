@@ -381,7 +381,8 @@ __device__ __forceinline__ int accepted_length(const CacheArgs &c, const BatchAr
     const bool asked = n >= 0 && !(e.ok && start < 0);
     bool again = false;
     if (x.row)
-        for (int o = lane; o < b; o += 64) again |= x.row[o] == e.row;
+        for (int o = lane; o < b; o += 64)
+            if (x.row[o] == e.row && x.start[o] >= 0) again |= read_entry(x, c, o).ok;
     again = __ballot(again) != 0;
     bool good = asked && e.ok && !again && n <= e.n && static_cast<long long>(start) + e.n <= row_room(c) && c.lens[e.row] == start + e.n;
     if (good) {
