@@ -509,7 +509,8 @@ DSLA_API dsla_status dsla_qk_rope(const dsla_rope *rope, int64_t total_rows, con
  * The work of a call is numbered in 32 bits: B * H_kv * ceil(r / t) * (max_pages * page / 128 + 3) has to be below 10^9 (else DSLA_ERR_SHAPE),
  * r = max_n * H / H_kv rows in tiles of t = 16 for r <= 16, 32 for r <= 32, beyond that 128 (io bf16) or 64 (io f32).
  * Tokens of a page that the table gives no valid number for are not seen (reported).
- * io bf16: bf16 operands on MFMA, fp32 accumulation and softmax statistics; io f32: fp32 throughout.
+ * io bf16: bf16 operands on MFMA, fp32 accumulation and softmax statistics; the weights of the second product keep 2^-15 of themselves up to
+ * max_n * H / H_kv = 16 rows, such as single tokens, and are rounded to bf16 (2^-8) beyond; io f32: fp32 throughout.
  * workspace: 16-byte aligned; calls that may overlap, also replayed ones, need buffers of their own.
  */
 DSLA_API size_t dsla_attention_paged_workspace_bytes(const dsla_cache *cache, const dsla_batch *batch, int32_t H, int64_t max_len);

@@ -11,7 +11,7 @@
 // loads hold all that it needs: in 32 bits as they are, in 16 bits after exchanging halves between the registers of two keys.
 //
 // Bound by reading: 64 requests of 100 to 8192 tokens, one token each, 32 heads on 8 of 128 in 16 bits, 492 MB in 84 us (5.9 TB/s), one of
-// 131072 tokens 537 MB in 88 us (6.1 TB/s; non-temporal loads made 93 of 120).  A short call is bound by what happens once: one request of
+// 131072 tokens 537 MB in 89 us (6.0 TB/s; non-temporal loads made 93 of 120).  A short call is bound by what happens once: one request of
 // 1000 tokens, 32 heads of 128, 11.5 us, of which 9.7 are the first kernel's.
 #include "attention_paged.h"
 
@@ -102,20 +102,36 @@ struct Block<bf16_t, D> {
         }
         return r;
     }
-    // The weights are rounded to 16 bits for the second product, by at most 2^-8 of each; their sum is that of the rounded ones, so that
-    // what the roundings have in common (weights that are nearly alike) cancels.
+    // With SPLIT the second product takes a weight in two parts of 16 bits, its upper bits and the rest of p (1 + 2^-20), which keeps it to 2^-15; without,
+    // it is rounded, by at most 2^-8.  The sum is that of the parts as they are, so that what the roundings have in common (weights that are
+    // nearly alike) cancels; neither part of a weight is zero or negative, so an infinite value reaches its sum as what it is.  A tile of 16 rows
+    // is bound by reading and splits, rounded / split (us, 32 heads on 8 of 128): 64 requests of 100 to 8192 tokens 83.7 / 83.9, one of
+    // 131072 88.6 / 89.0, one of 1000, 32 heads, 11.3 / 11.5 (11.6 with the rest on the chain of z).  Two tiles do not: 32 requests of 2000,
+    // 8 tokens each, 46.3 / 47.6, in heads of 64 27.9 / 29.9.
+    template <bool SPLIT>
     static __device__ __forceinline__ void accumulate(const Operand &v, const float (&p)[SLOTS], float &z, f32x4 (&acc)[TF])
     {
-        bf16x8 b;
-#pragma unroll
-        for (int j = 0; j < SLOTS; ++j) b[j] = static_cast<__bf16>(p[j]);
+        const bf16x2 one = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
+        u32x4 upper, rest;
+        float zr = 0.f;
 #pragma unroll
         for (int j = 0; j < SLOTS; j += 2) {
-            const bf16x2 one = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)}, two = {b[j], b[j + 1]};
-            z = __builtin_amdgcn_fdot2_f32_bf16(two, one, z, false);
+            const uint32_t a = __float_as_uint(p[j]), b = __float_as_uint(p[j + 1]), u = SPLIT ? __builtin_amdgcn_perm(b, a, 0x07060302u) : pack2(p[j], p[j + 1]);
+            z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, u), one, z, false);
+            upper[j / 2] = u;
+            if (SPLIT) {
+                const uint32_t r = pack2(fmaf(p[j], 1.f + 0x1p-20f, -__uint_as_float(a & 0xffff0000u)), fmaf(p[j + 1], 1.f + 0x1p-20f, -__uint_as_float(b & 0xffff0000u)));
+                zr = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, r), one, zr, false);
+                rest[j / 2] = r;
+            }
         }
 #pragma unroll
-        for (int t = 0; t < TF; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.a[t], b, acc[t], 0, 0, 0);
+        for (int t = 0; t < TF; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.a[t], __builtin_bit_cast(bf16x8, upper), acc[t], 0, 0, 0);
+        if (SPLIT) {
+            z += zr;
+#pragma unroll
+            for (int t = 0; t < TF; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.a[t], __builtin_bit_cast(bf16x8, rest), acc[t], 0, 0, 0);
+        }
     }
 };
 
@@ -180,6 +196,7 @@ struct Block<float, D> {
     }
     typedef Block<float, D> Operand;
     __device__ __forceinline__ const Operand &operand() const { return *this; }
+    template <bool>
     static __device__ __forceinline__ void accumulate(const Operand &b, const float (&p)[SLOTS], float &z, f32x4 (&acc)[TF])
     {
 #pragma unroll
@@ -361,7 +378,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void attention_paged_
             }
             const auto &v = x.operand();
 #pragma unroll
-            for (int n = 0; n < NT; ++n) B::accumulate(v, p[n], z[n], acc[n]);
+            for (int n = 0; n < NT; ++n) B::template accumulate<NT == 1>(v, p[n], z[n], acc[n]);
         }
 
         // the sums of a query's four lanes; then wavefronts 2 and 3 into 0 and 1, and 1 into 0
