@@ -512,9 +512,11 @@ def main():
     ap.add_argument("--T", type=int, default=8192)
     ap.add_argument("--H", type=int, default=32)
     ap.add_argument("--d", type=int, default=128)
-    ap.add_argument("--decode", type=int, default=128)
+    ap.add_argument("--decode", type=int, default=None, help="steps (default: 128, --paged-attention 64)")
     ap.add_argument("--repeat", type=int, default=5, help="timed repetitions of the prefill of all layers")
     a = ap.parse_args()
+    if a.decode is None:
+        a.decode = 64 if a.paged_attention else 128
     if a.project:
         return project(16384 if a.T == 8192 else a.T, a.K, a.H, a.d)
     if a.multi:
@@ -531,7 +533,7 @@ def main():
     if a.attention_prefill:
         return attention_prefill(a.B, a.T, a.H, a.d)
     if a.paged_attention:
-        return paged_attention(a.layers, a.B, a.T, a.H, a.Hkv or a.H, a.d, a.drafted, 64 if a.decode == 128 else a.decode)
+        return paged_attention(a.layers, a.B, a.T, a.H, a.Hkv or a.H, a.d, a.drafted, a.decode)
 
     import torch
     import paper_2506_09316_amd as dsla

@@ -1,0 +1,19 @@
+"""The arguments of serving_step.py's measurements of the paged cache."""
+import sys
+
+import pytest
+
+import serving_step
+
+
+@pytest.mark.parametrize("given, steps", [([], 64), (["--decode", "128"], 128), (["--decode", "1"], 1), (["--decode", "30"], 30)])
+def test_steps_as_asked_for(monkeypatch, given, steps):
+    seen = []
+    monkeypatch.setattr(serving_step, "paged_attention", lambda *a: seen.append(a))
+    monkeypatch.setattr(sys, "argv", ["serving_step.py", "--paged-attention", *given])
+    serving_step.main()
+    assert seen == [(16, 8, 8192, 32, 32, 128, 1, steps)]
+    monkeypatch.setattr(serving_step, "hybrid", lambda *a: seen.append(a))
+    monkeypatch.setattr(sys, "argv", ["serving_step.py", "--hybrid", *given])
+    serving_step.main()
+    assert seen[1][-1] == (int(given[1]) if given else 128)
