@@ -261,7 +261,7 @@ def paged_attention(L: int, B: int, T: int, H: int, Hkv: int, d: int, drafted: i
     with torch.cuda.graph(graph):
         step()
     timed(step, 3)
-    eager = timed(step, steps // 2)
+    eager = timed(step, max(1, steps // 2))
     timed(graph.replay, 3)
     replayed = timed(graph.replay, steps - steps // 2)
     keys = 2 * sum(lens) * Hkv * d * 2 * L
