@@ -501,7 +501,8 @@ DSLA_API dsla_status dsla_qk_rope(const dsla_rope *rope, int64_t total_rows, con
  *     tree == NULL : i <= j
  *     o_j = sum_{i seen} softmax_i(scale * q_j . k_i) v_i
  * A query that sees nothing gets zeros; a token that a query does not see has no part in its result, whatever it holds.  A score
- * of -inf weighs nothing (all of them: zeros); +inf and NaN among what a query sees reach its result as the formula has it.
+ * of -inf weighs nothing (all of them: zeros); +inf and NaN among what a query sees reach its result as the formula has it, but that a
+ * weight below 2^-100 of the largest may count as zero, which makes NaN of an infinite value.
  *   H       : query heads, a multiple of H_kv, up to 4096 H_kv; head h reads key/value head h / (H / H_kv)
  *   max_len : an upper bound of the lengths start[b] + n, used for planning only
  *   q, o    : [total][H][d] of the cache's type      tree : DEVICE [total] or NULL

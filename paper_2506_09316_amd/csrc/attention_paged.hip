@@ -11,8 +11,9 @@
 // loads hold all that it needs: in 32 bits as they are, in 16 bits after exchanging halves between the registers of two keys.
 //
 // Bound by reading: 64 requests of 100 to 8192 tokens, one token each, 32 heads on 8 of 128 in 16 bits, 492 MB in 84 us (5.9 TB/s), one of
-// 131072 tokens 537 MB in 89 us (6.0 TB/s; non-temporal loads made 93 of 120).  A short call is bound by what happens once: one request of
-// 1000 tokens, 32 heads of 128, 11.5 us, of which 9.7 are the first kernel's.
+// 131072 tokens 537 MB in 89 us (6.0 TB/s; non-temporal loads made 93 of 120).  A short call is bound by what happens once, one wait after
+// another (entries, queries, numbers of pages, keys) and code that is fetched: one request of 1000 tokens, 32 heads of 128, 11.5 us, the
+// first kernel 9.8 in a profile.
 #include "attention_paged.h"
 
 namespace dsla {

@@ -63,8 +63,9 @@ __device__ __forceinline__ void wave_pages(int n_pages, int idle, int *from, int
     *from = wave < 0 ? 0 : static_cast<int>(a < n_pages ? a : n_pages);
     *to = wave < 0 ? 0 : static_cast<int>(b < n_pages ? b : n_pages);
 }
-// f(first page, the reference count of page first + lane or -1 past the end) for 64 pages after 64, kBatch loads at a time; until f
-// returns false.  (One at a time: 20000 pages 4 us.)
+// f(first page, the reference count of page first + lane or -1 past the end) for 64 pages after 64; until f returns false.  The loads of kBatch
+// of them stand together, but each is conditional and the compiler waits for each in its branch: one is in flight, and long pools are bound by
+// that (64 new pages, the last ones of 20000 / 131072 / 2^20: 14 / 55 / 414 us, events around the launch, of which about 4 are there without any work).
 constexpr int kBatch = 4;
 template <class F>
 __device__ __forceinline__ void each_page(const int32_t *refs, int from, int to, F &&f)
@@ -214,7 +215,8 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(CacheArgs c,
     if (tid == 0) *n_moves = s_moves;
 }
 
-// The same for up to kFew entries and kFewPages pages, as decoding has them: bound by the chain of dependent reads, which is cut short.  The
+// The same for up to kFew entries and kFewPages pages, as decoding has them: bound by the chain of dependent reads, which is cut short, and by the
+// scan of the counts.  The
 // first wavefronts look at the entries while the others look for free pages (once: which are free stays in LDS as bits), an
 // entry's thread keeps what it read, and one that names a row again finds out by looking at the rows of those ahead.  The kernel above
 // and this one (us): 64 requests of which some need one of 20000 pages 9.2 / 8.7, 56 branches that all copy 10.4 / 8.2, 16 requests of up
@@ -329,7 +331,8 @@ __global__ __launch_bounds__(1024) void cache_copy_kernel(const Move *moves, con
     }
 }
 
-// A sequence is cut to `keep` tokens: by one wavefront.  (Ends, forks and cuts are a launch and two dependent reads: 2 to 5 us.)
+// A sequence is cut to `keep` tokens: by one wavefront, which waits for the numbers of 64 pages before it asks for the next.  (Ends, forks and cuts of up
+// to some hundred pages are a launch and two dependent reads, 2 to 5 us; rows of 8192 pages are ended or forked in 42.)
 __device__ __forceinline__ void cut_row(const CacheArgs &c, int row, int len, int keep)
 {
     const int have = pages_of(len, c.page_log2);
