@@ -7,7 +7,7 @@
 // 32 of them and take half of the keys of a block each.
 //
 // Bound by the vector and matrix instructions, which overlap as far as the two workgroups of a compute unit are at different steps: 8 requests
-// of 8192 tokens, 64 drafted, 32 heads on 8 of 128, 106 us for 68.7 GFLOP (650 TFLOP/s; 6.9 vector instructions to a matrix one, matrix pipes
+// of 8192 tokens, 64 drafted, 32 heads on 8 of 128, 106 to 110 us for 68.7 GFLOP (640 TFLOP/s; 6.9 vector instructions to a matrix one, matrix pipes
 // busy a third of the cycles, 274 MB read), of which 10 to 17 are the merge of 38 MB of records.  For heads of 128 all 256 vector registers are taken and
 // two more lie in scratch memory.
 //
