@@ -412,7 +412,8 @@ typedef struct {
     int32_t *start;      /* DEVICE [B]                                                                             */
 } dsla_batch;
 
-/* Pools that a call works on: HOST array [n_pools] of DEVICE pointers, 0 <= n_pools <= DSLA_MAX_POOLS, 16-byte aligned. */
+/* Pools that a call works on: HOST array [n_pools] of DEVICE pointers, 0 <= n_pools <= DSLA_MAX_POOLS, 16-byte aligned and
+ * different from each other (else DSLA_ERR_SHAPE). */
 #define DSLA_MAX_POOLS 256
 
 /* Scratch of dsla_cache_extend, dsla_cache_accept (for up to B entries) and dsla_cache_compact, 16-byte aligned; 0 for an invalid
@@ -470,20 +471,20 @@ DSLA_API dsla_status dsla_cache_compact(const dsla_cache *cache, int32_t *n_live
  * values written into their pages, in one pass:
  *     y = x / sqrt(mean(x^2) + eps) * w        (y_a, y_b) <- (y_a cos - y_b sin, y_a sin + y_b cos),  angle = position * inv_freq[i]
  *     pairs i = 0 .. rot_dim/2 - 1: (a, b) = (i, i + rot_dim/2), or (2i, 2i + 1) with interleaved != 0
- * fp32 arithmetic, angles in fp64; results are rounded once.
+ * fp32 arithmetic (squares too: norms are of features up to 10^18), angles in fp64; results are rounded once.
  *   q      : [total][H][d]      k, v : [total][H_kv][d]
  *   q_out  : [total][H][d], written; may be q      k_out : the same for k, or NULL where only the pages need them
  *   cache, batch, k_pages, v_pages : where keys and values go (cache->status as above), or all NULL: then every token takes
- *            part and v may be NULL.  A token's place is start[b] + its number in the entry
+ *            part and v may be NULL; k_pages and v_pages are different pools.  A token's place is start[b] + its number in the entry
  *   position = start[b] + offsets[m] (start = 0 without a batch), offsets NULL: the number in its entry (without a batch: m)
  * total_rows: tokens of the tensors; with a batch it is batch->total.
  */
 typedef struct {
-    int32_t H, H_kv, d;       /* d in {64, 128}                                                                          */
+    int32_t H, H_kv, d;       /* H and H_kv up to 2^16, d in {64, 128}                                                   */
     int32_t io_dtype;         /* dsla_dtype of q, k, v and the outputs; with a cache also its type                       */
     int32_t rot_dim;          /* features rotated: a multiple of 16, 0 .. d                                              */
     int32_t interleaved;      /* which features form pairs                                                               */
-    float eps;                /* > 0 with weights                                                                        */
+    float eps;                /* with weights > 0 and below 3e38                                                         */
     const float *inv_freq;    /* DEVICE [rot_dim / 2], radians per position; NULL where rot_dim = 0                      */
     const float *q_weight;    /* DEVICE [d], norm of q; NULL = no norm                                                   */
     const float *k_weight;    /* DEVICE [d], norm of k; NULL = no norm                                                   */
