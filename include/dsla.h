@@ -63,7 +63,11 @@ typedef enum {
     DSLA_ERR_HIP = 5          /* a HIP call failed                                    */
 } dsla_status;
 
-typedef enum { DSLA_F32 = 0, DSLA_BF16 = 1 } dsla_dtype;
+typedef enum {
+    DSLA_F32 = 0,
+    DSLA_BF16 = 1,
+    DSLA_E4M3 = 2   /* 8 bits: sign, 4 of exponent, 3 of mantissa, largest number 448, NaN, no infinity; with block scales (below) */
+} dsla_dtype;
 
 /*
  * What the gate tensors g1, g2 hold.  The paper describes the gates as driven by the data and produced by single linear
@@ -350,6 +354,98 @@ DSLA_API dsla_status dsla_project(int64_t M, int32_t K, int32_t n_out, int32_t w
                          const void *x, const void *W, const float *bias, void *const *outs, void *stream);
 
 /*
+ * What stands around the layer in a block of a model, with a residual stream x:
+ *     x' = x + residual_scale * act(gate) * norm_post(y)      y: the block's result, as its output projection leaves it
+ *     h  = norm_pre(x')                                       what the next block's projections read
+ * (dsla_residual_norm) and inside it, between the read-out and the output projection, norm and output gate of every head
+ * (dsla_head_norm).  norm(u) = u / sqrt(mean(u^2) + eps) * weight.  The layer itself applies none of them (Section 4.1).  Both
+ * calls write bf16, fp32, or e4m3 with block scales, the operands of dsla_project_fp8.
+ *
+ * Block scales.  An e4m3 tensor [rows][cols] stands for q * scale, one scale for each block of 128 columns of a row (activations), or of
+ * 128 x 128 (weights); the last blocks may be smaller.  Scales are [rows][P], or [ceil(rows / 128)][P], P = DSLA_SCALE_PITCH(cols): a
+ * row's ceil(cols / 128) scales, rounded up to a multiple of four; what lies behind them is neither read for a result nor written.
+ *   DSLA_SCALE_F32  : fp32, amax / 448
+ *   DSLA_SCALE_E8M0 : one byte b for 2^(b - 127), 255 = NaN; the smallest power of two that keeps amax within 448.  The matrix
+ *                     instructions multiply by it themselves
+ * with amax the largest finite magnitude of the block, taken as 2^-100 where it is below that.  q is the value times 448 / amax (in fp32), or
+ * 2^(127 - b), rounded to nearest even; what is not finite becomes NaN.
+ */
+#define DSLA_SCALE_PITCH(cols) (((cols) + 511) / 512 * 4)
+typedef enum { DSLA_SCALE_F32 = 0, DSLA_SCALE_E8M0 = 1 } dsla_scale_type;
+typedef enum { DSLA_ACT_NONE = 0, DSLA_ACT_SIGMOID = 1, DSLA_ACT_SILU = 2 } dsla_act;   /* z, 1 / (1 + e^-z), z / (1 + e^-z) */
+
+/*
+ * dsla_residual_norm - the border between two blocks in one pass.  Arithmetic is fp32; both results are rounded once, and h is
+ * computed from x' before its rounding.  Norms are of features up to 10^18.
+ *   rows     : tokens, >= 1
+ *   x, x_out : [rows][D] of x_dtype; x_out NULL: x' is not kept
+ *   y        : [rows][D] of y_dtype, or NULL: x' = x (then no gate, no post_weight)
+ *   gate     : [rows][D] of y_dtype, or NULL: no factor
+ *   h        : [rows][D] of h_dtype, or NULL: only x' is wanted (one of x_out and h is required; pre_weight is then not used)
+ *   h_scale  : scales of h where h_dtype is DSLA_E4M3, else NULL
+ * An output may be the buffer of an input whose elements are as large; otherwise nothing overlaps.
+ */
+typedef struct {
+    int32_t D;                 /* width, a multiple of 16 up to 32768                                 */
+    int32_t x_dtype;           /* dsla_dtype of x and x_out: DSLA_F32 or DSLA_BF16                    */
+    int32_t y_dtype;           /* of y and gate: DSLA_F32 or DSLA_BF16                                */
+    int32_t h_dtype;           /* of h: any                                                           */
+    int32_t scale_type;        /* dsla_scale_type of h_scale                                          */
+    int32_t gate_act;          /* dsla_act                                                            */
+    float eps;                 /* where there is a norm: > 0 and below 3e38                           */
+    float residual_scale;      /* any finite number                                                   */
+    const float *post_weight;  /* DEVICE [D]; NULL = no norm of y                                     */
+    const float *pre_weight;   /* DEVICE [D]; NULL = no norm of x': h = x' in its type                */
+} dsla_norm;
+DSLA_API dsla_status dsla_residual_norm(const dsla_norm *norm, int64_t rows, const void *x, const void *y, const void *gate,
+                                        void *x_out, void *h, void *h_scale, void *stream);
+
+/*
+ * dsla_head_norm - norm and gate of the layer's read-out: every head of o by its own root mean square, times the weight, times
+ * act(gate).  fp32 arithmetic, one rounding; features up to 10^18.
+ *   o, gate : [rows][H][d] of io_dtype; gate NULL: no factor     out : [rows][H d] of out_dtype; may be o or gate where its elements are as large
+ *   out_scale : scales of out where out_dtype is DSLA_E4M3 (a block holds one head of 128 or two of 64), else NULL
+ */
+typedef struct {
+    int32_t H, d;          /* H up to 2^16, d in {64, 128}                                          */
+    int32_t io_dtype;      /* DSLA_F32 or DSLA_BF16                                                 */
+    int32_t out_dtype;     /* any                                                                   */
+    int32_t scale_type;    /* dsla_scale_type of out_scale                                          */
+    int32_t gate_act;      /* dsla_act                                                              */
+    float eps;             /* with a weight: > 0 and below 3e38                                     */
+    const float *weight;   /* DEVICE [d], the same for every head; NULL = no norm                   */
+} dsla_heads;
+DSLA_API dsla_status dsla_head_norm(const dsla_heads *heads, int64_t rows, const void *o, const void *gate, void *out, void *out_scale,
+                                    void *stream);
+
+/*
+ * dsla_quantize - x [rows][cols] of in_dtype (DSLA_F32 or DSLA_BF16) to e4m3 with block scales: block_rows = 1 for activations, 128 for
+ * weights (each output of a stacked weight by a call of its own where its rows are no multiple of 128).  cols: a multiple of 16, up to 2^21.
+ */
+DSLA_API dsla_status dsla_quantize(int64_t rows, int32_t cols, int32_t in_dtype, int32_t block_rows, int32_t scale_type, const void *x,
+                                   void *q, void *scale, void *stream);
+
+/*
+ * dsla_project_fp8 - dsla_project with e4m3 operands and block scales; the outputs may differ in width (fewer key/value heads, an
+ * output projection):
+ *     out_j[m][c] = sum_k x[m][k] W_j[c][k] (+ bias_j[c]),     j = 0 .. n_out - 1
+ *   M       : rows of x, >= 1              K : a multiple of 16, up to 2^21
+ *   widths  : HOST array [n_out], columns of every output, multiples of 16, up to 2^24 in all; n_out = 1 .. DSLA_MAX_PROJECTIONS
+ *   x       : [M][K] e4m3 with scales for 128 columns of a row
+ *   W       : the W_j [width_j][K] e4m3 one behind the other; W_scale: their scales for blocks of 128 x 128 one behind the other,
+ *             ceil(width_j / 128) rows of DSLA_SCALE_PITCH(K) for each
+ *   bias    : fp32, the bias_j [width_j] one behind the other, or NULL
+ *   outs    : HOST array [n_out] of DEVICE pointers, [M][width_j] of out_dtype (DSLA_F32 or DSLA_BF16), written
+ * scale_type is that of x_scale and W_scale; the product of two fp32 scales should be a normal number.  fp32 accumulation, a block's
+ * products scaled as a whole; no workspace.  outs in bf16: e4m3 matrix instructions, which add products in groups of eight
+ * and keep of each what is above 2^-14 of its group's largest (random operands: 1.5e-5 of a result, against 2e-3 of its rounding); outs
+ * in fp32: the operands go through bf16 instructions (exactly), which add in fp32.
+ */
+DSLA_API dsla_status dsla_project_fp8(int64_t M, int32_t K, int32_t n_out, const int32_t *widths, int32_t scale_type, const void *x,
+                                      const void *x_scale, const void *W, const void *W_scale, const float *bias, int32_t out_dtype,
+                                      void *const *outs, void *stream);
+
+/*
  * dsla_attention_prefill - causal softmax attention over a whole prompt: the prefill of a layer that has NOT been
  * converted, which a partly converted model runs beside its DSLA layers (Section 4.3) and whose quadratic cost the
  * linear-time DSLA prefill is measured against (Section 5.3):
@@ -569,7 +665,8 @@ DSLA_API const char *dsla_last_hip_error(void);
  * Kernel ids: 0 state_init, 1 prefill_segment_state, 2 prefill_segment_scan,
  * 3 prefill_chunk_loop, 4 decode, 5 prefill_segment_list (packed sequences only), 6 attention_entropy,
  * 7 attention_decode (each with its merge kernel), 8 decode_multi, 9 attention_prefill, 10 project,
- * 11 cache (every launch of the dsla_cache calls), 12 qk_rope, 13 attention_paged (with its merge kernel).
+ * 11 cache (every launch of the dsla_cache calls), 12 qk_rope, 13 attention_paged (with its merge kernel), 14 residual_norm,
+ * 15 head_norm, 16 quantize, 17 project_fp8.
  */
 #define DSLA_KERNEL_STATE_INIT 0
 #define DSLA_KERNEL_PREFILL_SEGMENT_STATE 1
@@ -585,7 +682,11 @@ DSLA_API const char *dsla_last_hip_error(void);
 #define DSLA_KERNEL_CACHE 11
 #define DSLA_KERNEL_QK_ROPE 12
 #define DSLA_KERNEL_ATTENTION_PAGED 13
-#define DSLA_KERNEL_COUNT 14
+#define DSLA_KERNEL_RESIDUAL_NORM 14
+#define DSLA_KERNEL_HEAD_NORM 15
+#define DSLA_KERNEL_QUANTIZE 16
+#define DSLA_KERNEL_PROJECT_FP8 17
+#define DSLA_KERNEL_COUNT 18
 
 /* enable != 0: create the event pool (max_records launches can be recorded between two
  * collects) and start recording; enable == 0: stop and destroy the pool. */

@@ -17,3 +17,6 @@ from .binding import (DslaDesc, DslaError, DslaMulti, dsla_decode_multi, dsla_pr
 from .binding import (DslaBatch, DslaCache, DslaRope, make_batch, make_cache, make_pools, make_rope,  # noqa: F401
                       dsla_attention_paged, dsla_attention_paged_workspace_bytes, dsla_cache_accept, dsla_cache_compact, dsla_cache_extend,
                       dsla_cache_fork, dsla_cache_init, dsla_cache_truncate, dsla_cache_workspace_bytes, dsla_qk_rope)
+from .binding import (DSLA_ACT_NONE, DSLA_ACT_SIGMOID, DSLA_ACT_SILU, DSLA_BF16, DSLA_E4M3, DSLA_F32, DSLA_SCALE_E8M0, DSLA_SCALE_F32,  # noqa: F401
+                      DslaHeads, DslaNorm, dsla_head_norm, dsla_project_fp8, dsla_quantize, dsla_residual_norm, make_head_norm, make_norm,
+                      scale_pitch)

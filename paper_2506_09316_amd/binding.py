@@ -21,20 +21,24 @@ _torch = None   # torch._C once the library is loaded
 class _General:
     """In the place of _marshal: leaves every call to the general way."""
     decode = decode_slots = prefill = prefill_varlen = attention_decode = attention_prefill = project = staticmethod(lambda *a: None)
+    residual_norm = head_norm = quantize = project_fp8 = decode
     cache_extend = cache_fork = cache_truncate = cache_accept = cache_compact = qk_rope = attention_paged = decode
 
 
 _native = _General   # _marshal once the library is loaded, where it can be used
 
-DSLA_F32, DSLA_BF16 = 0, 1
+DSLA_F32, DSLA_BF16, DSLA_E4M3 = 0, 1, 2
+DSLA_SCALE_F32, DSLA_SCALE_E8M0 = 0, 1
+DSLA_ACT_NONE, DSLA_ACT_SIGMOID, DSLA_ACT_SILU = 0, 1, 2
 KERNEL_NAMES = ("state_init", "prefill_segment_state", "prefill_segment_scan", "prefill_chunk_loop", "decode",
                 "prefill_segment_list", "attention_entropy", "attention_decode", "decode_multi", "attention_prefill", "project",
-                "cache", "qk_rope", "attention_paged")
+                "cache", "qk_rope", "attention_paged", "residual_norm", "head_norm", "quantize", "project_fp8")
 EXPORTS = ("dsla_state_init", "dsla_prefill_workspace_bytes", "dsla_prefill", "dsla_prefill_static_ws", "dsla_decode",
            "dsla_prefill_varlen_workspace_bytes", "dsla_prefill_varlen", "dsla_decode_slots",
            "dsla_decode_multi", "dsla_prefill_multi_workspace_bytes", "dsla_prefill_multi",
            "dsla_attention_entropy_workspace_bytes", "dsla_attention_entropy",
            "dsla_attention_decode_workspace_bytes", "dsla_attention_decode", "dsla_attention_prefill", "dsla_project",
+           "dsla_residual_norm", "dsla_head_norm", "dsla_quantize", "dsla_project_fp8",
            "dsla_cache_workspace_bytes", "dsla_cache_init", "dsla_cache_extend", "dsla_cache_fork", "dsla_cache_truncate",
            "dsla_cache_accept", "dsla_cache_compact", "dsla_qk_rope", "dsla_attention_paged_workspace_bytes", "dsla_attention_paged",
            "dsla_rank_layers", "dsla_max_conversion_rate", "dsla_kv_cache_bytes", "dsla_conversion_plan",
@@ -75,6 +79,19 @@ class DslaRope(ctypes.Structure):
     _fields_ = [("H", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("d", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
                 ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float), ("inv_freq", ctypes.c_void_p), ("q_weight", ctypes.c_void_p),
                 ("k_weight", ctypes.c_void_p), ("offsets", ctypes.c_void_p)]
+
+
+class DslaNorm(ctypes.Structure):
+    """Mirror of `dsla_norm` in include/dsla.h."""
+    _fields_ = [("D", ctypes.c_int32), ("x_dtype", ctypes.c_int32), ("y_dtype", ctypes.c_int32), ("h_dtype", ctypes.c_int32),
+                ("scale_type", ctypes.c_int32), ("gate_act", ctypes.c_int32), ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float),
+                ("post_weight", ctypes.c_void_p), ("pre_weight", ctypes.c_void_p)]
+
+
+class DslaHeads(ctypes.Structure):
+    """Mirror of `dsla_heads` in include/dsla.h."""
+    _fields_ = [("H", ctypes.c_int32), ("d", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("scale_type", ctypes.c_int32), ("gate_act", ctypes.c_int32), ("eps", ctypes.c_float), ("weight", ctypes.c_void_p)]
 
 
 class DslaError(RuntimeError):
@@ -138,6 +155,15 @@ def load_library():
     lib.dsla_attention_decode.restype = ctypes.c_int
     lib.dsla_project.argtypes = [ctypes.c_int64] + [ctypes.c_int32] * 3 + [vp] * 3 + [ctypes.POINTER(ctypes.c_void_p), vp]
     lib.dsla_project.restype = ctypes.c_int
+    lib.dsla_residual_norm.argtypes = [ctypes.POINTER(DslaNorm), ctypes.c_int64] + [vp] * 7
+    lib.dsla_residual_norm.restype = ctypes.c_int
+    lib.dsla_head_norm.argtypes = [ctypes.POINTER(DslaHeads), ctypes.c_int64] + [vp] * 5
+    lib.dsla_head_norm.restype = ctypes.c_int
+    lib.dsla_quantize.argtypes = [ctypes.c_int64] + [ctypes.c_int32] * 4 + [vp] * 4
+    lib.dsla_quantize.restype = ctypes.c_int
+    lib.dsla_project_fp8.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_int32), ctypes.c_int32] + [vp] * 5 + [
+        ctypes.c_int32, ctypes.POINTER(ctypes.c_void_p), vp]
+    lib.dsla_project_fp8.restype = ctypes.c_int
     lib.dsla_attention_prefill.argtypes = [ctypes.c_int32] * 3 + [ctypes.c_int64, ctypes.c_int32, ctypes.c_float] + [vp] * 5
     lib.dsla_attention_prefill.restype = ctypes.c_int
     cp, bp, pools = ctypes.POINTER(DslaCache), ctypes.POINTER(DslaBatch), [ctypes.c_int32, ctypes.POINTER(ctypes.c_void_p)]
@@ -202,8 +228,8 @@ def _load_native(lib):
         return _General
     entries = (lib.dsla_decode, lib.dsla_decode_slots, lib.dsla_prefill, lib.dsla_prefill_varlen, lib.dsla_attention_decode,
                lib.dsla_attention_prefill, lib.dsla_project, lib.dsla_cache_extend, lib.dsla_cache_fork, lib.dsla_cache_truncate, lib.dsla_cache_accept,
-               lib.dsla_cache_compact, lib.dsla_qk_rope, lib.dsla_attention_paged)
-    _marshal.bind(*torch_calls, torch.nn.Parameter, DslaDesc, DslaCache, DslaBatch, DslaRope, *[ctypes.cast(f, ctypes.c_void_p).value for f in entries])
+               lib.dsla_cache_compact, lib.dsla_qk_rope, lib.dsla_attention_paged, lib.dsla_residual_norm, lib.dsla_head_norm, lib.dsla_quantize, lib.dsla_project_fp8)
+    _marshal.bind(*torch_calls, torch.nn.Parameter, DslaDesc, DslaCache, DslaBatch, DslaRope, DslaNorm, DslaHeads, *[ctypes.cast(f, ctypes.c_void_p).value for f in entries])
     return _marshal
 
 
@@ -607,6 +633,123 @@ def dsla_attention_paged(cache: DslaCache, batch: DslaBatch, q, k_pages, v_pages
     _check(lib.dsla_attention_paged(ctypes.byref(cache), ctypes.byref(batch), int(H), int(max_len), float(scale), _here(q, dtype, n),
                                                _here(k_pages, dtype, pool), _here(v_pages, dtype, pool),
                                                _here(tree, torch.int64, batch.total, optional=True), _here(o, dtype, n), *_scratch(workspace), _stream()))
+
+
+def scale_pitch(cols: int) -> int:
+    """Scales of a row of an e4m3 tensor (include/dsla.h: DSLA_SCALE_PITCH)."""
+    return (int(cols) + 511) // 512 * 4
+
+
+def _result_dtype(code):
+    import torch
+    return torch.float8_e4m3fn if code == DSLA_E4M3 else _io_dtype(code)
+
+
+def _scale_dtype(code):
+    import torch
+    return torch.float8_e8m0fnu if code == DSLA_SCALE_E8M0 else torch.float32
+
+
+def _scale_code(t):
+    import torch
+    if t.dtype not in (torch.float32, torch.float8_e8m0fnu):
+        raise TypeError(f"scales of {t.dtype}")
+    return DSLA_SCALE_F32 if t.dtype == torch.float32 else DSLA_SCALE_E8M0
+
+
+def make_norm(D, *, x_dtype, y_dtype, h_dtype, scale_type=DSLA_SCALE_E8M0, gate_act=DSLA_ACT_NONE, eps=1e-6, residual_scale=1.0, post_weight=None,
+              pre_weight=None) -> DslaNorm:
+    """dsla_norm: post_weight, pre_weight fp32 GPU tensors [D] or None (no norm).  The structure keeps the tensors alive."""
+    import torch
+    load_library()
+    n = DslaNorm(int(D), int(x_dtype), int(y_dtype), int(h_dtype), int(scale_type), int(gate_act), float(eps), float(residual_scale),
+                 _here(post_weight, torch.float32, D, optional=True), _here(pre_weight, torch.float32, D, optional=True))
+    n._keep = (post_weight, pre_weight)
+    if any(t is not None for t in n._keep):
+        n.device = _torch._cuda_getDevice()
+    return n
+
+
+def dsla_residual_norm(norm: DslaNorm, x, y, x_out, h, gate=None, h_scale=None):
+    """Residual, gate, scale and norms of a block's border (include/dsla.h: dsla_residual_norm).  x, x_out, y, gate, h: [rows, D]; y, x_out or h,
+    gate may be None.  h e4m3: h_scale [rows, scale_pitch(D)], float32 or float8_e8m0fnu."""
+    lib = _lib or load_library()
+    _same_device(norm)
+    status = _native.residual_norm(norm, x, y, gate, x_out, h, h_scale)
+    if status is not None:
+        return _check(status)
+    n, D = x.numel(), max(1, norm.D)
+    rows = n // D
+    _check(lib.dsla_residual_norm(ctypes.byref(norm), rows, _here(x, _io_dtype(norm.x_dtype), rows * D), _here(y, _io_dtype(norm.y_dtype), n, optional=True),
+                                  _here(gate, _io_dtype(norm.y_dtype), n, optional=True), _here(x_out, _io_dtype(norm.x_dtype), n, optional=True),
+                                  _here(h, _result_dtype(norm.h_dtype), n, optional=True),
+                                  _here(h_scale, _scale_dtype(norm.scale_type), rows * scale_pitch(D), optional=True), _stream()))
+
+
+def make_head_norm(H, d, *, io_dtype, out_dtype, scale_type=DSLA_SCALE_E8M0, gate_act=DSLA_ACT_SILU, eps=1e-6, weight=None) -> DslaHeads:
+    """dsla_heads: weight fp32 GPU tensor [d] or None (no norm).  The structure keeps the tensor alive."""
+    import torch
+    load_library()
+    x = DslaHeads(int(H), int(d), int(io_dtype), int(out_dtype), int(scale_type), int(gate_act), float(eps), _here(weight, torch.float32, d, optional=True))
+    x._keep = (weight,)
+    if weight is not None:
+        x.device = _torch._cuda_getDevice()
+    return x
+
+
+def dsla_head_norm(heads: DslaHeads, o, out, gate=None, out_scale=None):
+    """Norm and gate of every head (include/dsla.h: dsla_head_norm).  o, gate [rows, H, d]; out [rows, H * d]; out e4m3: out_scale [rows,
+    scale_pitch(H * d)], float32 or float8_e8m0fnu."""
+    lib = _lib or load_library()
+    _same_device(heads)
+    status = _native.head_norm(heads, o, gate, out, out_scale)
+    if status is not None:
+        return _check(status)
+    n, W = o.numel(), max(1, heads.H * heads.d)
+    rows = n // W
+    _check(lib.dsla_head_norm(ctypes.byref(heads), rows, _here(o, _io_dtype(heads.io_dtype), rows * W), _here(gate, _io_dtype(heads.io_dtype), n, optional=True),
+                              _here(out, _result_dtype(heads.out_dtype), n), _here(out_scale, _scale_dtype(heads.scale_type), rows * scale_pitch(W), optional=True),
+                              _stream()))
+
+
+def dsla_quantize(x, q, scale, block_rows: int = 1):
+    """e4m3 values with block scales (include/dsla.h: dsla_quantize).  x [rows, cols] bf16 or fp32, q the same in float8_e4m3fn, scale [rows or
+    ceil(rows / 128), scale_pitch(cols)] float32 or float8_e8m0fnu.  block_rows: 1 or 128."""
+    lib = _lib or load_library()
+    status = _native.quantize(x, q, scale, block_rows)
+    if status is not None:
+        return _check(status)
+    import torch
+    rows, cols = x.shape
+    n = -(-rows // max(1, int(block_rows))) * scale_pitch(cols)
+    _check(lib.dsla_quantize(int(rows), int(cols), _dtype_code(x), int(block_rows), _scale_code(scale), _here(x, x.dtype),
+                             _here(q, torch.float8_e4m3fn, rows * cols), _here(scale, scale.dtype, n), _stream()))
+
+
+def dsla_project_fp8(x, x_scale, W, W_scale, outs, bias=None):
+    """The projections as one product of e4m3 operands with block scales (include/dsla.h: dsla_project_fp8).  x [M, K], W [sum of widths, K]
+    float8_e4m3fn, their scales as dsla_quantize leaves them; outs: list of bf16 or fp32 GPU tensors [M, width]; bias: fp32 GPU tensor or None."""
+    lib = _lib or load_library()
+    status = _native.project_fp8(x, x_scale, W, W_scale, outs, bias)
+    if status is not None:
+        return _check(status)
+    import torch
+    M, K = x.shape
+    if not outs:
+        raise ValueError("no outputs")
+    dtype = outs[0].dtype
+    if any(t.dim() != 2 or t.shape[0] != M or t.shape[1] > 1 << 24 for t in outs):
+        raise ValueError("outputs are [M, width], of up to 2^24 columns")
+    n_out, code, widths = len(outs), _dtype_code(outs[0]), [t.shape[1] for t in outs]
+    N = sum(widths)
+    if W.dim() != 2 or W.shape[1] != K:
+        raise ValueError(f"weights of {tuple(W.shape)} for rows of {K}")
+    P = scale_pitch(K)
+    po = (ctypes.c_void_p * n_out)(*[_here(t, dtype) for t in outs])
+    _check(lib.dsla_project_fp8(int(M), int(K), n_out, (ctypes.c_int32 * n_out)(*widths), _scale_code(x_scale), _here(x, torch.float8_e4m3fn),
+                                _here(x_scale, x_scale.dtype, M * P), _here(W, torch.float8_e4m3fn, N * K),
+                                _here(W_scale, x_scale.dtype, sum(-(-w // 128) for w in widths) * P), _here(bias, torch.float32, N, optional=True),
+                                code, po, _stream()))
 
 
 PLAN_REASONS = ("no pressure", "memory relief", "quality limit", "all converted")

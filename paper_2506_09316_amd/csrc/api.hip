@@ -429,6 +429,110 @@ dsla_status dsla_project(int64_t M, int32_t K, int32_t n_out, int32_t width, con
     return hip_status(launch_project(M, K, n_out, width, x, W, bias, outs, static_cast<hipStream_t>(stream)));
 }
 
+namespace {
+bool io_type(int32_t t) { return t == DSLA_F32 || t == DSLA_BF16; }
+size_t type_bytes(int32_t t) { return t == DSLA_F32 ? 4 : (t == DSLA_BF16 ? 2 : 1); }
+bool scale_type_ok(int32_t t) { return t == DSLA_SCALE_F32 || t == DSLA_SCALE_E8M0; }
+bool good_eps(float eps) { return eps > 0.f && eps < 3e38f; }
+// A result and what it may be written over: an input whose elements are as large.
+bool in_place_ok(const void *out, size_t out_bytes, const void *in, size_t in_bytes) { return out != in || !out || out_bytes == in_bytes; }
+// Result type, its scales and the activation of its gate.
+dsla_status check_result(int32_t dtype, int32_t scale_type, const void *scale, int32_t act)
+{
+    if (!io_type(dtype) && dtype != DSLA_E4M3) return DSLA_ERR_UNSUPPORTED;
+    if (act != DSLA_ACT_NONE && act != DSLA_ACT_SIGMOID && act != DSLA_ACT_SILU) return DSLA_ERR_UNSUPPORTED;
+    if (dtype == DSLA_E4M3) {
+        if (!scale_type_ok(scale_type)) return DSLA_ERR_UNSUPPORTED;
+        if (!scale) return DSLA_ERR_NULL;
+        if (!aligned16(scale)) return DSLA_ERR_SHAPE;
+    } else if (scale) {
+        return DSLA_ERR_SHAPE;
+    }
+    return DSLA_OK;
+}
+}  // namespace
+
+dsla_status dsla_residual_norm(const dsla_norm *n, int64_t rows, const void *x, const void *y, const void *gate, void *x_out, void *h, void *h_scale,
+                               void *stream)
+{
+    if (!n) return DSLA_ERR_NULL;
+    if (rows <= 0 || n->D <= 0) return DSLA_ERR_SHAPE;
+    if (n->D % 16 != 0 || n->D > 32768 || !io_type(n->x_dtype) || !io_type(n->y_dtype)) return DSLA_ERR_UNSUPPORTED;
+    if (rows > 0x7fffffffLL / ((n->D + 127) / 128)) return DSLA_ERR_SHAPE;
+    if (!x || (!x_out && !h)) return DSLA_ERR_NULL;
+    if (!y && (gate || n->post_weight)) return DSLA_ERR_NULL;
+    if (h) {
+        const dsla_status s = check_result(n->h_dtype, n->scale_type, h_scale, n->gate_act);
+        if (s != DSLA_OK) return s;
+    } else {
+        if (h_scale) return DSLA_ERR_SHAPE;
+        if (n->gate_act != DSLA_ACT_NONE && n->gate_act != DSLA_ACT_SIGMOID && n->gate_act != DSLA_ACT_SILU) return DSLA_ERR_UNSUPPORTED;
+    }
+    if ((n->post_weight || n->pre_weight) && !good_eps(n->eps)) return DSLA_ERR_SHAPE;
+    if (!(n->residual_scale - n->residual_scale == 0.f)) return DSLA_ERR_SHAPE;   // inf, NaN
+    for (const void *p : {x, y, gate, static_cast<const void *>(x_out), static_cast<const void *>(h), static_cast<const void *>(n->post_weight),
+                          static_cast<const void *>(n->pre_weight)})
+        if (!aligned16(p)) return DSLA_ERR_SHAPE;
+    const size_t bx = type_bytes(n->x_dtype), by = type_bytes(n->y_dtype), bh = type_bytes(n->h_dtype);
+    if (h && h == x_out) return DSLA_ERR_SHAPE;
+    if (h_scale && (h_scale == h || h_scale == x_out || h_scale == x || h_scale == y || h_scale == gate)) return DSLA_ERR_SHAPE;
+    for (const void *in : {x, y, gate})
+        if (!in_place_ok(x_out, bx, in, in == x ? bx : by) || !in_place_ok(h, bh, in, in == x ? bx : by)) return DSLA_ERR_SHAPE;
+    return hip_status(launch_residual_norm(*n, rows, x, y, gate, x_out, h, h_scale, static_cast<hipStream_t>(stream)));
+}
+
+dsla_status dsla_head_norm(const dsla_heads *n, int64_t rows, const void *o, const void *gate, void *out, void *out_scale, void *stream)
+{
+    if (!n) return DSLA_ERR_NULL;
+    if (rows <= 0 || n->H <= 0 || n->H > (1 << 16)) return DSLA_ERR_SHAPE;
+    if ((n->d != 64 && n->d != 128) || !io_type(n->io_dtype)) return DSLA_ERR_UNSUPPORTED;
+    if (rows > 0x7fffffffLL / ((static_cast<int64_t>(n->H) * n->d + 127) / 128)) return DSLA_ERR_SHAPE;
+    if (!o || !out) return DSLA_ERR_NULL;
+    const dsla_status s = check_result(n->out_dtype, n->scale_type, out_scale, n->gate_act);
+    if (s != DSLA_OK) return s;
+    if (n->weight && !good_eps(n->eps)) return DSLA_ERR_SHAPE;
+    if (!aligned16(o) || !aligned16(gate) || !aligned16(out) || !aligned16(n->weight)) return DSLA_ERR_SHAPE;
+    if (out_scale && (out_scale == o || out_scale == gate || out_scale == out)) return DSLA_ERR_SHAPE;
+    const size_t bo = type_bytes(n->out_dtype), bi = type_bytes(n->io_dtype);
+    if (!in_place_ok(out, bo, o, bi) || !in_place_ok(out, bo, gate, bi)) return DSLA_ERR_SHAPE;
+    return hip_status(launch_head_norm(*n, rows, o, gate, out, out_scale, static_cast<hipStream_t>(stream)));
+}
+
+dsla_status dsla_quantize(int64_t rows, int32_t cols, int32_t in_dtype, int32_t block_rows, int32_t scale_type, const void *x, void *q, void *scale,
+                          void *stream)
+{
+    if (rows <= 0 || cols <= 0) return DSLA_ERR_SHAPE;
+    if (cols % 16 != 0 || cols > (1 << 21) || !io_type(in_dtype) || (block_rows != 1 && block_rows != 128) || !scale_type_ok(scale_type)) return DSLA_ERR_UNSUPPORTED;
+    if (rows > 0x7fffffffLL / ((cols + 127) / 128)) return DSLA_ERR_SHAPE;
+    if (!x || !q || !scale) return DSLA_ERR_NULL;
+    if (!aligned16(x) || !aligned16(q) || !aligned16(scale)) return DSLA_ERR_SHAPE;
+    if (q == x || scale == x || scale == q) return DSLA_ERR_SHAPE;
+    return hip_status(launch_quantize(rows, cols, in_dtype, block_rows, scale_type, x, q, scale, static_cast<hipStream_t>(stream)));
+}
+
+dsla_status dsla_project_fp8(int64_t M, int32_t K, int32_t n_out, const int32_t *widths, int32_t scale_type, const void *x, const void *x_scale,
+                             const void *W, const void *W_scale, const float *bias, int32_t out_dtype, void *const *outs, void *stream)
+{
+    if (M <= 0 || K <= 0 || n_out <= 0) return DSLA_ERR_SHAPE;
+    if (n_out > DSLA_MAX_PROJECTIONS || K % 16 != 0 || K > (1 << 21) || !scale_type_ok(scale_type) || !io_type(out_dtype)) return DSLA_ERR_UNSUPPORTED;
+    if (!widths || !outs) return DSLA_ERR_NULL;
+    int64_t columns = 0, blocks = 0;
+    for (int j = 0; j < n_out; ++j) {
+        if (widths[j] <= 0 || widths[j] > (1 << 24)) return DSLA_ERR_SHAPE;
+        if (widths[j] % 16 != 0) return DSLA_ERR_UNSUPPORTED;
+        columns += widths[j];
+        blocks += (widths[j] + 127) / 128;
+    }
+    if (columns > (1 << 24) || (M + 63) / 64 * 2 * blocks > 0x7ffffff0LL) return DSLA_ERR_SHAPE;
+    if (!x || !x_scale || !W || !W_scale) return DSLA_ERR_NULL;
+    if (!aligned16(x) || !aligned16(x_scale) || !aligned16(W) || !aligned16(W_scale) || !aligned16(bias)) return DSLA_ERR_SHAPE;
+    for (int j = 0; j < n_out; ++j) {
+        if (!outs[j]) return DSLA_ERR_NULL;
+        if (!aligned16(outs[j])) return DSLA_ERR_SHAPE;
+    }
+    return hip_status(launch_project_fp8(M, K, n_out, widths, scale_type, x, x_scale, W, W_scale, bias, out_dtype, outs, static_cast<hipStream_t>(stream)));
+}
+
 dsla_status dsla_attention_prefill(int32_t B, int32_t H, int32_t d, int64_t T, int32_t io_dtype, float scale,
                                    const void *q, const void *k, const void *v, void *o, void *stream)
 {

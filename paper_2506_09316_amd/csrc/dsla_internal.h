@@ -134,6 +134,13 @@ hipError_t launch_attn_decode(int B, int H, int d, int64_t T, int io_dtype, cons
                               void *workspace, hipStream_t stream);
 hipError_t launch_project(int64_t M, int K, int n_out, int width, const void *x, const void *w, const float *bias,
                           void *const *outs, hipStream_t stream);
+// Around a layer (norms.hip) and its projections in 8 bits (project_fp8.hip); arguments checked by api.hip.
+hipError_t launch_residual_norm(const dsla_norm &n, int64_t rows, const void *x, const void *y, const void *gate, void *x_out, void *h, void *h_scale,
+                                hipStream_t stream);
+hipError_t launch_head_norm(const dsla_heads &n, int64_t rows, const void *o, const void *gate, void *out, void *out_scale, hipStream_t stream);
+hipError_t launch_quantize(int64_t rows, int cols, int in_dtype, int block_rows, int scale_type, const void *x, void *q, void *scale, hipStream_t stream);
+hipError_t launch_project_fp8(int64_t M, int K, int n_out, const int32_t *widths, int scale_type, const void *x, const void *x_scale, const void *w,
+                              const void *w_scale, const float *bias, int out_dtype, void *const *outs, hipStream_t stream);
 hipError_t launch_attn_prefill(int B, int H, int d, int64_t T, float scale, const void *q, const void *k, const void *v,
                                void *o, hipStream_t stream);
 hipError_t launch_entropy(int B, int H, int d, int64_t T, int io_dtype, const EntropyPlan &plan, float scale,

@@ -14,8 +14,8 @@
 
 namespace {
 
-// torch._C._cuda_getDevice, _cuda_getCurrentRawStream; torch.nn.Parameter, binding.DslaDesc, DslaCache, DslaBatch, DslaRope
-PyObject *g_device, *g_raw_stream, *g_parameter, *g_desc, *g_cache, *g_batch, *g_rope;
+// torch._C._cuda_getDevice, _cuda_getCurrentRawStream; torch.nn.Parameter, binding.DslaDesc, DslaCache, DslaBatch, DslaRope, DslaNorm, DslaHeads
+PyObject *g_device, *g_raw_stream, *g_parameter, *g_desc, *g_cache, *g_batch, *g_rope, *g_norm, *g_heads;
 struct Entries {
     decltype(&dsla_decode) decode;
     decltype(&dsla_decode_slots) decode_slots;
@@ -31,6 +31,10 @@ struct Entries {
     decltype(&dsla_cache_compact) cache_compact;
     decltype(&dsla_qk_rope) qk_rope;
     decltype(&dsla_attention_paged) attention_paged;
+    decltype(&dsla_residual_norm) residual_norm;
+    decltype(&dsla_head_norm) head_norm;
+    decltype(&dsla_quantize) quantize;
+    decltype(&dsla_project_fp8) project_fp8;
 } g_entry;
 
 // A tensor whose memory can be handed over; other subclasses answer for themselves in Python.
@@ -432,11 +436,116 @@ PyObject *attention_paged(PyObject *, PyObject *const *args, Py_ssize_t n)   // 
     });
 }
 
+at::ScalarType type_of_result(int32_t dtype) { return dtype == DSLA_E4M3 ? at::ScalarType::Float8_e4m3fn : type_of(dtype); }
+at::ScalarType type_of_scale(int32_t scale_type) { return scale_type == DSLA_SCALE_E8M0 ? at::ScalarType::Float8_e8m0fnu : at::kFloat; }
+
+PyObject *residual_norm(PyObject *, PyObject *const *args, Py_ssize_t n)   // norm, x, y, gate, x_out, h, h_scale
+{
+    return guarded(args, n, 7, [](Args &a) -> int {
+        const dsla_norm d = a.structure<dsla_norm>(0, g_norm);
+        const at::Tensor *t = gpu_tensor(a.o[1]);
+        if (!a.ok || !t || d.D <= 0) {
+            a.ok = false;
+            return 0;
+        }
+        const int64_t size = t->numel(), rows = size / d.D;
+        const at::ScalarType tx = type_of(d.x_dtype), ty = type_of(d.y_dtype);
+        void *x = a.here(1, tx, rows * d.D), *y = a.here(2, ty, size, true), *gate = a.here(3, ty, size, true), *x_out = a.here(4, tx, size, true);
+        void *h = a.here(5, type_of_result(d.h_dtype), size, true);
+        void *scale = a.here(6, type_of_scale(d.scale_type), rows * DSLA_SCALE_PITCH(static_cast<int64_t>(d.D)), true), *s = a.stream();
+        int status = 0;
+        CALL(status, a, g_entry.residual_norm(&d, rows, x, y, gate, x_out, h, scale, s));
+        return status;
+    });
+}
+
+PyObject *head_norm(PyObject *, PyObject *const *args, Py_ssize_t n)   // heads, o, gate, out, out_scale
+{
+    return guarded(args, n, 5, [](Args &a) -> int {
+        const dsla_heads d = a.structure<dsla_heads>(0, g_heads);
+        const at::Tensor *t = gpu_tensor(a.o[1]);
+        const int64_t width = static_cast<int64_t>(d.H) * d.d;
+        if (!a.ok || !t || width <= 0) {
+            a.ok = false;
+            return 0;
+        }
+        const int64_t size = t->numel(), rows = size / width;
+        const at::ScalarType type = type_of(d.io_dtype);
+        void *o = a.here(1, type, rows * width), *gate = a.here(2, type, size, true), *out = a.here(3, type_of_result(d.out_dtype), size);
+        void *scale = a.here(4, type_of_scale(d.scale_type), rows * DSLA_SCALE_PITCH(width), true), *s = a.stream();
+        int status = 0;
+        CALL(status, a, g_entry.head_norm(&d, rows, o, gate, out, scale, s));
+        return status;
+    });
+}
+
+PyObject *quantize(PyObject *, PyObject *const *args, Py_ssize_t n)   // x, q, scale, block_rows
+{
+    return guarded(args, n, 4, [](Args &a) -> int {
+        const at::Tensor *t = gpu_tensor(a.o[0]), *sc = gpu_tensor(a.o[2]);
+        const int64_t per = a.integer(3);
+        if (!a.ok || !t || !sc || t->dim() != 2 || t->size(1) > 0x7fffffff || (per != 1 && per != 128) ||
+            (t->scalar_type() != at::kBFloat16 && t->scalar_type() != at::kFloat)) {
+            a.ok = false;
+            return 0;
+        }
+        const int64_t rows = t->size(0), cols = t->size(1);
+        const int32_t st = sc->scalar_type() == at::kFloat ? DSLA_SCALE_F32 : DSLA_SCALE_E8M0;
+        void *x = a.here(0, t->scalar_type(), rows * cols), *q = a.here(1, at::ScalarType::Float8_e4m3fn, rows * cols);
+        void *scale = a.here(2, type_of_scale(st), (rows + per - 1) / per * DSLA_SCALE_PITCH(cols)), *s = a.stream();
+        int status = 0;
+        CALL(status, a, g_entry.quantize(rows, static_cast<int32_t>(cols), t->scalar_type() == at::kFloat ? DSLA_F32 : DSLA_BF16, static_cast<int32_t>(per), st,
+                                         x, q, scale, s));
+        return status;
+    });
+}
+
+PyObject *project_fp8(PyObject *, PyObject *const *args, Py_ssize_t n)   // x, x_scale, W, W_scale, outs, bias
+{
+    return guarded(args, n, 6, [](Args &a) -> int {
+        void *po[DSLA_MAX_PROJECTIONS];
+        int32_t widths[DSLA_MAX_PROJECTIONS];
+        const at::Tensor *x = gpu_tensor(a.o[0]), *w = gpu_tensor(a.o[2]), *sc = gpu_tensor(a.o[1]);
+        if (!x || !w || !sc || !PyList_CheckExact(a.o[4]) || x->dim() != 2 || w->dim() != 2 || x->size(1) > 0x7fffffff || w->size(1) != x->size(1)) {
+            a.ok = false;
+            return 0;
+        }
+        const int64_t M = x->size(0), K = x->size(1), n_out = PyList_GET_SIZE(a.o[4]), P = DSLA_SCALE_PITCH(K);
+        const int32_t st = sc->scalar_type() == at::kFloat ? DSLA_SCALE_F32 : DSLA_SCALE_E8M0;
+        if (n_out < 1 || n_out > DSLA_MAX_PROJECTIONS) {
+            a.ok = false;
+            return 0;
+        }
+        int64_t N = 0, blocks = 0;
+        at::ScalarType type = at::kFloat;
+        for (int64_t i = 0; i < n_out; ++i) {
+            const at::Tensor *t = gpu_tensor(PyList_GET_ITEM(a.o[4], i));
+            if (i == 0 && t) type = t->scalar_type();
+            if (!t || t->dim() != 2 || t->size(0) != M || t->size(1) > (1 << 24) || t->scalar_type() != type || t->get_device() != a.device() ||
+                (type != at::kFloat && type != at::kBFloat16)) {
+                a.ok = false;
+                return 0;
+            }
+            po[i] = t->data_ptr();
+            widths[i] = static_cast<int32_t>(t->size(1));
+            N += widths[i];
+            blocks += (widths[i] + 127) / 128;
+        }
+        void *px = a.here(0, at::ScalarType::Float8_e4m3fn, M * K), *xs = a.here(1, type_of_scale(st), M * P);
+        void *pw = a.here(2, at::ScalarType::Float8_e4m3fn, N * K), *ws = a.here(3, type_of_scale(st), blocks * P);
+        void *bias = a.here(5, at::kFloat, N, true), *s = a.stream();
+        int status = 0;
+        CALL(status, a, g_entry.project_fp8(M, static_cast<int32_t>(K), static_cast<int32_t>(n_out), widths, st, px, xs, pw, ws, static_cast<float *>(bias),
+                                            type == at::kFloat ? DSLA_F32 : DSLA_BF16, po, s));
+        return status;
+    });
+}
+
 // device, raw_stream, parameter type, the structures' types, addresses of the entry points in the order of Entries
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     constexpr int kEntries = sizeof(Entries) / sizeof(void *);
-    constexpr int kObjects = 7;
+    constexpr int kObjects = 9;
     if (n != kObjects + kEntries) {
         PyErr_SetString(PyExc_TypeError, "bind: number of arguments");
         return nullptr;
@@ -447,7 +556,7 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
         if (PyErr_Occurred()) return nullptr;
     }
     std::memcpy(&g_entry, p, sizeof(p));
-    PyObject **to[kObjects] = {&g_device, &g_raw_stream, &g_parameter, &g_desc, &g_cache, &g_batch, &g_rope};
+    PyObject **to[kObjects] = {&g_device, &g_raw_stream, &g_parameter, &g_desc, &g_cache, &g_batch, &g_rope, &g_norm, &g_heads};
     for (int i = 0; i < kObjects; ++i) {
         Py_INCREF(args[i]);
         Py_XDECREF(*to[i]);
@@ -459,7 +568,8 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {METHOD(bind), METHOD(decode), METHOD(decode_slots), METHOD(prefill), METHOD(prefill_varlen), METHOD(attention_decode),
                            METHOD(attention_prefill), METHOD(project), METHOD(cache_extend), METHOD(cache_fork), METHOD(cache_truncate), METHOD(cache_accept),
-                           METHOD(cache_compact), METHOD(qk_rope), METHOD(attention_paged), {nullptr, nullptr, 0, nullptr}};
+                           METHOD(cache_compact), METHOD(qk_rope), METHOD(attention_paged), METHOD(residual_norm), METHOD(head_norm),
+                           METHOD(quantize), METHOD(project_fp8), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,378 @@
+// What stands around the layer (include/dsla.h): the norms, gate and residual scale of a block's border, the norm and gate of the
+// read-out's heads, and values to e4m3 with block scales.  All of them are bound by memory: every value is read once, kept in
+// registers and written once, 8 values of a lane at a time; sums and largest magnitudes go through the lanes.  A block of 128
+// columns is 16 lanes of 8, one row of the cross-lane operations.
+#include "fp8_common.h"
+
+namespace dsla {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ void load8(const bf16_t *p, float (&f)[8])
+{
+    const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(w[i] << 16);
+        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void load8(const float *p, float (&f)[8])
+{
+    const f32x4 a = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p)), b = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p + 4));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[i] = a[i];
+        f[4 + i] = b[i];
+    }
+}
+__device__ __forceinline__ void load8_kept(const float *p, float (&f)[8])   // weights: every row reads them again
+{
+    const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[i] = a[i];
+        f[4 + i] = b[i];
+    }
+}
+__device__ __forceinline__ void store8(bf16_t *p, const float (&f)[8])
+{
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = f32_to_bf16_bits(f[2 * i]) | static_cast<uint32_t>(f32_to_bf16_bits(f[2 * i + 1])) << 16;
+    __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(p));
+}
+__device__ __forceinline__ void store8(float *p, const float (&f)[8])
+{
+    __builtin_nontemporal_store(f32x4{f[0], f[1], f[2], f[3]}, reinterpret_cast<f32x4 *>(p));
+    __builtin_nontemporal_store(f32x4{f[4], f[5], f[6], f[7]}, reinterpret_cast<f32x4 *>(p + 4));
+}
+
+// The value of another lane of the 16: N places round.
+template <int N>
+__device__ __forceinline__ float row_rotate(float x)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + N, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float max16(float x)
+{
+    x = fmaxf(x, row_rotate<8>(x));
+    x = fmaxf(x, row_rotate<4>(x));
+    x = fmaxf(x, row_rotate<2>(x));
+    return fmaxf(x, row_rotate<1>(x));
+}
+__device__ __forceinline__ float sum16(float x)
+{
+    x += row_rotate<8>(x);
+    x += row_rotate<4>(x);
+    x += row_rotate<2>(x);
+    return x + row_rotate<1>(x);
+}
+
+// Sum over the T threads of a workgroup, or over a wavefront (T = 64).
+template <int T>
+__device__ __forceinline__ float sum_all(float x, float *s)
+{
+    x = sum16(x);
+    x += __shfl_xor(x, 16);
+    x += __shfl_xor(x, 32);
+    if (T == 64) return x;
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+    __syncthreads();
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < T / 64; ++i) t += s[i];
+    return t;
+}
+
+__device__ __forceinline__ float activated(float z, int act)
+{
+    if (act == DSLA_ACT_NONE) return z;
+    const float t = expf(-fabsf(z));   // (of a negative number: a large gate does not overflow)
+    const float top = z < 0.f ? t : 1.f;
+    return (act == DSLA_ACT_SIGMOID ? top : z * top) / (1.f + t);
+}
+
+// 8 values of a lane to where they go: as they are, or as e4m3 with the scale of the block that the lane's row of 16 holds (lanes without
+// values take part with zeros).
+struct Result {
+    void *p, *scale;
+    int dtype, scale_type, pitch;
+};
+template <bool E8M0>
+__device__ __forceinline__ void store_block(const Result &o, const float (&f)[8], bool valid, size_t at, long long row, int block)
+{
+    float a = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a = fmaxf(a, finite_magnitude(f[i]));
+    const BlockScale<E8M0> s(max16(a));
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = in_range(f[i], s.inverse);
+    if (valid) __builtin_nontemporal_store(u32x2{e4m3x4(v[0], v[1], v[2], v[3]), e4m3x4(v[4], v[5], v[6], v[7])},
+                                           reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(o.p) + at));
+    if (valid && threadIdx.x % 16 == 0) s.store(o.scale, static_cast<size_t>(row) * o.pitch + block);
+}
+__device__ __forceinline__ void store_result(const Result &o, const float (&f)[8], bool valid, size_t at, long long row, int block)
+{
+    if (o.dtype == DSLA_E4M3) {
+        if (o.scale_type == DSLA_SCALE_E8M0) store_block<true>(o, f, valid, at, row, block);
+        else store_block<false>(o, f, valid, at, row, block);
+    } else if (valid) {
+        if (o.dtype == DSLA_BF16) store8(static_cast<bf16_t *>(o.p) + at, f);
+        else store8(static_cast<float *>(o.p) + at, f);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// A block's border
+// ---------------------------------------------------------------------------------------------------------------
+struct BorderArgs {
+    const void *x, *y, *gate;
+    void *x_out;
+    const float *post_weight, *pre_weight;
+    Result h;
+    long long rows;
+    int D, act;
+    float eps, residual_scale;
+};
+
+// T threads to a row, NV times 8 values to a thread: value 8 (T c + t) .. + 7 of the row for c < NV.  T = 64: a wavefront to a row, four rows to a workgroup.
+template <int T, int NV, class TX, class TY>
+__global__ __launch_bounds__(T == 64 ? 256 : T) void residual_norm_kernel(BorderArgs a)
+{
+    __shared__ float s_post[T / 64], s_pre[T / 64];
+    const int t = T == 64 ? threadIdx.x & 63 : threadIdx.x;
+    const long long row = T == 64 ? blockIdx.x * 4LL + (threadIdx.x >> 6) : blockIdx.x;
+    if (row >= a.rows) return;   // (wavefronts of T = 64 share nothing)
+    const size_t base = static_cast<size_t>(row) * a.D;
+    float r[NV][8], u[NV][8], g[NV][8];
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        const int col = 8 * (T * c + t);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[c][i] = u[c][i] = g[c][i] = 0.f;
+        if (col >= a.D) continue;
+        load8(static_cast<const TX *>(a.x) + base + col, r[c]);
+        if (a.y) load8(static_cast<const TY *>(a.y) + base + col, u[c]);
+        if (a.gate) load8(static_cast<const TY *>(a.gate) + base + col, g[c]);
+    }
+    float factor = a.residual_scale;
+    if (a.post_weight) {
+        float q = 0.f;
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q += u[c][i] * u[c][i];
+        q = sum_all<T>(q, s_post);
+        const float inv = 1.f / sqrtf(q / a.D + a.eps);
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const int col = 8 * (T * c + t);
+            if (col >= a.D) continue;
+            float w[8];
+            load8_kept(a.post_weight + col, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[c][i] *= inv * w[i];
+        }
+    }
+    float q = 0.f;
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        const int col = 8 * (T * c + t);
+        if (col >= a.D) continue;
+        if (a.y) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r[c][i] += factor * (a.gate ? u[c][i] * activated(g[c][i], a.act) : u[c][i]);
+        }
+        if (a.x_out) store8(static_cast<TX *>(a.x_out) + base + col, r[c]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q += r[c][i] * r[c][i];
+    }
+    if (!a.h.p) return;
+    float inv = 1.f;
+    if (a.pre_weight) {
+        q = sum_all<T>(q, s_pre);
+        inv = 1.f / sqrtf(q / a.D + a.eps);
+    }
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        const int col = 8 * (T * c + t);
+        const bool valid = col < a.D;
+        if (valid && a.pre_weight) {
+            float w[8];
+            load8_kept(a.pre_weight + col, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r[c][i] *= inv * w[i];
+        }
+        store_result(a.h, r[c], valid, base + col, row, col >> 7);
+    }
+}
+
+template <int T, int NV>
+void launch_border(ProfileScope &ps, const BorderArgs &a, bool x32, bool y32, hipStream_t stream)
+{
+    const dim3 grid(static_cast<unsigned>(T == 64 ? (a.rows + 3) / 4 : a.rows)), block(T == 64 ? 256 : T);
+    if (x32 && y32) DSLA_LAUNCH(ps, (residual_norm_kernel<T, NV, float, float>), grid, block, 0, stream, a);
+    else if (x32) DSLA_LAUNCH(ps, (residual_norm_kernel<T, NV, float, bf16_t>), grid, block, 0, stream, a);
+    else if (y32) DSLA_LAUNCH(ps, (residual_norm_kernel<T, NV, bf16_t, float>), grid, block, 0, stream, a);
+    else DSLA_LAUNCH(ps, (residual_norm_kernel<T, NV, bf16_t, bf16_t>), grid, block, 0, stream, a);
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Heads, and plain rows
+// ---------------------------------------------------------------------------------------------------------------
+struct RowsArgs {
+    const void *x, *gate;
+    const float *weight;   // [d], null: no norm
+    Result o;
+    long long blocks;      // rows * blocks of a row
+    int cols, per_row, act;
+    float eps;
+};
+
+// 16 lanes to a block of 128 columns of a row: one head of 128, two of 64, or 128 plain values.
+template <int D, class TIO>
+__global__ __launch_bounds__(256) void rows_kernel(RowsArgs a)
+{
+    const int l = threadIdx.x & 15;
+    const long long n = blockIdx.x * 16LL + (threadIdx.x >> 4);
+    const bool there = n < a.blocks;
+    const long long row = there ? n / a.per_row : 0;
+    const int block = there ? static_cast<int>(n - row * a.per_row) : 0, col = 128 * block + 8 * l;
+    const bool valid = there && col < a.cols;
+    const size_t at = static_cast<size_t>(row) * a.cols + col;
+    float f[8] = {}, g[8] = {};
+    if (valid) {
+        load8(static_cast<const TIO *>(a.x) + at, f);
+        if (a.gate) load8(static_cast<const TIO *>(a.gate) + at, g);
+    }
+    if (D && a.weight) {
+        float q = 0.f, w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q += f[i] * f[i];
+        if (D == 128) {
+            q = sum16(q);
+        } else {   // 8 lanes: l ^ 4, l ^ 2, l ^ 1
+            q += __shfl_xor(q, 4);
+            q += __shfl_xor(q, 2);
+            q += __shfl_xor(q, 1);
+        }
+        const float inv = 1.f / sqrtf(q / D + a.eps);
+        load8_kept(a.weight + (8 * l) % D, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] *= inv * w[i];
+    }
+    if (a.gate) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] *= activated(g[i], a.act);
+    }
+    store_result(a.o, f, valid, at, row, block);
+}
+
+template <int D>
+void launch_rows(ProfileScope &ps, const RowsArgs &a, bool f32, hipStream_t stream)
+{
+    const dim3 grid(static_cast<unsigned>((a.blocks + 15) / 16));
+    if (f32) DSLA_LAUNCH(ps, (rows_kernel<D, float>), grid, dim3(256), 0, stream, a);
+    else DSLA_LAUNCH(ps, (rows_kernel<D, bf16_t>), grid, dim3(256), 0, stream, a);
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Blocks of 128 x 128
+// ---------------------------------------------------------------------------------------------------------------
+struct SquareArgs {
+    const void *x;
+    uint8_t *q;
+    void *scale;
+    long long rows;
+    int cols, pitch, per_row;
+};
+
+template <class TIO, bool E8M0>
+__global__ __launch_bounds__(256) void square_kernel(SquareArgs a)
+{
+    __shared__ float s_max[16];
+    const int l = threadIdx.x & 15, r0 = threadIdx.x >> 4;
+    const long long brow = blockIdx.x / a.per_row;
+    const int bcol = static_cast<int>(blockIdx.x - brow * a.per_row), col = 128 * bcol + 8 * l;
+    float f[8][8], m = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        const long long row = 128 * brow + 16 * c + r0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[c][i] = 0.f;
+        if (row < a.rows && col < a.cols) load8(static_cast<const TIO *>(a.x) + static_cast<size_t>(row) * a.cols + col, f[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, finite_magnitude(f[c][i]));
+    m = max16(m);
+    if (l == 0) s_max[r0] = m;
+    __syncthreads();
+    const BlockScale<E8M0> s(max16(s_max[l]));
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        const long long row = 128 * brow + 16 * c + r0;
+        if (row >= a.rows || col >= a.cols) continue;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = in_range(f[c][i], s.inverse);
+        __builtin_nontemporal_store(u32x2{e4m3x4(v[0], v[1], v[2], v[3]), e4m3x4(v[4], v[5], v[6], v[7])},
+                                    reinterpret_cast<u32x2 *>(a.q + static_cast<size_t>(row) * a.cols + col));
+    }
+    if (threadIdx.x == 0) s.store(a.scale, static_cast<size_t>(brow) * a.pitch + bcol);
+}
+
+Result result_of(void *p, void *scale, int dtype, int scale_type, int cols) { return Result{p, scale, dtype, scale_type, scale_pitch(cols)}; }
+}  // namespace
+
+hipError_t launch_residual_norm(const dsla_norm &n, int64_t rows, const void *x, const void *y, const void *gate, void *x_out, void *h, void *h_scale,
+                                hipStream_t stream)
+{
+    BorderArgs a{x, y, gate, x_out, n.post_weight, n.pre_weight, result_of(h, h_scale, n.h_dtype, n.scale_type, n.D), rows, n.D, n.gate_act, n.eps, n.residual_scale};
+    const bool x32 = n.x_dtype == DSLA_F32, y32 = n.y_dtype == DSLA_F32;
+    ProfileScope ps(DSLA_KERNEL_RESIDUAL_NORM, stream);
+    if (n.D <= 512) launch_border<64, 1>(ps, a, x32, y32, stream);
+    else if (n.D <= 1024) launch_border<64, 2>(ps, a, x32, y32, stream);
+    else if (n.D <= 2048) launch_border<256, 1>(ps, a, x32, y32, stream);
+    else if (n.D <= 4096) launch_border<256, 2>(ps, a, x32, y32, stream);
+    else if (n.D <= 8192) launch_border<256, 4>(ps, a, x32, y32, stream);
+    else if (n.D <= 16384) launch_border<1024, 2>(ps, a, x32, y32, stream);
+    else launch_border<1024, 4>(ps, a, x32, y32, stream);
+    return hipGetLastError();
+}
+
+hipError_t launch_head_norm(const dsla_heads &n, int64_t rows, const void *o, const void *gate, void *out, void *out_scale, hipStream_t stream)
+{
+    const int cols = n.H * n.d, per_row = (cols + 127) / 128;
+    RowsArgs a{o, gate, n.weight, result_of(out, out_scale, n.out_dtype, n.scale_type, cols), rows * per_row, cols, per_row, n.gate_act, n.eps};
+    ProfileScope ps(DSLA_KERNEL_HEAD_NORM, stream);
+    if (n.d == 128) launch_rows<128>(ps, a, n.io_dtype == DSLA_F32, stream);
+    else launch_rows<64>(ps, a, n.io_dtype == DSLA_F32, stream);
+    return hipGetLastError();
+}
+
+hipError_t launch_quantize(int64_t rows, int cols, int in_dtype, int block_rows, int scale_type, const void *x, void *q, void *scale, hipStream_t stream)
+{
+    const int per_row = (cols + 127) / 128;
+    ProfileScope ps(DSLA_KERNEL_QUANTIZE, stream);
+    if (block_rows == 1) {
+        RowsArgs a{x, nullptr, nullptr, result_of(q, scale, DSLA_E4M3, scale_type, cols), rows * per_row, cols, per_row, DSLA_ACT_NONE, 0.f};
+        launch_rows<0>(ps, a, in_dtype == DSLA_F32, stream);
+    } else {
+        const SquareArgs a{x, static_cast<uint8_t *>(q), scale, rows, cols, scale_pitch(cols), per_row};
+        const dim3 grid(static_cast<unsigned>((rows + 127) / 128 * per_row));
+        if (in_dtype == DSLA_F32 && scale_type == DSLA_SCALE_E8M0) DSLA_LAUNCH(ps, (square_kernel<float, true>), grid, dim3(256), 0, stream, a);
+        else if (in_dtype == DSLA_F32) DSLA_LAUNCH(ps, (square_kernel<float, false>), grid, dim3(256), 0, stream, a);
+        else if (scale_type == DSLA_SCALE_E8M0) DSLA_LAUNCH(ps, (square_kernel<bf16_t, true>), grid, dim3(256), 0, stream, a);
+        else DSLA_LAUNCH(ps, (square_kernel<bf16_t, false>), grid, dim3(256), 0, stream, a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace dsla

@@ -1,0 +1,453 @@
+// The projections with e4m3 operands and a scale for each block of 128 (include/dsla.h: dsla_project_fp8):
+//     out_j[m][c] = sum_b sx[m][b] sw[c / 128][b] sum_{k in block b} x[m][k] W_j[c][k] (+ bias_j[c])
+// One MFMA of 16 x 16 x 128 covers a block of K.  E8M0 scales ride in the instruction; with fp32 scales it starts from zero and the
+// block's sum is added times sx sw.  Columns are counted in blocks of 128 that never cross an output, as the scales of W are.
+#include "fp8_common.h"
+#include "project_common.h"
+
+#include <type_traits>
+
+namespace dsla {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+struct Fp8Args {
+    const uint8_t *x, *w;
+    const void *xs, *ws;
+    const float *bias;
+    void *out[DSLA_MAX_PROJECTIONS];
+    int width[DSLA_MAX_PROJECTIONS];
+    long long M;
+    int K, pitch, out_f32;
+};
+
+// A block of 128 columns: its output, where it starts there and in W, and how many columns exist.
+struct Columns {
+    int j, c0, row, count;
+};
+__device__ __forceinline__ Columns columns_of(const Fp8Args &a, int block)
+{
+    Columns c{0, 0, 0, 0};
+    int n = (a.width[0] + 127) / 128;
+    while (block >= n) {
+        block -= n;
+        c.row += a.width[c.j++];
+        n = (a.width[c.j] + 127) / 128;
+    }
+    c.c0 = 128 * block;
+    c.row += c.c0;
+    c.count = a.width[c.j] - c.c0 < 128 ? a.width[c.j] - c.c0 : 128;
+    return c;
+}
+
+__device__ __forceinline__ u32x2 pack4(f32x4 v)
+{
+    return u32x2{f32_to_bf16_bits(v[0]) | static_cast<uint32_t>(f32_to_bf16_bits(v[1])) << 16, f32_to_bf16_bits(v[2]) | static_cast<uint32_t>(f32_to_bf16_bits(v[3])) << 16};
+}
+__device__ __forceinline__ void store4(const Fp8Args &a, const Columns &c, long long m, int col, f32x4 v)   // columns col .. col + 3 of the block
+{
+    if (a.bias) v += *reinterpret_cast<const f32x4 *>(a.bias + c.row + col);
+    const size_t at = static_cast<size_t>(m) * a.width[c.j] + c.c0 + col;
+    if (a.out_f32) {
+        *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out[c.j]) + at) = v;
+    } else {
+        *reinterpret_cast<u32x2 *>(static_cast<bf16_t *>(a.out[c.j]) + at) = pack4(v);
+    }
+}
+
+constexpr int kOne = 127;   // E8M0
+
+__device__ __forceinline__ i32x8 join(u32x4 a, u32x4 b)
+{
+    return i32x8{static_cast<int>(a[0]), static_cast<int>(a[1]), static_cast<int>(a[2]), static_cast<int>(a[3]),
+                 static_cast<int>(b[0]), static_cast<int>(b[1]), static_cast<int>(b[2]), static_cast<int>(b[3])};
+}
+
+// The product of two fragments from zero.  EXACT: e4m3 is bf16 with fewer bits, and the bf16 instructions add in fp32; the e4m3 ones add in
+// groups of eight products and drop what is below 2^-14 of a group's largest (random operands: 1.4e-5 of the result's 2-norm against
+// 1e-8), which results in bf16 do not show and results in fp32 are asked for.
+__device__ __forceinline__ bf16x8 wide(uint32_t a, uint32_t b)
+{
+    const bf16x2 w[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true)};
+    return bf16x8{w[0][0], w[0][1], w[1][0], w[1][1], w[2][0], w[2][1], w[3][0], w[3][1]};
+}
+template <bool EXACT>
+struct Operand {
+    i32x8 f;
+    __device__ __forceinline__ void set(i32x8 x) { f = x; }
+};
+template <>
+struct Operand<true> {
+    bf16x8 f[4];
+    __device__ __forceinline__ void set(i32x8 x)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = wide(x[2 * i], x[2 * i + 1]);
+    }
+};
+__device__ __forceinline__ f32x4 product(const Operand<false> &w, const Operand<false> &x)
+{
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.f, x.f, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, kOne, 0, kOne);
+}
+__device__ __forceinline__ f32x4 product(const Operand<true> &w, const Operand<true> &x)
+{
+    f32x4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.f[i], x.f[i], t, 0, 0, 0);
+    return t;
+}
+// What a block's products are multiplied by: two numbers, or 2^exponent (two bytes reach beyond fp32; 255 is NaN).
+template <bool E8M0>
+struct Factor {
+    float f;
+    int exponent = 0;
+    __device__ __forceinline__ Factor(uint32_t x, uint32_t w)
+    {
+        if (E8M0) {
+            f = x == 255u || w == 255u ? __builtin_nanf("") : 1.f;
+            exponent = static_cast<int>(x + w) - 2 * kOne;
+        } else {
+            f = __uint_as_float(x) * __uint_as_float(w);
+        }
+    }
+    __device__ __forceinline__ void add(f32x4 &acc, f32x4 t) const
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += (E8M0 ? ldexpf(t[e], exponent) : t[e]) * f;
+    }
+};
+
+template <bool E8M0, bool EXACT>
+__global__ __launch_bounds__(256) void project_fp8_kernel(Fp8Args a, unsigned tiles_m)
+{
+    __shared__ __attribute__((aligned(16))) u32x4 sx[128 * 8], sw[128 * 8];
+    const int block = blockIdx.x / tiles_m;
+    const long long m0 = 128LL * (blockIdx.x - static_cast<unsigned>(block) * tiles_m);
+    const Columns cb = columns_of(a, block);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4;
+    const int wm = wave >> 1, wn = wave & 1;
+    f32x4 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int nk = (a.K + 127) / 128;
+    for (int ks = 0; ks < nk; ++ks) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int n = tid + 256 * i, row = n >> 3, c = n & 7, k = 128 * ks + 16 * c, at = row * 8 + (c ^ ((row >> 1) & 7));
+            sx[at] = m0 + row < a.M && k < a.K ? *reinterpret_cast<const u32x4 *>(a.x + static_cast<size_t>(m0 + row) * a.K + k) : u32x4{0, 0, 0, 0};
+            sw[at] = row < cb.count && k < a.K ? *reinterpret_cast<const u32x4 *>(a.w + static_cast<size_t>(cb.row + row) * a.K + k) : u32x4{0, 0, 0, 0};
+        }
+        __syncthreads();
+        Operand<EXACT> fx[4], fw[4];
+        uint32_t scale_x[4];
+        auto scale_at = [&](const void *p, size_t row) -> uint32_t {
+            return E8M0 ? static_cast<const uint8_t *>(p)[row * a.pitch + ks] : static_cast<const uint32_t *>(p)[row * a.pitch + ks];
+        };
+        const uint32_t scale_w = scale_at(a.ws, block);   // (a row of scales for every block of columns)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int rx = 64 * wm + 16 * i + r, rw = 64 * wn + 16 * i + r;
+            fx[i].set(join(sx[rx * 8 + (g ^ ((rx >> 1) & 7))], sx[rx * 8 + ((4 + g) ^ ((rx >> 1) & 7))]));
+            fw[i].set(join(sw[rw * 8 + (g ^ ((rw >> 1) & 7))], sw[rw * 8 + ((4 + g) ^ ((rw >> 1) & 7))]));
+            scale_x[i] = m0 + rx < a.M ? scale_at(a.xs, m0 + rx) : 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const Factor<E8M0> factor(scale_x[i], scale_w);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (E8M0 && !EXACT) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[j].f, fx[i].f, acc[i][j], 0, 0, 0, scale_w, 0, scale_x[i]);
+                else factor.add(acc[i][j], product(fw[j], fx[i]));
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const long long m = m0 + 64 * wm + 16 * i + r;
+        if (m >= a.M) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int col = 64 * wn + 16 * j + 4 * g;
+            if (col < cb.count) store4(a, cb, m, col, acc[i][j]);
+        }
+    }
+}
+// 16 bytes per lane from a buffer (lane offset `voff`, uniform offset `soff`) into LDS at `lds` (uniform) + 16 * lane
+__device__ __forceinline__ void buffer_load_lds16(__amdgpu_buffer_rsrc_t res, char *lds, uint32_t voff, int soff)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void *)(lds), 16, voff, soff, 0, 0);
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const uint8_t *p, size_t offset, long long bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p + offset), 0, static_cast<int>(bytes), 0x00020000);
+}
+constexpr uint32_t kNowhere = 0x80000000u;   // an offset past the end of every buffer here: zeros
+
+// ---------------------------------------------------------------------------------------------------------------
+// 256 x 256 tiles
+// ---------------------------------------------------------------------------------------------------------------
+// The product of two fragments added to what stands in the accumulation registers, with scales from byte B of two registers.  (The
+// compiler gives the result registers of its own and copies, which 256 accumulators leave no room for.)
+template <int B>
+__device__ __forceinline__ void product_in_place(f32x4 &acc, const i32x8 &w, const i32x8 &x, uint32_t scale_w, uint32_t scale_x)
+{
+    if (B) asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[0,0,0]" : "+a"(acc) : "v"(w), "v"(x), "v"(scale_w), "v"(scale_x));
+    else asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]" : "+a"(acc) : "v"(w), "v"(x), "v"(scale_w), "v"(scale_x));
+}
+
+template <bool E8M0>
+__global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8Args a, int tiles_m, int tiles_n, int blocks, int group, long long per_xcd)
+{
+    constexpr int WN = E8M0 ? 2 : 4, NW = 2 * WN;    // wavefronts along the columns, in all
+    constexpr int NJ = 16 / WN;                       // 16 x 16 tiles of a wavefront along the columns; 8 along the rows
+    constexpr int OPB = 256 * 128;                    // bytes of an operand's tile and step
+    constexpr int LOADS = 32 / NW;                    // instructions of a wavefront per operand and step
+    __shared__ __attribute__((aligned(1024))) char st0[2 * OPB];
+    __shared__ __attribute__((aligned(1024))) char st1[2 * OPB];
+    int tm, tn;
+    if (!tile_of(tiles_m, tiles_n, group, per_xcd, tm, tn)) return;
+    const long long m0 = 256LL * tm;
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
+    const int second = 2 * tn + 1 < blocks ? 2 * tn + 1 : 2 * tn;
+    const Columns cb0 = columns_of(a, 2 * tn);
+    Columns cb1 = columns_of(a, second);
+    if (second == 2 * tn) cb1.count = 0;
+
+    // ---- loading: an instruction fills 8 rows of 128 bytes; lane l fills position l % 8 of row l / 8, where piece c of a row R sits at
+    // c ^ (R / 2 % 8).  The pieces behind K are asked for nowhere, and come as zeros, as rows that do not exist do. ----
+    const long long rows_a = a.M - m0 < 256 ? a.M - m0 : 256;
+    const __amdgpu_buffer_rsrc_t res_x = buffer_of(a.x, static_cast<size_t>(m0) * a.K, rows_a * a.K);
+    const __amdgpu_buffer_rsrc_t res_w0 = buffer_of(a.w, static_cast<size_t>(cb0.row) * a.K, static_cast<long long>(cb0.count) * a.K);
+    const __amdgpu_buffer_rsrc_t res_w1 = buffer_of(a.w, static_cast<size_t>(cb1.row) * a.K, static_cast<long long>(cb1.count) * a.K);
+    const int piece = (lane & 7) ^ (((8 * wave + (lane >> 3)) >> 1) & 7);   // (the same for all of its rows: they are 8 NW apart)
+    uint32_t voff[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) voff[i] = static_cast<uint32_t>(8 * (wave + NW * i) + (lane >> 3)) * static_cast<uint32_t>(a.K) + 16 * piece;
+    auto fetch = [&](char *st, int ks, int i) {   // instruction i of both operands
+        const int k0 = 128 * ks, n = wave + NW * i;
+        const bool there = 16 * piece < a.K - k0;
+        buffer_load_lds16(res_x, st + n * 1024, there ? voff[i] : kNowhere, k0);
+        if (i < LOADS / 2) buffer_load_lds16(res_w0, st + OPB + n * 1024, there ? voff[i] : kNowhere, k0);
+        else buffer_load_lds16(res_w1, st + OPB + n * 1024, there ? voff[i - LOADS / 2] : kNowhere, k0);
+    };
+
+    // ---- scales: of two steps as bytes, or of one as numbers, for every row of the wavefront, and for its block of columns ----
+    const int nk = (a.K + 127) / 128;
+    constexpr int SB = E8M0 ? 1 : 4;
+    const __amdgpu_buffer_rsrc_t res_xs = buffer_of(static_cast<const uint8_t *>(a.xs), static_cast<size_t>(m0) * a.pitch * SB, rows_a * a.pitch * SB);
+    const uint32_t xs_row = static_cast<uint32_t>(128 * wm + r) * static_cast<uint32_t>(a.pitch * SB), xs_step = 16u * static_cast<uint32_t>(a.pitch * SB);
+    const uint8_t *ws = static_cast<const uint8_t *>(a.ws) + static_cast<size_t>(wn / (WN / 2) ? second : 2 * tn) * a.pitch * SB;
+    struct Scales {
+        uint32_t x[8], w;
+    };
+    // E8M0: of steps ks and ks + 1 (ks even).  What stands behind a row's last scale may be anything, and its products are of zeros: one.
+    auto read_scales = [&](Scales &s, int ks) {
+        const int at = (ks < nk ? ks : nk - 1) * SB;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (E8M0) s.x[i] = __builtin_amdgcn_raw_buffer_load_b16(res_xs, xs_row + i * xs_step, at & ~1, 0);
+            else s.x[i] = __builtin_amdgcn_raw_buffer_load_b32(res_xs, xs_row + i * xs_step, at, 0);
+        }
+        s.w = E8M0 ? *reinterpret_cast<const uint16_t *>(ws + (at & ~1)) : *reinterpret_cast<const uint32_t *>(ws + at);
+    };
+    auto close_scales = [&](Scales &s, int ks) {
+        const uint32_t keep = ks + 1 < nk ? 0xffffu : 0xffu, put = ks + 1 < nk ? 0u : 0x7f00u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s.x[i] = (s.x[i] & keep) | put;
+        s.w = (s.w & keep) | put;
+    };
+
+    // ---- fragments: lane (r, g) holds row r, pieces g and 4 + g ----
+    const uint32_t pos = static_cast<uint32_t>(g ^ ((r >> 1) & 7)) << 4;
+    const uint32_t fx = static_cast<uint32_t>(128 * wm + r) * 128, fw = OPB + static_cast<uint32_t>(16 * NJ * wn + r) * 128;
+    auto fragment = [&](const char *st, uint32_t row) {
+        return join(*reinterpret_cast<const u32x4 *>(st + row + pos), *reinterpret_cast<const u32x4 *>(st + row + (pos ^ 64)));
+    };
+    f32x4 acc[8][NJ];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (E8M0) {
+        // A step multiplies rows of tiles 0 .. 2 column by column, then rows 3 and 4, then 5 .. 7 column by column.  On entry the fragments of
+        // the columns and of rows 0 .. 2 are in registers or on their way; the other rows' are read under the first products.  The barrier in
+        // front of the last rows says that everybody has what it needs of `cur`, which takes step ks + 2, and that step ks + 1 has landed in
+        // `nxt`: as the last rows are done with a column, the next step's fragment takes its registers.
+        i32x8 w[NJ], x[8];
+        auto product = [&](int i, int j, const Scales &s, auto odd) {
+            product_in_place<decltype(odd)::value>(acc[i][j], w[j], x[i], s.w, s.x[i]);
+        };
+        auto step = [&](const Scales &s, Scales &ns, char *cur, char *nxt, int ks, auto odd) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                if (j < 5) x[3 + j] = fragment(cur, fx + (3 + j) * 2048);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) product(i, j, s, odd);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int i = 3; i < 5; ++i)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) product(i, j, s, odd);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            if (decltype(odd)::value == 0) read_scales(ns, ks + 2);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                fetch(cur, ks + 2, j);
+#pragma unroll
+                for (int i = 5; i < 8; ++i) product(i, j, s, odd);
+                w[j] = fragment(nxt, fw + j * 2048);
+                if (j < 3) x[j] = fragment(nxt, fx + j * 2048);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        Scales s0, s1;
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) fetch(st0, 0, j);
+        read_scales(s0, 0);
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) fetch(st1, 1, j);
+        __builtin_amdgcn_s_waitcnt(0x0070);
+        __builtin_amdgcn_s_barrier();
+#pragma unroll
+        for (int i = 0; i < 3; ++i) x[i] = fragment(st0, fx + i * 2048);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) w[j] = fragment(st0, fw + j * 2048);
+        for (int ks = 0; ks < nk; ks += 2) {
+            close_scales(s0, ks);
+            asm volatile("s_nop 1" : "+v"(s0.w), "+v"(s0.x[0]), "+v"(s0.x[1]), "+v"(s0.x[2]), "+v"(s0.x[3]), "+v"(s0.x[4]), "+v"(s0.x[5]), "+v"(s0.x[6]), "+v"(s0.x[7]));
+            step(s0, s1, st0, st1, ks, std::integral_constant<int, 0>{});
+            step(s0, s1, st1, st0, ks + 1, std::integral_constant<int, 1>{});
+            s0 = s1;
+        }
+        asm volatile("s_nop 15");
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) asm volatile("" : "+a"(acc[i][j]));
+    } else {
+        // Two wavefronts to a SIMD, one buffer read while the other fills; a row of tiles' sums are added under the next row's products.
+        auto step = [&](const Scales &s, Scales &ns, char *cur, char *nxt, int ks) {
+            __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
+            __builtin_amdgcn_s_barrier();         // step ks has landed, and everybody is done with the other buffer
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) fetch(nxt, ks + 1, i);
+            read_scales(ns, ks + 1);
+            i32x8 w[NJ];
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) w[j] = fragment(cur, fw + j * 2048);
+            f32x4 t[2][NJ];
+#pragma unroll
+            for (int i = 0; i <= 8; ++i) {
+                if (i < 8) {
+                    const i32x8 x = fragment(cur, fx + i * 2048);
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j)
+                        t[i & 1][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[j], x, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, kOne, 0, kOne);
+                }
+                if (i > 0) {
+                    const float scale = __uint_as_float(s.x[i - 1]) * __uint_as_float(s.w);
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i - 1][j][e] += t[(i - 1) & 1][j][e] * scale;
+                }
+            }
+        };
+        Scales s0, s1;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) fetch(st0, 0, i);
+        read_scales(s0, 0);
+        int ks = 0;
+        for (; ks + 1 < nk; ks += 2) {
+            step(s0, s1, st0, st1, ks);
+            step(s1, s0, st1, st0, ks + 1);
+        }
+        if (ks < nk) step(s0, s1, st0, st1, ks);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0070);
+    __builtin_amdgcn_s_barrier();   // nothing in flight; everybody is done reading
+
+    // ---- results: each wavefront turns its part round in LDS, 128 rows of 16 NJ columns in bf16, the 16-byte piece c of row R at position
+    // c ^ (R % pieces), so that it leaves as whole rows ----
+    constexpr int PPR = 2 * NJ, ROWB = 32 * NJ;
+    const Columns c = wn / (WN / 2) ? cb1 : cb0;
+    const int first = (16 * NJ * wn) % 128;   // the wavefront's first column in its block
+    char *epi = (wave < NW / 2 ? st0 : st1) + (wave % (NW / 2)) * 128 * ROWB;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const int col = 16 * j + 4 * g, row = 16 * i + r, at = col >> 3;
+            f32x4 v = acc[i][j];
+            if (a.bias && first + col < c.count) v += *reinterpret_cast<const f32x4 *>(a.bias + c.row + first + col);
+            *reinterpret_cast<u32x2 *>(epi + row * ROWB + ((at ^ (row & (PPR - 1))) << 4) + (col & 4) * 2) = pack4(v);
+        }
+    bf16_t *out = static_cast<bf16_t *>(a.out[c.j]) + c.c0 + first;
+    const int width = a.width[c.j], at = lane % PPR;
+#pragma unroll 4
+    for (int it = 0; it < 128 * PPR / 64; ++it) {
+        const int row = 64 / PPR * it + lane / PPR;
+        const long long m = m0 + 128 * wm + row;
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(epi + row * ROWB + ((at ^ (row & (PPR - 1))) << 4));
+        if (m < a.M && first + 8 * at < c.count)
+            __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(out + static_cast<size_t>(m) * width + 8 * at));
+    }
+}
+}  // namespace
+
+hipError_t launch_project_fp8(int64_t M, int K, int n_out, const int32_t *widths, int scale_type, const void *x, const void *x_scale, const void *w,
+                              const void *w_scale, const float *bias, int out_dtype, void *const *outs, hipStream_t stream)
+{
+    Fp8Args a{};
+    a.x = static_cast<const uint8_t *>(x);
+    a.w = static_cast<const uint8_t *>(w);
+    a.xs = x_scale;
+    a.ws = w_scale;
+    a.bias = bias;
+    a.M = M;
+    a.K = K;
+    a.pitch = scale_pitch(K);
+    a.out_f32 = out_dtype == DSLA_F32;
+    int blocks = 0;
+    for (int j = 0; j < DSLA_MAX_PROJECTIONS; ++j) {
+        a.out[j] = j < n_out ? outs[j] : nullptr;
+        a.width[j] = j < n_out ? widths[j] : 0;
+        blocks += (a.width[j] + 127) / 128;
+    }
+    ProfileScope ps(DSLA_KERNEL_PROJECT_FP8, stream);
+    if (out_dtype == DSLA_BF16 && M > 512) {
+        const int tiles_m = static_cast<int>((M + 255) / 256), tiles_n = (blocks + 1) / 2;
+        const long long per_xcd = (static_cast<long long>(tiles_m) * tiles_n + 7) / 8;
+        const dim3 grid(static_cast<unsigned>(8 * per_xcd));
+        const int group = tiles_m <= 5 ? tiles_m : 4;
+        if (scale_type == DSLA_SCALE_E8M0) DSLA_LAUNCH(ps, project_fp8_tile_kernel<true>, grid, dim3(256), 0, stream, a, tiles_m, tiles_n, blocks, group, per_xcd);
+        else DSLA_LAUNCH(ps, project_fp8_tile_kernel<false>, grid, dim3(512), 0, stream, a, tiles_m, tiles_n, blocks, group, per_xcd);
+        return hipGetLastError();
+    }
+    const unsigned tiles_m = static_cast<unsigned>((M + 127) / 128);
+    const dim3 grid(tiles_m * static_cast<unsigned>(blocks));
+    const bool e8m0 = scale_type == DSLA_SCALE_E8M0, exact = out_dtype == DSLA_F32;
+    if (e8m0 && exact) DSLA_LAUNCH(ps, (project_fp8_kernel<true, true>), grid, dim3(256), 0, stream, a, tiles_m);
+    else if (e8m0) DSLA_LAUNCH(ps, (project_fp8_kernel<true, false>), grid, dim3(256), 0, stream, a, tiles_m);
+    else if (exact) DSLA_LAUNCH(ps, (project_fp8_kernel<false, true>), grid, dim3(256), 0, stream, a, tiles_m);
+    else DSLA_LAUNCH(ps, (project_fp8_kernel<false, false>), grid, dim3(256), 0, stream, a, tiles_m);
+    return hipGetLastError();
+}
+
+}  // namespace dsla
