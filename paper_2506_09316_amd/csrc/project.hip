@@ -76,11 +76,6 @@ __device__ __forceinline__ void buffer_load_lds16(__amdgpu_buffer_rsrc_t res, ch
 {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void *)(lds), 16, voff, soff, 0, 0);
 }
-template <int N>
-__device__ __forceinline__ void wait_loads()   // at most N of this wavefront's loads are still in flight
-{
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
 
 // One 32 x 32 result tile, held transposed (tile rows = output columns): register r of lane (ln, g) is output row
 // m_tile + ln, output column n_tile + 8 (r / 4) + 4 g + r % 4, so a lane stores 4 adjacent columns at a time.

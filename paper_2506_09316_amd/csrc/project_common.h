@@ -4,6 +4,12 @@
 
 namespace dsla {
 
+template <int N>
+__device__ __forceinline__ void wait_loads()   // at most N of this wavefront's loads are still in flight
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
 // Tile order: the 8 XCDs each take a contiguous run of the linear tile order (workgroup ids go round-robin over the
 // XCDs, each XCD has its own L2), and the linear order runs in groups of GM row tiles: inside a group the row tile
 // runs fastest, then the column tile, so the tiles in flight at one time (a few dozen per XCD) share GM panels of x

@@ -409,6 +409,189 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
             __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(out + static_cast<size_t>(m) * width + 8 * at));
     }
 }
+// ---------------------------------------------------------------------------------------------------------------
+// Few rows: the weights are the traffic
+// ---------------------------------------------------------------------------------------------------------------
+// A workgroup of four wavefronts has all rows of x (16 MT) and 16 NT columns; the wavefronts share K, one step of 128 to each in turn, and
+// nothing else until their sums are added at the end: no barrier stands between a wavefront's loads.  Its steps go through a ring of its
+// own in LDS, filled by buffer loads that write LDS directly: an instruction fills 8 rows of 128 bytes, or one scale of every row.
+template <int MT, int NT>
+struct Few {
+    static constexpr int LOADS = 2 * (NT + MT) + 2;                        // instructions of a step
+    static constexpr uint32_t SCALES = (NT + MT) * 2048, STAGE = SCALES + 512;
+    static constexpr int FIT = 38 * 1024 / static_cast<int>(STAGE), MOST = 1 + 60 / LOADS;   // (the counter of loads in flight ends at 63)
+    static constexpr int DEPTH = FIT < MOST ? FIT : MOST;
+};
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// Loads that the compiler does not know: whoever reads what they bring waits with wait_loads() first.
+__device__ __forceinline__ void load_to_lds16(uint32_t lds, uint32_t voff, u32x4 res, uint32_t soff)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(voff), "s"(res), "s"(soff) : "m0", "memory");
+}
+__device__ __forceinline__ void load_to_lds4(uint32_t lds, uint32_t voff, u32x4 res, uint32_t soff)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds), "v"(voff), "s"(res), "s"(soff) : "m0", "memory");
+}
+#pragma clang diagnostic pop
+__device__ __forceinline__ u32x4 resource_of(const void *p, size_t offset, uint32_t bytes)
+{
+    const uint64_t at = reinterpret_cast<uint64_t>(p) + offset;
+    return u32x4{static_cast<uint32_t>(at), static_cast<uint32_t>(at >> 32) & 0xffffu, bytes, 0x00020000u};
+}
+
+// 16 columns from column `col` of all outputs on: their output, first column there, and their row of scales.
+struct Tile {
+    int j, c0, scale_row;
+};
+__device__ __forceinline__ Tile tile_at(const Fp8Args &a, int col)
+{
+    Tile t{0, col, 0};
+    while (t.c0 >= a.width[t.j]) {
+        t.scale_row += (a.width[t.j] + 127) / 128;
+        t.c0 -= a.width[t.j++];
+    }
+    t.scale_row += t.c0 / 128;
+    return t;
+}
+
+template <int MT, int NT, bool E8M0, bool EXACT>
+__global__ __launch_bounds__(256) void project_fp8_rows_kernel(Fp8Args a, int N)
+{
+    using F = Few<MT, NT>;
+    constexpr int DEPTH = F::DEPTH, SB = E8M0 ? 1 : 4;
+    __shared__ __attribute__((aligned(1024))) char ring[4 * DEPTH * F::STAGE];
+    const int n0 = blockIdx.x * 16 * NT, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    const int M = static_cast<int>(a.M);
+    char *mine = ring + wave * DEPTH * F::STAGE;
+    const uint32_t mine_lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char *)mine));
+
+    // ---- loading: piece c of a row R sits at position c ^ (R / 2 % 8).  What does not exist - rows, pieces behind K - arrives as zeros. ----
+    const int cols = N - n0 < 16 * NT ? N - n0 : 16 * NT;
+    const u32x4 res_w = resource_of(a.w, static_cast<size_t>(n0) * a.K, static_cast<uint32_t>(cols) * static_cast<uint32_t>(a.K));
+    const u32x4 res_x = resource_of(a.x, 0, static_cast<uint32_t>(M) * static_cast<uint32_t>(a.K));
+    const int first_scale = tile_at(a, n0).scale_row, last_scale = tile_at(a, n0 + cols - 16).scale_row;
+    const uint32_t scale_bytes = static_cast<uint32_t>(a.pitch) * SB;
+    const u32x4 res_ws = resource_of(a.ws, static_cast<size_t>(first_scale) * scale_bytes, (last_scale - first_scale + 1) * scale_bytes);
+    const u32x4 res_xs = resource_of(a.xs, 0, static_cast<uint32_t>(M) * scale_bytes);
+    const uint32_t ws_off = lane < NT && 16 * lane < cols ? (tile_at(a, n0 + 16 * lane).scale_row - first_scale) * scale_bytes : kNowhere;
+    const uint32_t xs_off = lane * scale_bytes;
+    const int piece[2] = {(lane & 7) ^ (lane >> 4), (lane & 7) ^ (4 + (lane >> 4))};   // of instructions with an even and an odd number
+    const uint32_t row_off = static_cast<uint32_t>(lane >> 3) * static_cast<uint32_t>(a.K), row_step = 8u * static_cast<uint32_t>(a.K);
+    const int nk = (a.K + 127) / 128, rot = static_cast<int>((3 * (blockIdx.x / 8)) % nk);
+    auto step_of = [&](int i) {   // this wavefront's i-th step; workgroups begin at different places, so that what they ask for at one time spreads over the memory channels
+        const int s = wave + 4 * i + rot;
+        return s < nk ? s : s - nk;
+    };
+    auto issue = [&](int i, int slot) {
+        const int ks = step_of(i), left = a.K - 128 * ks;
+        const uint32_t at = mine_lds + slot * F::STAGE, k0 = 128 * ks;
+        const bool there[2] = {16 * piece[0] < left, 16 * piece[1] < left};
+#pragma unroll
+        for (int n = 0; n < 2 * NT; ++n) load_to_lds16(at + n * 1024, there[n & 1] ? row_off + n * row_step + 16 * piece[n & 1] : kNowhere, res_w, k0);
+#pragma unroll
+        for (int n = 0; n < 2 * MT; ++n) load_to_lds16(at + (2 * NT + n) * 1024, there[n & 1] ? row_off + n * row_step + 16 * piece[n & 1] : kNowhere, res_x, k0);
+        const uint32_t s0 = E8M0 ? ks & ~3 : 4 * ks;
+        load_to_lds4(at + F::SCALES, xs_off, res_xs, s0);
+        load_to_lds4(at + F::SCALES + 256, ws_off, res_ws, s0);
+    };
+
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int steps = nk > wave ? (nk - wave + 3) / 4 : 0;
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i)
+        if (i < steps) issue(i, i);
+    const uint32_t pos = static_cast<uint32_t>(g ^ (r >> 1)) << 4;
+    int slot = 0;
+    for (int i = 0; i < steps; ++i) {
+        if (i + DEPTH <= steps) wait_loads<F::LOADS * (DEPTH - 1)>();
+        else wait_loads<0>();
+        const char *st = mine + slot * F::STAGE;
+        const int ks = step_of(i);
+        i32x8 w[NT], x[MT];
+        uint32_t sw[NT], sx[MT];
+        auto fragment = [&](int tile) {
+            const char *row = st + tile * 2048 + r * 128;
+            return join(*reinterpret_cast<const u32x4 *>(row + pos), *reinterpret_cast<const u32x4 *>(row + (pos ^ 64)));
+        };
+        const int shift = 8 * (ks & 3);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            w[j] = fragment(j);
+            sw[j] = *reinterpret_cast<const uint32_t *>(st + F::SCALES + 256 + 4 * j);
+            if (E8M0) sw[j] = sw[j] >> shift & 255u;
+        }
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+            x[j] = fragment(NT + j);
+            sx[j] = *reinterpret_cast<const uint32_t *>(st + F::SCALES + 4 * (16 * j + r));
+            if (E8M0) sx[j] = sx[j] >> shift & 255u;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (i + DEPTH < steps) issue(i + DEPTH, slot);
+        slot = slot + 1 == DEPTH ? 0 : slot + 1;
+        Operand<EXACT> ow[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) ow[j].set(w[j]);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            Operand<EXACT> ox;
+            ox.set(x[m]);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                if constexpr (E8M0 && !EXACT) acc[m][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ow[j].f, ox.f, acc[m][j], 0, 0, 0, sw[j], 0, sx[m]);
+                else Factor<E8M0>(sx[m], sw[j]).add(acc[m][j], product(ow[j], ox));
+            }
+        }
+    }
+
+    // ---- the wavefronts' sums, in order ----
+    __syncthreads();
+    f32x4 *sums = reinterpret_cast<f32x4 *>(ring);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) sums[(wave * MT * NT + i * NT + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    for (int n = wave; n < MT * NT; n += 4) {
+        const int m = 16 * (n / NT) + r, col = n0 + 16 * (n % NT);
+        if (m >= M || col >= N) continue;
+        f32x4 v = sums[n * 64 + lane];
+#pragma unroll
+        for (int k = 1; k < 4; ++k) v += sums[(k * MT * NT + n) * 64 + lane];
+        const Tile t = tile_at(a, col);
+        if (a.bias) v += *reinterpret_cast<const f32x4 *>(a.bias + col + 4 * g);
+        const size_t at = static_cast<size_t>(m) * a.width[t.j] + t.c0 + 4 * g;
+        if (EXACT) *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out[t.j]) + at) = v;
+        else *reinterpret_cast<u32x2 *>(static_cast<bf16_t *>(a.out[t.j]) + at) = pack4(v);
+    }
+}
+
+template <int MT, int NT>
+void launch_few(ProfileScope &ps, const Fp8Args &a, int N, bool e8m0, hipStream_t stream)
+{
+    const dim3 grid(static_cast<unsigned>((N + 16 * NT - 1) / (16 * NT)));
+    if (e8m0 && a.out_f32) DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, true, true>), grid, dim3(256), 0, stream, a, N);
+    else if (e8m0) DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, true, false>), grid, dim3(256), 0, stream, a, N);
+    else if (a.out_f32) DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, false, true>), grid, dim3(256), 0, stream, a, N);
+    else DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, false, false>), grid, dim3(256), 0, stream, a, N);
+}
+template <int MT>
+void launch_few_n(ProfileScope &ps, const Fp8Args &a, int N, bool e8m0, hipStream_t stream)
+{
+    // Columns of a workgroup: the fewest that leave no compute unit a second one.
+    const int nt = (N + 16 * 256 - 1) / (16 * 256);
+    if (nt <= 1) launch_few<MT, 1>(ps, a, N, e8m0, stream);
+    else if (nt == 2) launch_few<MT, 2>(ps, a, N, e8m0, stream);
+    else if (nt == 3) launch_few<MT, 3>(ps, a, N, e8m0, stream);
+    else if (nt == 4) launch_few<MT, 4>(ps, a, N, e8m0, stream);
+    else launch_few<MT, 5>(ps, a, N, e8m0, stream);
+}
 }  // namespace
 
 hipError_t launch_project_fp8(int64_t M, int K, int n_out, const int32_t *widths, int scale_type, const void *x, const void *x_scale, const void *w,
@@ -424,25 +607,32 @@ hipError_t launch_project_fp8(int64_t M, int K, int n_out, const int32_t *widths
     a.K = K;
     a.pitch = scale_pitch(K);
     a.out_f32 = out_dtype == DSLA_F32;
-    int blocks = 0;
+    int blocks = 0, N = 0;
     for (int j = 0; j < DSLA_MAX_PROJECTIONS; ++j) {
         a.out[j] = j < n_out ? outs[j] : nullptr;
         a.width[j] = j < n_out ? widths[j] : 0;
         blocks += (a.width[j] + 127) / 128;
+        N += a.width[j];
     }
     ProfileScope ps(DSLA_KERNEL_PROJECT_FP8, stream);
-    if (out_dtype == DSLA_BF16 && M > 512) {
+    const bool e8m0 = scale_type == DSLA_SCALE_E8M0, exact = out_dtype == DSLA_F32;
+    if (M <= 64) {
+        if (M <= 16) launch_few_n<1>(ps, a, N, e8m0, stream);
+        else if (M <= 32) launch_few_n<2>(ps, a, N, e8m0, stream);
+        else launch_few_n<4>(ps, a, N, e8m0, stream);
+        return hipGetLastError();
+    }
+    if (!exact && M > 512) {
         const int tiles_m = static_cast<int>((M + 255) / 256), tiles_n = (blocks + 1) / 2;
         const long long per_xcd = (static_cast<long long>(tiles_m) * tiles_n + 7) / 8;
         const dim3 grid(static_cast<unsigned>(8 * per_xcd));
         const int group = tiles_m <= 5 ? tiles_m : 4;
-        if (scale_type == DSLA_SCALE_E8M0) DSLA_LAUNCH(ps, project_fp8_tile_kernel<true>, grid, dim3(256), 0, stream, a, tiles_m, tiles_n, blocks, group, per_xcd);
+        if (e8m0) DSLA_LAUNCH(ps, project_fp8_tile_kernel<true>, grid, dim3(256), 0, stream, a, tiles_m, tiles_n, blocks, group, per_xcd);
         else DSLA_LAUNCH(ps, project_fp8_tile_kernel<false>, grid, dim3(512), 0, stream, a, tiles_m, tiles_n, blocks, group, per_xcd);
         return hipGetLastError();
     }
     const unsigned tiles_m = static_cast<unsigned>((M + 127) / 128);
     const dim3 grid(tiles_m * static_cast<unsigned>(blocks));
-    const bool e8m0 = scale_type == DSLA_SCALE_E8M0, exact = out_dtype == DSLA_F32;
     if (e8m0 && exact) DSLA_LAUNCH(ps, (project_fp8_kernel<true, true>), grid, dim3(256), 0, stream, a, tiles_m);
     else if (e8m0) DSLA_LAUNCH(ps, (project_fp8_kernel<true, false>), grid, dim3(256), 0, stream, a, tiles_m);
     else if (exact) DSLA_LAUNCH(ps, (project_fp8_kernel<false, true>), grid, dim3(256), 0, stream, a, tiles_m);
