@@ -412,15 +412,18 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
 // ---------------------------------------------------------------------------------------------------------------
 // Few rows: the weights are the traffic
 // ---------------------------------------------------------------------------------------------------------------
-// A workgroup of four wavefronts has all rows of x (16 MT) and 16 NT columns; the wavefronts share K, one step of 128 to each in turn, and
-// nothing else until their sums are added at the end: no barrier stands between a wavefront's loads.  Its steps go through a ring of its
-// own in LDS, filled by buffer loads that write LDS directly: an instruction fills 8 rows of 128 bytes, or one scale of every row.
-template <int MT, int NT>
+// A workgroup has 16 MT rows and 16 NT columns; its wavefronts take a stretch of K each and share nothing until their sums are added at the
+// end: no barrier stands between a wavefront's loads.  Its steps of 128 go through a ring of its own in LDS, filled by buffer loads that write
+// LDS directly, an instruction 8 rows of 128 bytes.  What counts is the lines that are asked for, and a scale alone would be one: they come
+// as 16 bytes of every row, 12 steps of E8M0 (from a multiple of four down) or four of fp32 at a time.
+template <int MT, int NT, int NW>
 struct Few {
-    static constexpr int LOADS = 2 * (NT + MT) + 2;                        // instructions of a step
-    static constexpr uint32_t SCALES = (NT + MT) * 2048, STAGE = SCALES + 512;
-    static constexpr int FIT = 38 * 1024 / static_cast<int>(STAGE), MOST = 1 + 60 / LOADS;   // (the counter of loads in flight ends at 63)
-    static constexpr int DEPTH = FIT < MOST ? FIT : MOST;
+    static constexpr int LOADS = 2 * (NT + MT);                            // instructions of a step, scales apart
+    static constexpr uint32_t STAGE = (NT + MT) * 2048, SLOT = (MT + 1) * 256;   // a step's values; 16 bytes of scales of every row
+    static constexpr int ROOM = 160 * 1024 / NW;                           // bytes of a wavefront
+    static constexpr int SLOTS = ROOM / static_cast<int>(STAGE) == (ROOM - 2 * static_cast<int>(SLOT)) / static_cast<int>(STAGE) ? 2 : 1;
+    static constexpr int FIT = (ROOM - SLOTS * static_cast<int>(SLOT)) / static_cast<int>(STAGE), MOST = 1 + 60 / LOADS;   // (the counter of loads in flight ends at 63)
+    static constexpr int DEPTH = FIT < MOST ? FIT : MOST, MINE = DEPTH * STAGE + SLOTS * SLOT;
 };
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
@@ -455,46 +458,55 @@ __device__ __forceinline__ Tile tile_at(const Fp8Args &a, int col)
     return t;
 }
 
-template <int MT, int NT, bool E8M0, bool EXACT>
-__global__ __launch_bounds__(256) void project_fp8_rows_kernel(Fp8Args a, int N)
+template <int MT, int NT, int NW, bool E8M0, bool EXACT>
+__global__ __launch_bounds__(64 * NW) void project_fp8_rows_kernel(Fp8Args a, int N, int tiles_m, int tiles_n, long long per_xcd)
 {
-    using F = Few<MT, NT>;
+    using F = Few<MT, NT, NW>;
     constexpr int DEPTH = F::DEPTH, SB = E8M0 ? 1 : 4;
-    __shared__ __attribute__((aligned(1024))) char ring[4 * DEPTH * F::STAGE];
-    const int n0 = blockIdx.x * 16 * NT, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    __shared__ __attribute__((aligned(1024))) char ring[NW * F::MINE];
+    int tm, tn;
+    if (!tile_of(tiles_m, tiles_n, tiles_m, per_xcd, tm, tn)) return;
+    const int n0 = tn * 16 * NT, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-    const int M = static_cast<int>(a.M);
-    char *mine = ring + wave * DEPTH * F::STAGE;
+    const long long m0 = 16LL * MT * tm;
+    const int M = a.M - m0 < 16 * MT ? static_cast<int>(a.M - m0) : 16 * MT;   // rows here
+    char *mine = ring + wave * F::MINE;
     const uint32_t mine_lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char *)mine));
 
     // ---- loading: piece c of a row R sits at position c ^ (R / 2 % 8).  What does not exist - rows, pieces behind K - arrives as zeros. ----
     const int cols = N - n0 < 16 * NT ? N - n0 : 16 * NT;
     const u32x4 res_w = resource_of(a.w, static_cast<size_t>(n0) * a.K, static_cast<uint32_t>(cols) * static_cast<uint32_t>(a.K));
-    const u32x4 res_x = resource_of(a.x, 0, static_cast<uint32_t>(M) * static_cast<uint32_t>(a.K));
+    const u32x4 res_x = resource_of(a.x, static_cast<size_t>(m0) * a.K, static_cast<uint32_t>(M) * static_cast<uint32_t>(a.K));
     const int first_scale = tile_at(a, n0).scale_row, last_scale = tile_at(a, n0 + cols - 16).scale_row;
     const uint32_t scale_bytes = static_cast<uint32_t>(a.pitch) * SB;
     const u32x4 res_ws = resource_of(a.ws, static_cast<size_t>(first_scale) * scale_bytes, (last_scale - first_scale + 1) * scale_bytes);
-    const u32x4 res_xs = resource_of(a.xs, 0, static_cast<uint32_t>(M) * scale_bytes);
+    const u32x4 res_xs = resource_of(a.xs, static_cast<size_t>(m0) * scale_bytes, static_cast<uint32_t>(M) * scale_bytes);
+    constexpr uint32_t SCALES = DEPTH * F::STAGE;
     const uint32_t ws_off = lane < NT && 16 * lane < cols ? (tile_at(a, n0 + 16 * lane).scale_row - first_scale) * scale_bytes : kNowhere;
     const uint32_t xs_off = lane * scale_bytes;
     const int piece[2] = {(lane & 7) ^ (lane >> 4), (lane & 7) ^ (4 + (lane >> 4))};   // of instructions with an even and an odd number
     const uint32_t row_off = static_cast<uint32_t>(lane >> 3) * static_cast<uint32_t>(a.K), row_step = 8u * static_cast<uint32_t>(a.K);
-    const int nk = (a.K + 127) / 128, rot = static_cast<int>((3 * (blockIdx.x / 8)) % nk);
-    auto step_of = [&](int i) {   // this wavefront's i-th step; workgroups begin at different places, so that what they ask for at one time spreads over the memory channels
-        const int s = wave + 4 * i + rot;
-        return s < nk ? s : s - nk;
+    // This wavefront's stretch of K; neighbours in N begin with another one, so that what is asked for at one time spreads over the memory channels.
+    const int nk = (a.K + 127) / 128, part = (wave + tn) % NW, first = static_cast<int>(static_cast<long long>(nk) * part / NW);
+    const int steps = static_cast<int>(static_cast<long long>(nk) * (part + 1) / NW) - first;
+    constexpr int CHUNK = E8M0 ? 12 : 4;   // steps that 16 bytes of scales reach for
+    auto issue_scales = [&](int i) {   // of the steps from i on (the waits below count without them, and so wait for a little more)
+        const int ks = first + i;
+        const uint32_t at = mine_lds + SCALES + i / CHUNK % F::SLOTS * F::SLOT, s0 = E8M0 ? ks & ~3 : 4 * ks;
+#pragma unroll
+        for (int n = 0; n < (MT + 3) / 4; ++n)
+            if (lane < 16 * MT - 64 * n) load_to_lds16(at + n * 1024, xs_off + 64 * n * scale_bytes, res_xs, s0);
+        if (lane < NT) load_to_lds16(at + MT * 256, ws_off, res_ws, s0);
     };
     auto issue = [&](int i, int slot) {
-        const int ks = step_of(i), left = a.K - 128 * ks;
+        const int ks = first + i, left = a.K - 128 * ks;
         const uint32_t at = mine_lds + slot * F::STAGE, k0 = 128 * ks;
         const bool there[2] = {16 * piece[0] < left, 16 * piece[1] < left};
+        if (i % CHUNK == 0 && (F::SLOTS == 2 || i == 0)) issue_scales(i);
 #pragma unroll
         for (int n = 0; n < 2 * NT; ++n) load_to_lds16(at + n * 1024, there[n & 1] ? row_off + n * row_step + 16 * piece[n & 1] : kNowhere, res_w, k0);
 #pragma unroll
         for (int n = 0; n < 2 * MT; ++n) load_to_lds16(at + (2 * NT + n) * 1024, there[n & 1] ? row_off + n * row_step + 16 * piece[n & 1] : kNowhere, res_x, k0);
-        const uint32_t s0 = E8M0 ? ks & ~3 : 4 * ks;
-        load_to_lds4(at + F::SCALES, xs_off, res_xs, s0);
-        load_to_lds4(at + F::SCALES + 256, ws_off, res_ws, s0);
     };
 
     f32x4 acc[MT][NT];
@@ -502,35 +514,42 @@ __global__ __launch_bounds__(256) void project_fp8_rows_kernel(Fp8Args a, int N)
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int steps = nk > wave ? (nk - wave + 3) / 4 : 0;
 #pragma unroll
     for (int i = 0; i < DEPTH; ++i)
         if (i < steps) issue(i, i);
     const uint32_t pos = static_cast<uint32_t>(g ^ (r >> 1)) << 4;
     int slot = 0;
     for (int i = 0; i < steps; ++i) {
-        if (i + DEPTH <= steps) wait_loads<F::LOADS * (DEPTH - 1)>();
-        else wait_loads<0>();
+        if (F::SLOTS == 1 && i > 0 && i % CHUNK == 0) {   // (the scales before have been read)
+            issue_scales(i);
+            wait_loads<0>();
+        } else if (i + DEPTH <= steps) {
+            wait_loads<F::LOADS * (DEPTH - 1)>();
+        } else {
+            wait_loads<0>();
+        }
         const char *st = mine + slot * F::STAGE;
-        const int ks = step_of(i);
         i32x8 w[NT], x[MT];
         uint32_t sw[NT], sx[MT];
         auto fragment = [&](int tile) {
             const char *row = st + tile * 2048 + r * 128;
             return join(*reinterpret_cast<const u32x4 *>(row + pos), *reinterpret_cast<const u32x4 *>(row + (pos ^ 64)));
         };
-        const int shift = 8 * (ks & 3);
+        const int chunk = i - i % CHUNK, ahead = E8M0 ? first + i - ((first + chunk) & ~3) : i - chunk;
+        const char *scales = mine + SCALES + i / CHUNK % F::SLOTS * F::SLOT;
+        auto scale_of = [&](int row) -> uint32_t {
+            if (E8M0) return reinterpret_cast<const uint8_t *>(scales)[16 * row + ahead];
+            return *reinterpret_cast<const uint32_t *>(scales + 16 * row + 4 * ahead);
+        };
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             w[j] = fragment(j);
-            sw[j] = *reinterpret_cast<const uint32_t *>(st + F::SCALES + 256 + 4 * j);
-            if (E8M0) sw[j] = sw[j] >> shift & 255u;
+            sw[j] = scale_of(16 * MT + j);
         }
 #pragma unroll
         for (int j = 0; j < MT; ++j) {
             x[j] = fragment(NT + j);
-            sx[j] = *reinterpret_cast<const uint32_t *>(st + F::SCALES + 4 * (16 * j + r));
-            if (E8M0) sx[j] = sx[j] >> shift & 255u;
+            sx[j] = scale_of(16 * j + r);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (i + DEPTH < steps) issue(i + DEPTH, slot);
@@ -551,14 +570,26 @@ __global__ __launch_bounds__(256) void project_fp8_rows_kernel(Fp8Args a, int N)
     }
 
     // ---- the wavefronts' sums, in order ----
-    __syncthreads();
     f32x4 *sums = reinterpret_cast<f32x4 *>(ring);
+    auto put = [&](int at) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) sums[(wave * MT * NT + i * NT + j) * 64 + lane] = acc[i][j];
+            for (int j = 0; j < NT; ++j) sums[(at * MT * NT + i * NT + j) * 64 + lane] = acc[i][j];
+    };
     __syncthreads();
-    for (int n = wave; n < MT * NT; n += 4) {
+    if (NW == 8) {   // (all eight would not fit)
+        if (wave >= 4) put(wave - 4);
+        __syncthreads();
+        if (wave < 4)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] += sums[(wave * MT * NT + i * NT + j) * 64 + lane];
+    }
+    if (wave < 4) put(wave);
+    __syncthreads();
+    for (int n = wave; n < MT * NT; n += NW) {
         const int m = 16 * (n / NT) + r, col = n0 + 16 * (n % NT);
         if (m >= M || col >= N) continue;
         f32x4 v = sums[n * 64 + lane];
@@ -566,7 +597,7 @@ __global__ __launch_bounds__(256) void project_fp8_rows_kernel(Fp8Args a, int N)
         for (int k = 1; k < 4; ++k) v += sums[(k * MT * NT + n) * 64 + lane];
         const Tile t = tile_at(a, col);
         if (a.bias) v += *reinterpret_cast<const f32x4 *>(a.bias + col + 4 * g);
-        const size_t at = static_cast<size_t>(m) * a.width[t.j] + t.c0 + 4 * g;
+        const size_t at = static_cast<size_t>(m0 + m) * a.width[t.j] + t.c0 + 4 * g;
         if (EXACT) *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out[t.j]) + at) = v;
         else *reinterpret_cast<u32x2 *>(static_cast<bf16_t *>(a.out[t.j]) + at) = pack4(v);
     }
@@ -575,22 +606,31 @@ __global__ __launch_bounds__(256) void project_fp8_rows_kernel(Fp8Args a, int N)
 template <int MT, int NT>
 void launch_few(ProfileScope &ps, const Fp8Args &a, int N, bool e8m0, hipStream_t stream)
 {
-    const dim3 grid(static_cast<unsigned>((N + 16 * NT - 1) / (16 * NT)));
-    if (e8m0 && a.out_f32) DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, true, true>), grid, dim3(256), 0, stream, a, N);
-    else if (e8m0) DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, true, false>), grid, dim3(256), 0, stream, a, N);
-    else if (a.out_f32) DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, false, true>), grid, dim3(256), 0, stream, a, N);
-    else DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, false, false>), grid, dim3(256), 0, stream, a, N);
+    constexpr int NW = Few<MT, NT, 8>::DEPTH >= 1 ? 8 : 4;
+    const int tiles_m = static_cast<int>((a.M + 16 * MT - 1) / (16 * MT)), tiles_n = (N + 16 * NT - 1) / (16 * NT);
+    const long long per_xcd = ((static_cast<long long>(tiles_m) * tiles_n + 7) / 8 + tiles_m - 1) / tiles_m * tiles_m;   // whole columns to an XCD
+    const dim3 grid(static_cast<unsigned>(8 * per_xcd));
+    if (e8m0 && a.out_f32) DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, NW, true, true>), grid, dim3(64 * NW), 0, stream, a, N, tiles_m, tiles_n, per_xcd);
+    else if (e8m0) DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, NW, true, false>), grid, dim3(64 * NW), 0, stream, a, N, tiles_m, tiles_n, per_xcd);
+    else if (a.out_f32) DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, NW, false, true>), grid, dim3(64 * NW), 0, stream, a, N, tiles_m, tiles_n, per_xcd);
+    else DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, NW, false, false>), grid, dim3(64 * NW), 0, stream, a, N, tiles_m, tiles_n, per_xcd);
 }
 template <int MT>
-void launch_few_n(ProfileScope &ps, const Fp8Args &a, int N, bool e8m0, hipStream_t stream)
+void launch_few_n(ProfileScope &ps, const Fp8Args &a, int N, int nt, bool e8m0, hipStream_t stream)
 {
-    // Columns of a workgroup: the fewest that leave no compute unit a second one.
-    const int nt = (N + 16 * 256 - 1) / (16 * 256);
     if (nt <= 1) launch_few<MT, 1>(ps, a, N, e8m0, stream);
     else if (nt == 2) launch_few<MT, 2>(ps, a, N, e8m0, stream);
     else if (nt == 3) launch_few<MT, 3>(ps, a, N, e8m0, stream);
     else if (nt == 4) launch_few<MT, 4>(ps, a, N, e8m0, stream);
     else launch_few<MT, 5>(ps, a, N, e8m0, stream);
+}
+void launch_few_m(ProfileScope &ps, const Fp8Args &a, int N, int mt, int nt, bool e8m0, hipStream_t stream)
+{
+    if (mt <= 1) launch_few_n<1>(ps, a, N, nt, e8m0, stream);
+    else if (mt == 2) launch_few_n<2>(ps, a, N, nt, e8m0, stream);
+    else if (mt == 3) launch_few_n<3>(ps, a, N, nt, e8m0, stream);
+    else if (mt == 4) launch_few_n<4>(ps, a, N, nt, e8m0, stream);
+    else launch_few_n<5>(ps, a, N, nt, e8m0, stream);
 }
 }  // namespace
 
@@ -617,9 +657,8 @@ hipError_t launch_project_fp8(int64_t M, int K, int n_out, const int32_t *widths
     ProfileScope ps(DSLA_KERNEL_PROJECT_FP8, stream);
     const bool e8m0 = scale_type == DSLA_SCALE_E8M0, exact = out_dtype == DSLA_F32;
     if (M <= 64) {
-        if (M <= 16) launch_few_n<1>(ps, a, N, e8m0, stream);
-        else if (M <= 32) launch_few_n<2>(ps, a, N, e8m0, stream);
-        else launch_few_n<4>(ps, a, N, e8m0, stream);
+        const int nt = (N + 16 * 256 - 1) / (16 * 256);
+        launch_few_m(ps, a, N, static_cast<int>((M + 15) / 16), nt, e8m0, stream);
         return hipGetLastError();
     }
     if (!exact && M > 512) {
