@@ -420,7 +420,7 @@ template <int MT, int NT, int NW>
 struct Few {
     static constexpr int LOADS = 2 * (NT + MT);                            // instructions of a step, scales apart
     static constexpr uint32_t STAGE = (NT + MT) * 2048, SLOT = (MT + 1) * 256;   // a step's values; 16 bytes of scales of every row
-    static constexpr int ROOM = 160 * 1024 / NW;                           // bytes of a wavefront
+    static constexpr int ROOM = (160 * 1024 - 256) / NW;                   // bytes of a wavefront
     static constexpr int SLOTS = ROOM / static_cast<int>(STAGE) == (ROOM - 2 * static_cast<int>(SLOT)) / static_cast<int>(STAGE) ? 2 : 1;
     static constexpr int FIT = (ROOM - SLOTS * static_cast<int>(SLOT)) / static_cast<int>(STAGE), MOST = 1 + 60 / LOADS;   // (the counter of loads in flight ends at 63)
     static constexpr int DEPTH = FIT < MOST ? FIT : MOST, MINE = DEPTH * STAGE + SLOTS * SLOT;
@@ -477,12 +477,31 @@ __global__ __launch_bounds__(64 * NW) void project_fp8_rows_kernel(Fp8Args a, in
     const int cols = N - n0 < 16 * NT ? N - n0 : 16 * NT;
     const u32x4 res_w = resource_of(a.w, static_cast<size_t>(n0) * a.K, static_cast<uint32_t>(cols) * static_cast<uint32_t>(a.K));
     const u32x4 res_x = resource_of(a.x, static_cast<size_t>(m0) * a.K, static_cast<uint32_t>(M) * static_cast<uint32_t>(a.K));
-    const int first_scale = tile_at(a, n0).scale_row, last_scale = tile_at(a, n0 + cols - 16).scale_row;
     const uint32_t scale_bytes = static_cast<uint32_t>(a.pitch) * SB;
-    const u32x4 res_ws = resource_of(a.ws, static_cast<size_t>(first_scale) * scale_bytes, (last_scale - first_scale + 1) * scale_bytes);
+    // The 16-column tiles one after the other: where their scales are and where their results go.
+    __shared__ u32x4 table[NT];   // (address of the first column in the first row, width)
+    Tile t = tile_at(a, n0);
+    const int first_scale = t.scale_row;
+    uint32_t ws_off = kNowhere;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        if (16 * j >= cols) break;
+        if (lane == j) ws_off = static_cast<uint32_t>(t.scale_row - first_scale) * scale_bytes;
+        const uint64_t to = reinterpret_cast<uint64_t>(a.out[t.j]) + (static_cast<size_t>(m0) * a.width[t.j] + t.c0) * (EXACT ? 4 : 2);
+        if (threadIdx.x == 0) table[j] = u32x4{static_cast<uint32_t>(to), static_cast<uint32_t>(to >> 32), static_cast<uint32_t>(a.width[t.j]), 0u};
+        if (16 * (j + 1) >= cols) break;
+        t.c0 += 16;
+        if (t.c0 >= a.width[t.j]) {
+            t.c0 = 0;
+            ++t.scale_row;
+            ++t.j;
+        } else if (t.c0 % 128 == 0) {
+            ++t.scale_row;
+        }
+    }
+    const u32x4 res_ws = resource_of(a.ws, static_cast<size_t>(first_scale) * scale_bytes, static_cast<uint32_t>(t.scale_row - first_scale + 1) * scale_bytes);
     const u32x4 res_xs = resource_of(a.xs, static_cast<size_t>(m0) * scale_bytes, static_cast<uint32_t>(M) * scale_bytes);
     constexpr uint32_t SCALES = DEPTH * F::STAGE;
-    const uint32_t ws_off = lane < NT && 16 * lane < cols ? (tile_at(a, n0 + 16 * lane).scale_row - first_scale) * scale_bytes : kNowhere;
     const uint32_t xs_off = lane * scale_bytes;
     const int piece[2] = {(lane & 7) ^ (lane >> 4), (lane & 7) ^ (4 + (lane >> 4))};   // of instructions with an even and an odd number
     const uint32_t row_off = static_cast<uint32_t>(lane >> 3) * static_cast<uint32_t>(a.K), row_step = 8u * static_cast<uint32_t>(a.K);
@@ -569,37 +588,35 @@ __global__ __launch_bounds__(64 * NW) void project_fp8_rows_kernel(Fp8Args a, in
         }
     }
 
-    // ---- the wavefronts' sums, in order ----
+    // ---- the wavefronts' sums, added in the order of K, as many rows of tiles at a time as fit; then whole rows leave.  Lane (r, g) of a tile in
+    // column j sits at (r + j) % 16, g: 16 lanes that read a row find their own banks ----
+    constexpr int ROWS = static_cast<int>(sizeof(ring)) / (NW * NT * 1024) < MT ? static_cast<int>(sizeof(ring)) / (NW * NT * 1024) : MT;
+    static_assert(ROWS >= 1, "the sums of a row of tiles have to fit");
     f32x4 *sums = reinterpret_cast<f32x4 *>(ring);
-    auto put = [&](int at) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) sums[(at * MT * NT + i * NT + j) * 64 + lane] = acc[i][j];
-    };
-    __syncthreads();
-    if (NW == 8) {   // (all eight would not fit)
-        if (wave >= 4) put(wave - 4);
+    for (int p = 0; p < MT; p += ROWS) {
         __syncthreads();
-        if (wave < 4)
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+        for (int i = p; i < p + ROWS && i < MT; ++i)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] += sums[(wave * MT * NT + i * NT + j) * 64 + lane];
-    }
-    if (wave < 4) put(wave);
-    __syncthreads();
-    for (int n = wave; n < MT * NT; n += NW) {
-        const int m = 16 * (n / NT) + r, col = n0 + 16 * (n % NT);
-        if (m >= M || col >= N) continue;
-        f32x4 v = sums[n * 64 + lane];
+            for (int j = 0; j < NT; ++j) sums[((wave * ROWS + i - p) * NT + j) * 64 + ((r + j) & 15) * 4 + g] = acc[i][j];
+        __syncthreads();
+        constexpr int G = 4 * NT, AT_ONCE = 64 * NW / G;   // groups of four columns of a row; rows at a time
+        const int c = threadIdx.x % G, col = n0 + 4 * c, last = M - 16 * p < 16 * ROWS ? M - 16 * p : 16 * ROWS;
+        if (threadIdx.x >= AT_ONCE * G || col >= N) continue;
+        const u32x4 to = table[c >> 2];
+        char *out = reinterpret_cast<char *>(static_cast<uint64_t>(to[1]) << 32 | to[0]) + 4 * (c & 3) * (EXACT ? 4 : 2);
+        const f32x4 bias = a.bias ? *reinterpret_cast<const f32x4 *>(a.bias + col) : f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int row = threadIdx.x / G; row < last; row += AT_ONCE) {
+            const int at = ((row >> 4) * NT + (c >> 2)) * 64 + ((row + (c >> 2)) & 15) * 4 + (c & 3);
+            f32x4 v = sums[(-tn & (NW - 1)) * ROWS * NT * 64 + at];
 #pragma unroll
-        for (int k = 1; k < 4; ++k) v += sums[(k * MT * NT + n) * 64 + lane];
-        const Tile t = tile_at(a, col);
-        if (a.bias) v += *reinterpret_cast<const f32x4 *>(a.bias + col + 4 * g);
-        const size_t at = static_cast<size_t>(m0 + m) * a.width[t.j] + t.c0 + 4 * g;
-        if (EXACT) *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out[t.j]) + at) = v;
-        else *reinterpret_cast<u32x2 *>(static_cast<bf16_t *>(a.out[t.j]) + at) = pack4(v);
+            for (int k = 1; k < NW; ++k) v += sums[((k - tn) & (NW - 1)) * ROWS * NT * 64 + at];
+            v += bias;
+            char *here = out + static_cast<size_t>(16 * p + row) * to[2] * (EXACT ? 4 : 2);
+            if (EXACT) *reinterpret_cast<f32x4 *>(here) = v;
+            else *reinterpret_cast<u32x2 *>(here) = pack4(v);
+        }
     }
 }
 
