@@ -234,12 +234,22 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
     uint32_t voff[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) voff[i] = static_cast<uint32_t>(8 * (wave + NW * i) + (lane >> 3)) * static_cast<uint32_t>(a.K) + 16 * piece;
-    auto fetch = [&](char *st, int ks, int i) {   // instruction i of both operands
-        const int k0 = 128 * ks, n = wave + NW * i;
+    auto fetch_x = [&](char *st, int ks, int i) {   // instruction i of an operand
+        const int k0 = 128 * ks;
+        buffer_load_lds16(res_x, st + (wave + NW * i) * 1024, 16 * piece < a.K - k0 ? voff[i] : kNowhere, k0);
+    };
+    auto fetch_w = [&](char *st, int ks, int i) {
+        const int k0 = 128 * ks;
         const bool there = 16 * piece < a.K - k0;
-        buffer_load_lds16(res_x, st + n * 1024, there ? voff[i] : kNowhere, k0);
-        if (i < LOADS / 2) buffer_load_lds16(res_w0, st + OPB + n * 1024, there ? voff[i] : kNowhere, k0);
-        else buffer_load_lds16(res_w1, st + OPB + n * 1024, there ? voff[i - LOADS / 2] : kNowhere, k0);
+        if (i < LOADS / 2) buffer_load_lds16(res_w0, st + OPB + (wave + NW * i) * 1024, there ? voff[i] : kNowhere, k0);
+        else buffer_load_lds16(res_w1, st + OPB + (wave + NW * i) * 1024, there ? voff[i - LOADS / 2] : kNowhere, k0);
+    };
+    auto fetch = [&](char *st, int ks) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            fetch_x(st, ks, i);
+            fetch_w(st, ks, i);
+        }
     };
 
     // ---- scales: of two steps as bytes, or of one as numbers, for every row of the wavefront, and for its block of columns ----
@@ -280,10 +290,11 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if constexpr (E8M0) {
-        // A step multiplies rows of tiles 0 .. 2 column by column, then rows 3 and 4, then 5 .. 7 column by column.  On entry the fragments of
-        // the columns and of rows 0 .. 2 are in registers or on their way; the other rows' are read under the first products.  The barrier in
-        // front of the last rows says that everybody has what it needs of `cur`, which takes step ks + 2, and that step ks + 1 has landed in
-        // `nxt`: as the last rows are done with a column, the next step's fragment takes its registers.
+        // A step multiplies rows of tiles 0 and 1 column by column, then rows 2 .. 4, then 5 .. 7 column by column.  On entry the fragments of the
+        // columns and of rows 0 and 1 are in registers or on their way; the other rows' are read under the first products.  Then everybody
+        // has all it needs of `cur`, says so at a barrier, and the loads of step ks + 2 go there.  In front of the last rows a second barrier
+        // says that step ks + 1 has landed in `nxt`: as these rows are done with a column, the next step's fragment takes its registers.
+        // So a load has 1.4 steps to arrive; with one barrier for both it has one.
         i32x8 w[NJ], x[8];
         auto product = [&](int i, int j, const Scales &s, auto odd) {
             product_in_place<decltype(odd)::value>(acc[i][j], w[j], x[i], s.w, s.x[i]);
@@ -291,40 +302,45 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
         auto step = [&](const Scales &s, Scales &ns, char *cur, char *nxt, int ks, auto odd) {
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
-                if (j < 5) x[3 + j] = fragment(cur, fx + (3 + j) * 2048);
+                if (j < 6) x[2 + j] = fragment(cur, fx + (2 + j) * 2048);
 #pragma unroll
-                for (int i = 0; i < 3; ++i) product(i, j, s, odd);
+                for (int i = 0; i < 2; ++i) product(i, j, s, odd);
                 __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int i = 3; i < 5; ++i)
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) product(i, j, s, odd);
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
+            __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
             if (decltype(odd)::value == 0) read_scales(ns, ks + 2);
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
-                fetch(cur, ks + 2, j);
+                fetch_x(cur, ks + 2, j);
+#pragma unroll
+                for (int i = 2; i < 5; ++i) product(i, j, s, odd);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // all but what this step has asked for: 8 rows of x, and 9 scales
+            if (decltype(odd)::value == 0) __builtin_amdgcn_s_waitcnt(0x4f71);   // vmcnt(17)
+            else __builtin_amdgcn_s_waitcnt(0x0f78);                               // vmcnt(8)
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                fetch_w(cur, ks + 2, j);
 #pragma unroll
                 for (int i = 5; i < 8; ++i) product(i, j, s, odd);
                 w[j] = fragment(nxt, fw + j * 2048);
-                if (j < 3) x[j] = fragment(nxt, fx + j * 2048);
+                if (j < 2) x[j] = fragment(nxt, fx + j * 2048);
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
         Scales s0, s1;
-#pragma unroll
-        for (int j = 0; j < LOADS; ++j) fetch(st0, 0, j);
+        fetch(st0, 0);
         read_scales(s0, 0);
-#pragma unroll
-        for (int j = 0; j < LOADS; ++j) fetch(st1, 1, j);
+        fetch(st1, 1);
         __builtin_amdgcn_s_waitcnt(0x0070);
         __builtin_amdgcn_s_barrier();
 #pragma unroll
-        for (int i = 0; i < 3; ++i) x[i] = fragment(st0, fx + i * 2048);
+        for (int i = 0; i < 2; ++i) x[i] = fragment(st0, fx + i * 2048);
 #pragma unroll
         for (int j = 0; j < NJ; ++j) w[j] = fragment(st0, fw + j * 2048);
         for (int ks = 0; ks < nk; ks += 2) {
@@ -345,8 +361,7 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
             __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
             __builtin_amdgcn_s_barrier();         // step ks has landed, and everybody is done with the other buffer
             __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) fetch(nxt, ks + 1, i);
+            fetch(nxt, ks + 1);
             read_scales(ns, ks + 1);
             i32x8 w[NJ];
 #pragma unroll
@@ -370,8 +385,7 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
             }
         };
         Scales s0, s1;
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) fetch(st0, 0, i);
+        fetch(st0, 0);
         read_scales(s0, 0);
         int ks = 0;
         for (; ks + 1 < nk; ks += 2) {
