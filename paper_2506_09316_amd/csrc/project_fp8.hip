@@ -397,32 +397,46 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
     __builtin_amdgcn_s_waitcnt(0x0070);
     __builtin_amdgcn_s_barrier();   // nothing in flight; everybody is done reading
 
-    // ---- results: each wavefront turns its part round in LDS, 128 rows of 16 NJ columns in bf16, the 16-byte piece c of row R at position
-    // c ^ (R % pieces), so that it leaves as whole rows ----
-    constexpr int PPR = 2 * NJ, ROWB = 32 * NJ;
+    // ---- results: each wavefront turns a row of tiles at a time round in LDS, 16 rows of 16 NJ columns in bf16, the 16-byte piece c of row R
+    // at position c ^ (R % pieces), so that they leave as whole rows.  (A wavefront's LDS instructions keep their order: it waits for nobody.) ----
+    constexpr int PPR = 2 * NJ, ROWB = 32 * NJ, READS = 16 * PPR / 64;
     const Columns c = wn / (WN / 2) ? cb1 : cb0;
     const int first = (16 * NJ * wn) % 128;   // the wavefront's first column in its block
-    char *epi = (wave < NW / 2 ? st0 : st1) + (wave % (NW / 2)) * 128 * ROWB;
+    char *epi = st0 + wave * 2 * 16 * ROWB;
+    const int width = a.width[c.j], at = lane % PPR, sub = lane / PPR;
+    const bool there = first + 8 * at < c.count;
+    const long long left = a.M - m0 - 128 * wm;   // rows of the wavefront's that exist
+    bf16_t *out = static_cast<bf16_t *>(a.out[c.j]) + static_cast<size_t>(m0 + 128 * wm + sub) * width + c.c0 + first + 8 * at;
+    auto leave = [&](auto with_bias, auto whole) {
+        constexpr bool BIAS = decltype(with_bias)::value, WHOLE = decltype(whole)::value;
+        f32x4 bias[NJ];
+        if (BIAS) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const int col = 16 * j + 4 * g, row = 16 * i + r, at = col >> 3;
-            f32x4 v = acc[i][j];
-            if (a.bias && first + col < c.count) v += *reinterpret_cast<const f32x4 *>(a.bias + c.row + first + col);
-            *reinterpret_cast<u32x2 *>(epi + row * ROWB + ((at ^ (row & (PPR - 1))) << 4) + (col & 4) * 2) = pack4(v);
+            for (int j = 0; j < NJ; ++j) {
+                const int col = first + 16 * j + 4 * g;
+                bias[j] = a.bias && col < c.count ? *reinterpret_cast<const f32x4 *>(a.bias + c.row + col) : f32x4{0.f, 0.f, 0.f, 0.f};
+            }
         }
-    bf16_t *out = static_cast<bf16_t *>(a.out[c.j]) + c.c0 + first;
-    const int width = a.width[c.j], at = lane % PPR;
-#pragma unroll 4
-    for (int it = 0; it < 128 * PPR / 64; ++it) {
-        const int row = 64 / PPR * it + lane / PPR;
-        const long long m = m0 + 128 * wm + row;
-        const u32x4 v = *reinterpret_cast<const u32x4 *>(epi + row * ROWB + ((at ^ (row & (PPR - 1))) << 4));
-        if (m < a.M && first + 8 * at < c.count)
-            __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(out + static_cast<size_t>(m) * width + 8 * at));
-    }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            char *turn = epi + (i & 1) * 16 * ROWB;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+                *reinterpret_cast<u32x2 *>(turn + r * ROWB + (((2 * j + (g >> 1)) ^ (r & (PPR - 1))) << 4) + (g & 1) * 8) = pack4(BIAS ? acc[i][j] + bias[j] : acc[i][j]);
+#pragma unroll
+            for (int q = 0; q < READS; ++q) {
+                const int row = 64 / PPR * q + sub;
+                const u32x4 v = *reinterpret_cast<const u32x4 *>(turn + row * ROWB + ((at ^ (row & (PPR - 1))) << 4));
+                if (WHOLE || (there && 16 * i + row < left)) __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(out));
+                out += static_cast<size_t>(64 / PPR) * width;
+            }
+        }
+    };
+    if (left < 128 || first + 16 * NJ > c.count) leave(std::true_type{}, std::false_type{});
+    else if (a.bias) leave(std::true_type{}, std::true_type{});
+    else leave(std::false_type{}, std::true_type{});
 }
+
 // ---------------------------------------------------------------------------------------------------------------
 // Few rows: the weights are the traffic
 // ---------------------------------------------------------------------------------------------------------------
