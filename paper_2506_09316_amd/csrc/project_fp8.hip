@@ -363,25 +363,24 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
             __builtin_amdgcn_sched_barrier(0);
             fetch(nxt, ks + 1);
             read_scales(ns, ks + 1);
-            i32x8 w[NJ];
+            i32x8 w[NJ], x[2];
+            x[0] = fragment(cur, fx);
 #pragma unroll
             for (int j = 0; j < NJ; ++j) w[j] = fragment(cur, fw + j * 2048);
-            f32x4 t[2][NJ];
+            // product n starts from zero, and its sums are added three products later
+            constexpr int BEHIND = 3;
+            f32x4 t[BEHIND + 1];
+            float scale[8];
 #pragma unroll
-            for (int i = 0; i <= 8; ++i) {
-                if (i < 8) {
-                    const i32x8 x = fragment(cur, fx + i * 2048);
+            for (int n = 0; n < 8 * NJ + BEHIND; ++n) {
+                const int i = n / NJ, j = n % NJ, k = n - BEHIND;
+                if (j == 0 && i < 7) x[(i + 1) & 1] = fragment(cur, fx + (i + 1) * 2048);
+                if (j == 0 && i < 8) scale[i] = __uint_as_float(s.x[i]) * __uint_as_float(s.w);
+                if (n < 8 * NJ) t[n % (BEHIND + 1)] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[j], x[i & 1], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, kOne, 0, kOne);
+                if (k >= 0)
 #pragma unroll
-                    for (int j = 0; j < NJ; ++j)
-                        t[i & 1][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[j], x, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, kOne, 0, kOne);
-                }
-                if (i > 0) {
-                    const float scale = __uint_as_float(s.x[i - 1]) * __uint_as_float(s.w);
-#pragma unroll
-                    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i - 1][j][e] += t[(i - 1) & 1][j][e] * scale;
-                }
+                    for (int e = 0; e < 4; ++e) acc[k / NJ][k % NJ][e] += t[k % (BEHIND + 1)][e] * scale[k / NJ];
+                __builtin_amdgcn_sched_barrier(0);
             }
         };
         Scales s0, s1;
