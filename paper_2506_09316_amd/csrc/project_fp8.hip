@@ -191,7 +191,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const uint8_t *p, si
 {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p + offset), 0, static_cast<int>(bytes), 0x00020000);
 }
-constexpr uint32_t kNowhere = 0x80000000u;   // an offset past the end of every buffer here: zeros
+// An offset past the end of every buffer here: zeros.  (The range of a buffer is checked dword by dword, with both offsets.)
+constexpr uint32_t kNowhere = 0x80000000u;
 
 // ---------------------------------------------------------------------------------------------------------------
 // 256 x 256 tiles
@@ -252,25 +253,35 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
         }
     };
 
-    // ---- scales: of two steps as bytes, or of one as numbers, for every row of the wavefront, and for its block of columns ----
+    // ---- scales: 16 bytes of every row at a time, for CHUNK steps, through LDS (an instruction that asks for one scale of 16 rows asks for as
+    // many lines as two that fill 8 rows: with fp32 scales these were two thirds of all) ----
     const int nk = (a.K + 127) / 128;
-    constexpr int SB = E8M0 ? 1 : 4;
-    const __amdgpu_buffer_rsrc_t res_xs = buffer_of(static_cast<const uint8_t *>(a.xs), static_cast<size_t>(m0) * a.pitch * SB, rows_a * a.pitch * SB);
-    const uint32_t xs_row = static_cast<uint32_t>(128 * wm + r) * static_cast<uint32_t>(a.pitch * SB), xs_step = 16u * static_cast<uint32_t>(a.pitch * SB);
-    const uint8_t *ws = static_cast<const uint8_t *>(a.ws) + static_cast<size_t>(wn / (WN / 2) ? second : 2 * tn) * a.pitch * SB;
+    constexpr int SB = E8M0 ? 1 : 4, CHUNK = 16 / SB, SLOT = 4096 + 1024;
+    __shared__ __attribute__((aligned(16))) char scales[3 * SLOT];
+    const uint32_t row_scales = static_cast<uint32_t>(a.pitch) * SB;
+    const __amdgpu_buffer_rsrc_t res_xs = buffer_of(static_cast<const uint8_t *>(a.xs), static_cast<size_t>(m0) * row_scales, rows_a * row_scales);
+    const __amdgpu_buffer_rsrc_t res_ws = buffer_of(static_cast<const uint8_t *>(a.ws), static_cast<size_t>(2 * tn) * row_scales, (second - 2 * tn + 1) * row_scales);
+    const uint32_t xs_from = static_cast<uint32_t>(64 * (wave & 3) + lane) * row_scales;
+    const uint32_t ws_from = lane < 2 ? (lane ? (second - 2 * tn) * row_scales : 0u) : kNowhere;
+    auto fetch_scales = [&](int ks, bool now = true) {   // of steps ks .. ks + CHUNK - 1; not now: nothing, to where nobody reads
+        char *to = scales + (now ? ks / CHUNK & 1 : 2) * SLOT;
+        buffer_load_lds16(res_xs, to + (wave & 3) * 1024, now ? xs_from : kNowhere, ks * SB);
+        buffer_load_lds16(res_ws, to + 4096, now ? ws_from : kNowhere, ks * SB);
+    };
     struct Scales {
         uint32_t x[8], w;
     };
-    // E8M0: of steps ks and ks + 1 (ks even).  What stands behind a row's last scale may be anything, and its products are of zeros: one.
-    auto read_scales = [&](Scales &s, int ks) {
-        const int at = (ks < nk ? ks : nk - 1) * SB;
+    const uint32_t xs_at = static_cast<uint32_t>(128 * wm + r) * 16, ws_at = 4096u + static_cast<uint32_t>(wn / (WN / 2)) * 16;
+    auto read_scales = [&](Scales &s, int ks) {   // E8M0: of steps ks and ks + 1 (ks even)
+        const char *from = scales + (ks / CHUNK & 1) * SLOT + ks % CHUNK * SB;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (E8M0) s.x[i] = __builtin_amdgcn_raw_buffer_load_b16(res_xs, xs_row + i * xs_step, at & ~1, 0);
-            else s.x[i] = __builtin_amdgcn_raw_buffer_load_b32(res_xs, xs_row + i * xs_step, at, 0);
+            if (E8M0) s.x[i] = *reinterpret_cast<const uint16_t *>(from + xs_at + i * 256);
+            else s.x[i] = *reinterpret_cast<const uint32_t *>(from + xs_at + i * 256);
         }
-        s.w = E8M0 ? *reinterpret_cast<const uint16_t *>(ws + (at & ~1)) : *reinterpret_cast<const uint32_t *>(ws + at);
+        s.w = E8M0 ? *reinterpret_cast<const uint16_t *>(from + ws_at) : *reinterpret_cast<const uint32_t *>(from + ws_at);
     };
+    // What stands behind a row's last scale may be anything, and its products are of zeros: one.
     auto close_scales = [&](Scales &s, int ks) {
         const uint32_t keep = ks + 1 < nk ? 0xffffu : 0xffu, put = ks + 1 < nk ? 0u : 0x7f00u;
 #pragma unroll
@@ -310,7 +321,6 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
             __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
-            if (decltype(odd)::value == 0) read_scales(ns, ks + 2);
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
                 fetch_x(cur, ks + 2, j);
@@ -318,11 +328,11 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
                 for (int i = 2; i < 5; ++i) product(i, j, s, odd);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            // all but what this step has asked for: 8 rows of x, and 9 scales
-            if (decltype(odd)::value == 0) __builtin_amdgcn_s_waitcnt(0x4f71);   // vmcnt(17)
-            else __builtin_amdgcn_s_waitcnt(0x0f78);                               // vmcnt(8)
+            __builtin_amdgcn_s_waitcnt(0x0f78);   // vmcnt(8): all but what this step has asked for
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
+            if (decltype(odd)::value == 0 && (ks + 2) % CHUNK == 0) fetch_scales(ks + 2);
+            if (decltype(odd)::value) read_scales(ns, ks + 1);
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
                 fetch_w(cur, ks + 2, j);
@@ -334,11 +344,12 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
             }
         };
         Scales s0, s1;
+        fetch_scales(0);
         fetch(st0, 0);
-        read_scales(s0, 0);
         fetch(st1, 1);
         __builtin_amdgcn_s_waitcnt(0x0070);
         __builtin_amdgcn_s_barrier();
+        read_scales(s0, 0);
 #pragma unroll
         for (int i = 0; i < 2; ++i) x[i] = fragment(st0, fx + i * 2048);
 #pragma unroll
@@ -357,12 +368,15 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
             for (int j = 0; j < NJ; ++j) asm volatile("" : "+a"(acc[i][j]));
     } else {
         // Two wavefronts to a SIMD, one buffer read while the other fills; a row of tiles' sums are added under the next row's products.
-        auto step = [&](const Scales &s, Scales &ns, char *cur, char *nxt, int ks) {
+        auto step = [&](char *cur, char *nxt, int ks) {
             __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
             __builtin_amdgcn_s_barrier();         // step ks has landed, and everybody is done with the other buffer
             __builtin_amdgcn_sched_barrier(0);
+            Scales s;
+            read_scales(s, ks);   // (ahead of the loads: behind them it would wait for them)
+            __builtin_amdgcn_sched_barrier(0);
             fetch(nxt, ks + 1);
-            read_scales(ns, ks + 1);
+            fetch_scales(ks + 1, (ks + 1) % CHUNK == 0);   // (a branch here, and the accumulators do not stay where they are)
             i32x8 w[NJ], x[2];
             x[0] = fragment(cur, fx);
 #pragma unroll
@@ -383,15 +397,14 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
-        Scales s0, s1;
+        fetch_scales(0);
         fetch(st0, 0);
-        read_scales(s0, 0);
         int ks = 0;
         for (; ks + 1 < nk; ks += 2) {
-            step(s0, s1, st0, st1, ks);
-            step(s1, s0, st1, st0, ks + 1);
+            step(st0, st1, ks);
+            step(st1, st0, ks + 1);
         }
-        if (ks < nk) step(s0, s1, st0, st1, ks);
+        if (ks < nk) step(st0, st1, ks);
     }
     __builtin_amdgcn_s_waitcnt(0x0070);
     __builtin_amdgcn_s_barrier();   // nothing in flight; everybody is done reading
