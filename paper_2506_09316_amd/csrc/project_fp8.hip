@@ -2,186 +2,13 @@
 //     out_j[m][c] = sum_b sx[m][b] sw[c / 128][b] sum_{k in block b} x[m][k] W_j[c][k] (+ bias_j[c])
 // One MFMA of 16 x 16 x 128 covers a block of K.  E8M0 scales ride in the instruction; with fp32 scales it starts from zero and the
 // block's sum is added times sx sw.  Columns are counted in blocks of 128 that never cross an output, as the scales of W are.
-#include "fp8_common.h"
-#include "project_common.h"
+#include "project_fp8.h"
 
 #include <type_traits>
 
 namespace dsla {
 namespace {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
-struct Fp8Args {
-    const uint8_t *x, *w;
-    const void *xs, *ws;
-    const float *bias;
-    void *out[DSLA_MAX_PROJECTIONS];
-    int width[DSLA_MAX_PROJECTIONS];
-    long long M;
-    int K, pitch, out_f32;
-};
-
-// A block of 128 columns: its output, where it starts there and in W, and how many columns exist.
-struct Columns {
-    int j, c0, row, count;
-};
-__device__ __forceinline__ Columns columns_of(const Fp8Args &a, int block)
-{
-    Columns c{0, 0, 0, 0};
-    int n = (a.width[0] + 127) / 128;
-    while (block >= n) {
-        block -= n;
-        c.row += a.width[c.j++];
-        n = (a.width[c.j] + 127) / 128;
-    }
-    c.c0 = 128 * block;
-    c.row += c.c0;
-    c.count = a.width[c.j] - c.c0 < 128 ? a.width[c.j] - c.c0 : 128;
-    return c;
-}
-
-__device__ __forceinline__ u32x2 pack4(f32x4 v)
-{
-    return u32x2{f32_to_bf16_bits(v[0]) | static_cast<uint32_t>(f32_to_bf16_bits(v[1])) << 16, f32_to_bf16_bits(v[2]) | static_cast<uint32_t>(f32_to_bf16_bits(v[3])) << 16};
-}
-__device__ __forceinline__ void store4(const Fp8Args &a, const Columns &c, long long m, int col, f32x4 v)   // columns col .. col + 3 of the block
-{
-    if (a.bias) v += *reinterpret_cast<const f32x4 *>(a.bias + c.row + col);
-    const size_t at = static_cast<size_t>(m) * a.width[c.j] + c.c0 + col;
-    if (a.out_f32) {
-        *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out[c.j]) + at) = v;
-    } else {
-        *reinterpret_cast<u32x2 *>(static_cast<bf16_t *>(a.out[c.j]) + at) = pack4(v);
-    }
-}
-
-constexpr int kOne = 127;   // E8M0
-
-__device__ __forceinline__ i32x8 join(u32x4 a, u32x4 b)
-{
-    return i32x8{static_cast<int>(a[0]), static_cast<int>(a[1]), static_cast<int>(a[2]), static_cast<int>(a[3]),
-                 static_cast<int>(b[0]), static_cast<int>(b[1]), static_cast<int>(b[2]), static_cast<int>(b[3])};
-}
-
-// The product of two fragments from zero.  EXACT: e4m3 is bf16 with fewer bits, and the bf16 instructions add in fp32; the e4m3 ones add in
-// groups of eight products and drop what is below 2^-14 of a group's largest (random operands: 1.4e-5 of the result's 2-norm against
-// 1e-8), which results in bf16 do not show and results in fp32 are asked for.
-__device__ __forceinline__ bf16x8 wide(uint32_t a, uint32_t b)
-{
-    const bf16x2 w[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true)};
-    return bf16x8{w[0][0], w[0][1], w[1][0], w[1][1], w[2][0], w[2][1], w[3][0], w[3][1]};
-}
-template <bool EXACT>
-struct Operand {
-    i32x8 f;
-    __device__ __forceinline__ void set(i32x8 x) { f = x; }
-};
-template <>
-struct Operand<true> {
-    bf16x8 f[4];
-    __device__ __forceinline__ void set(i32x8 x)
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = wide(x[2 * i], x[2 * i + 1]);
-    }
-};
-__device__ __forceinline__ f32x4 product(const Operand<false> &w, const Operand<false> &x)
-{
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.f, x.f, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, kOne, 0, kOne);
-}
-__device__ __forceinline__ f32x4 product(const Operand<true> &w, const Operand<true> &x)
-{
-    f32x4 t = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.f[i], x.f[i], t, 0, 0, 0);
-    return t;
-}
-// What a block's products are multiplied by: two numbers, or 2^exponent (two bytes reach beyond fp32; 255 is NaN).
-template <bool E8M0>
-struct Factor {
-    float f;
-    int exponent = 0;
-    __device__ __forceinline__ Factor(uint32_t x, uint32_t w)
-    {
-        if (E8M0) {
-            f = x == 255u || w == 255u ? __builtin_nanf("") : 1.f;
-            exponent = static_cast<int>(x + w) - 2 * kOne;
-        } else {
-            f = __uint_as_float(x) * __uint_as_float(w);
-        }
-    }
-    __device__ __forceinline__ void add(f32x4 &acc, f32x4 t) const
-    {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] += (E8M0 ? ldexpf(t[e], exponent) : t[e]) * f;
-    }
-};
-
-template <bool E8M0, bool EXACT>
-__global__ __launch_bounds__(256) void project_fp8_kernel(Fp8Args a, unsigned tiles_m)
-{
-    __shared__ __attribute__((aligned(16))) u32x4 sx[128 * 8], sw[128 * 8];
-    const int block = blockIdx.x / tiles_m;
-    const long long m0 = 128LL * (blockIdx.x - static_cast<unsigned>(block) * tiles_m);
-    const Columns cb = columns_of(a, block);
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4;
-    const int wm = wave >> 1, wn = wave & 1;
-    f32x4 acc[4][4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int nk = (a.K + 127) / 128;
-    for (int ks = 0; ks < nk; ++ks) {
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int n = tid + 256 * i, row = n >> 3, c = n & 7, k = 128 * ks + 16 * c, at = row * 8 + (c ^ ((row >> 1) & 7));
-            sx[at] = m0 + row < a.M && k < a.K ? *reinterpret_cast<const u32x4 *>(a.x + static_cast<size_t>(m0 + row) * a.K + k) : u32x4{0, 0, 0, 0};
-            sw[at] = row < cb.count && k < a.K ? *reinterpret_cast<const u32x4 *>(a.w + static_cast<size_t>(cb.row + row) * a.K + k) : u32x4{0, 0, 0, 0};
-        }
-        __syncthreads();
-        Operand<EXACT> fx[4], fw[4];
-        uint32_t scale_x[4];
-        auto scale_at = [&](const void *p, size_t row) -> uint32_t {
-            return E8M0 ? static_cast<const uint8_t *>(p)[row * a.pitch + ks] : static_cast<const uint32_t *>(p)[row * a.pitch + ks];
-        };
-        const uint32_t scale_w = scale_at(a.ws, block);   // (a row of scales for every block of columns)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int rx = 64 * wm + 16 * i + r, rw = 64 * wn + 16 * i + r;
-            fx[i].set(join(sx[rx * 8 + (g ^ ((rx >> 1) & 7))], sx[rx * 8 + ((4 + g) ^ ((rx >> 1) & 7))]));
-            fw[i].set(join(sw[rw * 8 + (g ^ ((rw >> 1) & 7))], sw[rw * 8 + ((4 + g) ^ ((rw >> 1) & 7))]));
-            scale_x[i] = m0 + rx < a.M ? scale_at(a.xs, m0 + rx) : 0u;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const Factor<E8M0> factor(scale_x[i], scale_w);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (E8M0 && !EXACT) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[j].f, fx[i].f, acc[i][j], 0, 0, 0, scale_w, 0, scale_x[i]);
-                else factor.add(acc[i][j], product(fw[j], fx[i]));
-            }
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const long long m = m0 + 64 * wm + 16 * i + r;
-        if (m >= a.M) continue;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int col = 64 * wn + 16 * j + 4 * g;
-            if (col < cb.count) store4(a, cb, m, col, acc[i][j]);
-        }
-    }
-}
 // 16 bytes per lane from a buffer (lane offset `voff`, uniform offset `soff`) into LDS at `lds` (uniform) + 16 * lane
 __device__ __forceinline__ void buffer_load_lds16(__amdgpu_buffer_rsrc_t res, char *lds, uint32_t voff, int soff)
 {
@@ -191,8 +18,6 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const uint8_t *p, si
 {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p + offset), 0, static_cast<int>(bytes), 0x00020000);
 }
-// An offset past the end of every buffer here: zeros.  (The range of a buffer is checked dword by dword, with both offsets.)
-constexpr uint32_t kNowhere = 0x80000000u;
 
 // ---------------------------------------------------------------------------------------------------------------
 // 256 x 256 tiles
@@ -450,244 +275,40 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Few rows: the weights are the traffic
+// Which kernel, which tiles
 // ---------------------------------------------------------------------------------------------------------------
-// A workgroup has 16 MT rows and 16 NT columns; its wavefronts take a stretch of K each and share nothing until their sums are added at the
-// end: no barrier stands between a wavefront's loads.  Its steps of 128 go through a ring of its own in LDS, filled by buffer loads that write
-// LDS directly, an instruction 8 rows of 128 bytes.  What counts is the lines that are asked for, and a scale alone would be one: they come
-// as 16 bytes of every row, 12 steps of E8M0 (from a multiple of four down) or four of fp32 at a time.
-template <int MT, int NT, int NW>
-struct Few {
-    static constexpr int LOADS = 2 * (NT + MT);                            // instructions of a step, scales apart
-    static constexpr uint32_t STAGE = (NT + MT) * 2048, SLOT = (MT + 1) * 256;   // a step's values; 16 bytes of scales of every row
-    static constexpr int ROOM = (160 * 1024 - 256) / NW;                   // bytes of a wavefront
-    static constexpr int SLOTS = ROOM / static_cast<int>(STAGE) == (ROOM - 2 * static_cast<int>(SLOT)) / static_cast<int>(STAGE) ? 2 : 1;
-    static constexpr int FIT = (ROOM - SLOTS * static_cast<int>(SLOT)) / static_cast<int>(STAGE), MOST = 1 + 60 / LOADS;   // (the counter of loads in flight ends at 63)
-    static constexpr int DEPTH = FIT < MOST ? FIT : MOST, MINE = DEPTH * STAGE + SLOTS * SLOT;
+struct Pair {
+    int8_t mt, nt;
 };
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-// Loads that the compiler does not know: whoever reads what they bring waits with wait_loads() first.
-__device__ __forceinline__ void load_to_lds16(uint32_t lds, uint32_t voff, u32x4 res, uint32_t soff)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(voff), "s"(res), "s"(soff) : "m0", "memory");
-}
-__device__ __forceinline__ void load_to_lds4(uint32_t lds, uint32_t voff, u32x4 res, uint32_t soff)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds), "v"(voff), "s"(res), "s"(soff) : "m0", "memory");
-}
-#pragma clang diagnostic pop
-__device__ __forceinline__ u32x4 resource_of(const void *p, size_t offset, uint32_t bytes)
-{
-    const uint64_t at = reinterpret_cast<uint64_t>(p) + offset;
-    return u32x4{static_cast<uint32_t>(at), static_cast<uint32_t>(at >> 32) & 0xffffu, bytes, 0x00020000u};
-}
+constexpr Pair kPairs[] = {{1, 1}, {1, 2}, {1, 3}, {1, 4}, {1, 5}, {2, 1}, {2, 2}, {2, 3}, {2, 4}, {2, 5}, {3, 2}, {3, 3}, {3, 4}, {3, 5}, {4, 2}, {4, 3},
+                           {4, 4}, {4, 5}, {4, 6}, {4, 8}, {5, 4}, {5, 5}, {6, 4}, {6, 5}, {6, 6}, {8, 4}, {8, 5}, {8, 6}, {5, 8}, {6, 8}, {8, 8}};
+constexpr int kExactPairs = 28;   // of them for results in fp32
 
-// 16 columns from column `col` of all outputs on: their output, first column there, and their row of scales.
-struct Tile {
-    int j, c0, scale_row;
+struct Choice {
+    int mt, nt;   // 0: the 256 x 256 tiles
+    double us;
 };
-__device__ __forceinline__ Tile tile_at(const Fp8Args &a, int col)
+Choice choose(long long M, int K, int N, int blocks, bool e8m0, bool exact)
 {
-    Tile t{0, col, 0};
-    while (t.c0 >= a.width[t.j]) {
-        t.scale_row += (a.width[t.j] + 127) / 128;
-        t.c0 -= a.width[t.j++];
+    const double k = 128.0 * ((K + 127) / 128) / 1024;
+    const double bytes = (static_cast<double>(M) + N) * K + static_cast<double>(M) * N * (exact ? 4 : 2), memory = bytes / 5.4e6;
+    Choice best{0, 0, 1e30};
+    for (int n = 0; n < (exact ? kExactPairs : static_cast<int>(sizeof(kPairs) / sizeof(Pair))); ++n) {
+        const int mt = kPairs[n].mt, nt = kPairs[n].nt;
+        if (mt > 1 && 16 * (mt - 1) >= M) continue;   // rows of tiles that nobody needs
+        const double tiles = static_cast<double>((M + 16 * mt - 1) / (16 * mt)) * ((N + 16 * nt - 1) / (16 * nt)), rounds = __builtin_ceil(tiles / 256);
+        const double p = mt + nt, q = mt * nt;
+        const double work = 3 + rounds * (0.14 * q + (0.19 * p + (exact ? 0.03 : (e8m0 ? 0.006 : 0.02)) * q) * k);
+        const double wait = 2.5 + memory * (1 + 0.3 * (256 * rounds / tiles - 1)) + (rounds - 1);
+        const double us = (work > wait || tiles < 256 ? work : wait) + 0.1 * work;
+        if (us < best.us) best = Choice{mt, nt, us};
     }
-    t.scale_row += t.c0 / 128;
-    return t;
-}
-
-template <int MT, int NT, int NW, bool E8M0, bool EXACT>
-__global__ __launch_bounds__(64 * NW) void project_fp8_rows_kernel(Fp8Args a, int N, int tiles_m, int tiles_n, long long per_xcd)
-{
-    using F = Few<MT, NT, NW>;
-    constexpr int DEPTH = F::DEPTH, SB = E8M0 ? 1 : 4;
-    __shared__ __attribute__((aligned(1024))) char ring[NW * F::MINE];
-    int tm, tn;
-    if (!tile_of(tiles_m, tiles_n, tiles_m, per_xcd, tm, tn)) return;
-    const int n0 = tn * 16 * NT, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-    const long long m0 = 16LL * MT * tm;
-    const int M = a.M - m0 < 16 * MT ? static_cast<int>(a.M - m0) : 16 * MT;   // rows here
-    char *mine = ring + wave * F::MINE;
-    const uint32_t mine_lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char *)mine));
-
-    // ---- loading: piece c of a row R sits at position c ^ (R / 2 % 8).  What does not exist - rows, pieces behind K - arrives as zeros. ----
-    const int cols = N - n0 < 16 * NT ? N - n0 : 16 * NT;
-    const u32x4 res_w = resource_of(a.w, static_cast<size_t>(n0) * a.K, static_cast<uint32_t>(cols) * static_cast<uint32_t>(a.K));
-    const u32x4 res_x = resource_of(a.x, static_cast<size_t>(m0) * a.K, static_cast<uint32_t>(M) * static_cast<uint32_t>(a.K));
-    const uint32_t scale_bytes = static_cast<uint32_t>(a.pitch) * SB;
-    // The 16-column tiles one after the other: where their scales are and where their results go.
-    __shared__ u32x4 table[NT];   // (address of the first column in the first row, width)
-    Tile t = tile_at(a, n0);
-    const int first_scale = t.scale_row;
-    uint32_t ws_off = kNowhere;
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        if (16 * j >= cols) break;
-        if (lane == j) ws_off = static_cast<uint32_t>(t.scale_row - first_scale) * scale_bytes;
-        const uint64_t to = reinterpret_cast<uint64_t>(a.out[t.j]) + (static_cast<size_t>(m0) * a.width[t.j] + t.c0) * (EXACT ? 4 : 2);
-        if (threadIdx.x == 0) table[j] = u32x4{static_cast<uint32_t>(to), static_cast<uint32_t>(to >> 32), static_cast<uint32_t>(a.width[t.j]), 0u};
-        if (16 * (j + 1) >= cols) break;
-        t.c0 += 16;
-        if (t.c0 >= a.width[t.j]) {
-            t.c0 = 0;
-            ++t.scale_row;
-            ++t.j;
-        } else if (t.c0 % 128 == 0) {
-            ++t.scale_row;
-        }
+    if (!exact) {
+        const double tiles = static_cast<double>((M + 255) / 256) * ((blocks + 1) / 2), rounds = __builtin_ceil(tiles / 256);
+        const double work = 3 + rounds * (e8m0 ? 6.5 + 10.9 * k : 5 + 13.5 * k), us = 1.1 * (work > memory ? work : memory);
+        if (us < best.us) best = Choice{0, 0, us};
     }
-    const u32x4 res_ws = resource_of(a.ws, static_cast<size_t>(first_scale) * scale_bytes, static_cast<uint32_t>(t.scale_row - first_scale + 1) * scale_bytes);
-    const u32x4 res_xs = resource_of(a.xs, static_cast<size_t>(m0) * scale_bytes, static_cast<uint32_t>(M) * scale_bytes);
-    constexpr uint32_t SCALES = DEPTH * F::STAGE;
-    const uint32_t xs_off = lane * scale_bytes;
-    const int piece[2] = {(lane & 7) ^ (lane >> 4), (lane & 7) ^ (4 + (lane >> 4))};   // of instructions with an even and an odd number
-    const uint32_t row_off = static_cast<uint32_t>(lane >> 3) * static_cast<uint32_t>(a.K), row_step = 8u * static_cast<uint32_t>(a.K);
-    // This wavefront's stretch of K; neighbours in N begin with another one, so that what is asked for at one time spreads over the memory channels.
-    const int nk = (a.K + 127) / 128, part = (wave + tn) % NW, first = static_cast<int>(static_cast<long long>(nk) * part / NW);
-    const int steps = static_cast<int>(static_cast<long long>(nk) * (part + 1) / NW) - first;
-    constexpr int CHUNK = E8M0 ? 12 : 4;   // steps that 16 bytes of scales reach for
-    auto issue_scales = [&](int i) {   // of the steps from i on (the waits below count without them, and so wait for a little more)
-        const int ks = first + i;
-        const uint32_t at = mine_lds + SCALES + i / CHUNK % F::SLOTS * F::SLOT, s0 = E8M0 ? ks & ~3 : 4 * ks;
-#pragma unroll
-        for (int n = 0; n < (MT + 3) / 4; ++n)
-            if (lane < 16 * MT - 64 * n) load_to_lds16(at + n * 1024, xs_off + 64 * n * scale_bytes, res_xs, s0);
-        if (lane < NT) load_to_lds16(at + MT * 256, ws_off, res_ws, s0);
-    };
-    auto issue = [&](int i, int slot) {
-        const int ks = first + i, left = a.K - 128 * ks;
-        const uint32_t at = mine_lds + slot * F::STAGE, k0 = 128 * ks;
-        const bool there[2] = {16 * piece[0] < left, 16 * piece[1] < left};
-        if (i % CHUNK == 0 && (F::SLOTS == 2 || i == 0)) issue_scales(i);
-#pragma unroll
-        for (int n = 0; n < 2 * NT; ++n) load_to_lds16(at + n * 1024, there[n & 1] ? row_off + n * row_step + 16 * piece[n & 1] : kNowhere, res_w, k0);
-#pragma unroll
-        for (int n = 0; n < 2 * MT; ++n) load_to_lds16(at + (2 * NT + n) * 1024, there[n & 1] ? row_off + n * row_step + 16 * piece[n & 1] : kNowhere, res_x, k0);
-    };
-
-    f32x4 acc[MT][NT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < DEPTH; ++i)
-        if (i < steps) issue(i, i);
-    const uint32_t pos = static_cast<uint32_t>(g ^ (r >> 1)) << 4;
-    int slot = 0;
-    for (int i = 0; i < steps; ++i) {
-        if (F::SLOTS == 1 && i > 0 && i % CHUNK == 0) {   // (the scales before have been read)
-            issue_scales(i);
-            wait_loads<0>();
-        } else if (i + DEPTH <= steps) {
-            wait_loads<F::LOADS * (DEPTH - 1)>();
-        } else {
-            wait_loads<0>();
-        }
-        const char *st = mine + slot * F::STAGE;
-        i32x8 w[NT], x[MT];
-        uint32_t sw[NT], sx[MT];
-        auto fragment = [&](int tile) {
-            const char *row = st + tile * 2048 + r * 128;
-            return join(*reinterpret_cast<const u32x4 *>(row + pos), *reinterpret_cast<const u32x4 *>(row + (pos ^ 64)));
-        };
-        const int chunk = i - i % CHUNK, ahead = E8M0 ? first + i - ((first + chunk) & ~3) : i - chunk;
-        const char *scales = mine + SCALES + i / CHUNK % F::SLOTS * F::SLOT;
-        auto scale_of = [&](int row) -> uint32_t {
-            if (E8M0) return reinterpret_cast<const uint8_t *>(scales)[16 * row + ahead];
-            return *reinterpret_cast<const uint32_t *>(scales + 16 * row + 4 * ahead);
-        };
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            w[j] = fragment(j);
-            sw[j] = scale_of(16 * MT + j);
-        }
-#pragma unroll
-        for (int j = 0; j < MT; ++j) {
-            x[j] = fragment(NT + j);
-            sx[j] = scale_of(16 * j + r);
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (i + DEPTH < steps) issue(i + DEPTH, slot);
-        slot = slot + 1 == DEPTH ? 0 : slot + 1;
-        Operand<EXACT> ow[NT];
-#pragma unroll
-        for (int j = 0; j < NT; ++j) ow[j].set(w[j]);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            Operand<EXACT> ox;
-            ox.set(x[m]);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                if constexpr (E8M0 && !EXACT) acc[m][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ow[j].f, ox.f, acc[m][j], 0, 0, 0, sw[j], 0, sx[m]);
-                else Factor<E8M0>(sx[m], sw[j]).add(acc[m][j], product(ow[j], ox));
-            }
-        }
-    }
-
-    // ---- the wavefronts' sums, added in the order of K, as many rows of tiles at a time as fit; then whole rows leave.  Lane (r, g) of a tile in
-    // column j sits at (r + j) % 16, g: 16 lanes that read a row find their own banks ----
-    constexpr int ROWS = static_cast<int>(sizeof(ring)) / (NW * NT * 1024) < MT ? static_cast<int>(sizeof(ring)) / (NW * NT * 1024) : MT;
-    static_assert(ROWS >= 1, "the sums of a row of tiles have to fit");
-    f32x4 *sums = reinterpret_cast<f32x4 *>(ring);
-#pragma unroll
-    for (int p = 0; p < MT; p += ROWS) {
-        __syncthreads();
-#pragma unroll
-        for (int i = p; i < p + ROWS && i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) sums[((wave * ROWS + i - p) * NT + j) * 64 + ((r + j) & 15) * 4 + g] = acc[i][j];
-        __syncthreads();
-        constexpr int G = 4 * NT, AT_ONCE = 64 * NW / G;   // groups of four columns of a row; rows at a time
-        const int c = threadIdx.x % G, col = n0 + 4 * c, last = M - 16 * p < 16 * ROWS ? M - 16 * p : 16 * ROWS;
-        if (threadIdx.x >= AT_ONCE * G || col >= N) continue;
-        const u32x4 to = table[c >> 2];
-        char *out = reinterpret_cast<char *>(static_cast<uint64_t>(to[1]) << 32 | to[0]) + 4 * (c & 3) * (EXACT ? 4 : 2);
-        const f32x4 bias = a.bias ? *reinterpret_cast<const f32x4 *>(a.bias + col) : f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int row = threadIdx.x / G; row < last; row += AT_ONCE) {
-            const int at = ((row >> 4) * NT + (c >> 2)) * 64 + ((row + (c >> 2)) & 15) * 4 + (c & 3);
-            f32x4 v = sums[(-tn & (NW - 1)) * ROWS * NT * 64 + at];
-#pragma unroll
-            for (int k = 1; k < NW; ++k) v += sums[((k - tn) & (NW - 1)) * ROWS * NT * 64 + at];
-            v += bias;
-            char *here = out + static_cast<size_t>(16 * p + row) * to[2] * (EXACT ? 4 : 2);
-            if (EXACT) *reinterpret_cast<f32x4 *>(here) = v;
-            else *reinterpret_cast<u32x2 *>(here) = pack4(v);
-        }
-    }
-}
-
-template <int MT, int NT>
-void launch_few(ProfileScope &ps, const Fp8Args &a, int N, bool e8m0, hipStream_t stream)
-{
-    constexpr int NW = Few<MT, NT, 8>::DEPTH >= 1 ? 8 : 4;
-    const int tiles_m = static_cast<int>((a.M + 16 * MT - 1) / (16 * MT)), tiles_n = (N + 16 * NT - 1) / (16 * NT);
-    const long long per_xcd = ((static_cast<long long>(tiles_m) * tiles_n + 7) / 8 + tiles_m - 1) / tiles_m * tiles_m;   // whole columns to an XCD
-    const dim3 grid(static_cast<unsigned>(8 * per_xcd));
-    if (e8m0 && a.out_f32) DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, NW, true, true>), grid, dim3(64 * NW), 0, stream, a, N, tiles_m, tiles_n, per_xcd);
-    else if (e8m0) DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, NW, true, false>), grid, dim3(64 * NW), 0, stream, a, N, tiles_m, tiles_n, per_xcd);
-    else if (a.out_f32) DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, NW, false, true>), grid, dim3(64 * NW), 0, stream, a, N, tiles_m, tiles_n, per_xcd);
-    else DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, NW, false, false>), grid, dim3(64 * NW), 0, stream, a, N, tiles_m, tiles_n, per_xcd);
-}
-template <int MT>
-void launch_few_n(ProfileScope &ps, const Fp8Args &a, int N, int nt, bool e8m0, hipStream_t stream)
-{
-    if (nt <= 1) launch_few<MT, 1>(ps, a, N, e8m0, stream);
-    else if (nt == 2) launch_few<MT, 2>(ps, a, N, e8m0, stream);
-    else if (nt == 3) launch_few<MT, 3>(ps, a, N, e8m0, stream);
-    else if (nt == 4) launch_few<MT, 4>(ps, a, N, e8m0, stream);
-    else launch_few<MT, 5>(ps, a, N, e8m0, stream);
-}
-void launch_few_m(ProfileScope &ps, const Fp8Args &a, int N, int mt, int nt, bool e8m0, hipStream_t stream)
-{
-    if (mt <= 1) launch_few_n<1>(ps, a, N, nt, e8m0, stream);
-    else if (mt == 2) launch_few_n<2>(ps, a, N, nt, e8m0, stream);
-    else if (mt == 3) launch_few_n<3>(ps, a, N, nt, e8m0, stream);
-    else if (mt == 4) launch_few_n<4>(ps, a, N, nt, e8m0, stream);
-    else launch_few_n<5>(ps, a, N, nt, e8m0, stream);
+    return best;
 }
 }  // namespace
 
@@ -713,26 +334,17 @@ hipError_t launch_project_fp8(int64_t M, int K, int n_out, const int32_t *widths
     }
     ProfileScope ps(DSLA_KERNEL_PROJECT_FP8, stream);
     const bool e8m0 = scale_type == DSLA_SCALE_E8M0, exact = out_dtype == DSLA_F32;
-    if (M <= 64) {
-        const int nt = (N + 16 * 256 - 1) / (16 * 256);
-        launch_few_m(ps, a, N, static_cast<int>((M + 15) / 16), nt, e8m0, stream);
+    const Choice c = choose(M, K, N, blocks, e8m0, exact);
+    if (c.mt) {
+        if (!(exact ? launch_fp8_rows_exact : launch_fp8_rows)(ps, a, N, c.mt, c.nt, e8m0, stream)) return hipErrorInvalidValue;
         return hipGetLastError();
     }
-    if (!exact && M > 512) {
-        const int tiles_m = static_cast<int>((M + 255) / 256), tiles_n = (blocks + 1) / 2;
-        const long long per_xcd = (static_cast<long long>(tiles_m) * tiles_n + 7) / 8;
-        const dim3 grid(static_cast<unsigned>(8 * per_xcd));
-        const int group = tiles_m <= 5 ? tiles_m : 4;
-        if (e8m0) DSLA_LAUNCH(ps, project_fp8_tile_kernel<true>, grid, dim3(256), 0, stream, a, tiles_m, tiles_n, blocks, group, per_xcd);
-        else DSLA_LAUNCH(ps, project_fp8_tile_kernel<false>, grid, dim3(512), 0, stream, a, tiles_m, tiles_n, blocks, group, per_xcd);
-        return hipGetLastError();
-    }
-    const unsigned tiles_m = static_cast<unsigned>((M + 127) / 128);
-    const dim3 grid(tiles_m * static_cast<unsigned>(blocks));
-    if (e8m0 && exact) DSLA_LAUNCH(ps, (project_fp8_kernel<true, true>), grid, dim3(256), 0, stream, a, tiles_m);
-    else if (e8m0) DSLA_LAUNCH(ps, (project_fp8_kernel<true, false>), grid, dim3(256), 0, stream, a, tiles_m);
-    else if (exact) DSLA_LAUNCH(ps, (project_fp8_kernel<false, true>), grid, dim3(256), 0, stream, a, tiles_m);
-    else DSLA_LAUNCH(ps, (project_fp8_kernel<false, false>), grid, dim3(256), 0, stream, a, tiles_m);
+    const int tiles_m = static_cast<int>((M + 255) / 256), tiles_n = (blocks + 1) / 2;
+    const long long per_xcd = (static_cast<long long>(tiles_m) * tiles_n + 7) / 8;
+    const dim3 grid(static_cast<unsigned>(8 * per_xcd));
+    const int group = tiles_m <= 5 ? tiles_m : 4;
+    if (e8m0) DSLA_LAUNCH(ps, project_fp8_tile_kernel<true>, grid, dim3(256), 0, stream, a, tiles_m, tiles_n, blocks, group, per_xcd);
+    else DSLA_LAUNCH(ps, project_fp8_tile_kernel<false>, grid, dim3(512), 0, stream, a, tiles_m, tiles_n, blocks, group, per_xcd);
     return hipGetLastError();
 }
 
