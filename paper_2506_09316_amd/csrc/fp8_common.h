@@ -8,6 +8,17 @@ namespace dsla {
 constexpr float kLeastAmax = 0x1p-100f;
 constexpr float kMostE4m3 = 448.f;
 
+// n / d for n below 2^31 (Granlund and Montgomery's multiplication).
+struct Divisor {
+    uint32_t factor, shift;
+    explicit Divisor(uint32_t d) : factor(0), shift(0)
+    {
+        while ((1ull << shift) < d) ++shift;
+        factor = static_cast<uint32_t>(((1ull << 32) * ((1ull << shift) - d)) / d + 1);
+    }
+    __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return (__umulhi(n, factor) + n) >> shift; }
+};
+
 __host__ __device__ __forceinline__ int scale_pitch(int cols) { return DSLA_SCALE_PITCH(cols); }
 
 // A block's scale from its largest finite magnitude: what is stored, and what values are multiplied by.  E8M0: 448 = 1.75 * 2^8, so
@@ -41,15 +52,23 @@ __device__ __forceinline__ float finite_magnitude(float x)
     const float a = fabsf(x);
     return a < __builtin_inff() ? a : 0.f;   // (NaN: 0)
 }
-
-// x / scale as e4m3 sees it: at most 448 (the product may be an ulp above), NaN for what was not finite.
-__device__ __forceinline__ float in_range(float x, float inverse)
+// The largest of them among n values: the maximum passes over NaN, and only where an infinity is among them they are looked at again.
+template <int N>
+__device__ __forceinline__ float largest(const float (&f)[N])
 {
-    const float v = x * inverse;
-    return fabsf(v) < 512.f ? fminf(fmaxf(v, -kMostE4m3), kMostE4m3) : __builtin_nanf("");
+    float a = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) a = fmaxf(a, fabsf(f[i]));
+    if (a == __builtin_inff()) {
+        a = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) a = fmaxf(a, finite_magnitude(f[i]));
+    }
+    return a;
 }
 
-// Four values to four bytes, rounded to nearest even.
+// Four values to four bytes, rounded to nearest even.  Times the inverse of their scale they are at most 448, or with fp32 scales an ulp more,
+// which rounds to 448; infinities and NaN become NaN.
 __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d)
 {
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);

@@ -88,12 +88,19 @@ __device__ __forceinline__ float sum_all(float x, float *s)
     return t;
 }
 
+// act(z), to 6 ulps: e^-|z| (a large gate does not overflow) as a power of two whose exponent carries the rounding of |z| log2 e along, and an inverse
+// with one step of Newton's.  The library's exponential and quotient are more instructions, which bound the kernels: 16384 rows of 32 heads 82 us
+// with them.
 __device__ __forceinline__ float activated(float z, int act)
 {
     if (act == DSLA_ACT_NONE) return z;
-    const float t = expf(-fabsf(z));   // (of a negative number: a large gate does not overflow)
+    constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f;
+    const float a = fabsf(z) > 200.f ? -200.f : -fabsf(z);   // (e^-200 is 0; NaN stays)
+    const float p = a * kLog2e, n = rintf(p), rest = fmaf(a, kLog2eRest, fmaf(a, kLog2e, -p));
+    const float t = ldexpf(__builtin_amdgcn_exp2f((p - n) + rest), static_cast<int>(n));   // (the instruction alone has no results below 2^-126)
+    const float d = 1.f + t, y = __builtin_amdgcn_rcpf(d), inverse = fmaf(y, fmaf(-d, y, 1.f), y);
     const float top = z < 0.f ? t : 1.f;
-    return (act == DSLA_ACT_SIGMOID ? top : z * top) / (1.f + t);
+    return (act == DSLA_ACT_SIGMOID ? top : z * top) * inverse;
 }
 
 // 8 values of a lane to where they go: as they are, or as e4m3 with the scale of the block that the lane's row of 16 holds (lanes without
@@ -105,13 +112,10 @@ struct Result {
 template <bool E8M0>
 __device__ __forceinline__ void store_block(const Result &o, const float (&f)[8], bool valid, size_t at, long long row, int block)
 {
-    float a = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) a = fmaxf(a, finite_magnitude(f[i]));
-    const BlockScale<E8M0> s(max16(a));
+    const BlockScale<E8M0> s(max16(largest(f)));
     float v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = in_range(f[i], s.inverse);
+    for (int i = 0; i < 8; ++i) v[i] = f[i] * s.inverse;
     if (valid) __builtin_nontemporal_store(u32x2{e4m3x4(v[0], v[1], v[2], v[3]), e4m3x4(v[4], v[5], v[6], v[7])},
                                            reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(o.p) + at));
     if (valid && threadIdx.x % 16 == 0) s.store(o.scale, static_cast<size_t>(row) * o.pitch + block);
@@ -229,56 +233,77 @@ struct RowsArgs {
     const void *x, *gate;
     const float *weight;   // [d], null: no norm
     Result o;
-    long long blocks;      // rows * blocks of a row
+    uint32_t blocks;       // rows * blocks of a row
     int cols, per_row, act;
     float eps;
+    Divisor by_row;
 };
 
-// 16 lanes to a block of 128 columns of a row: one head of 128, two of 64, or 128 plain values.
-template <int D, class TIO>
+// 16 lanes to a block of 128 columns of a row - one head of 128, two of 64, or 128 plain values - and NB blocks to 16 lanes, all of them
+// asked for before the first is used.
+template <int D, int NB, class TIO>
 __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a)
 {
     const int l = threadIdx.x & 15;
-    const long long n = blockIdx.x * 16LL + (threadIdx.x >> 4);
-    const bool there = n < a.blocks;
-    const long long row = there ? n / a.per_row : 0;
-    const int block = there ? static_cast<int>(n - row * a.per_row) : 0, col = 128 * block + 8 * l;
-    const bool valid = there && col < a.cols;
-    const size_t at = static_cast<size_t>(row) * a.cols + col;
-    float f[8] = {}, g[8] = {};
-    if (valid) {
-        load8(static_cast<const TIO *>(a.x) + at, f);
-        if (a.gate) load8(static_cast<const TIO *>(a.gate) + at, g);
-    }
-    if (D && a.weight) {
-        float q = 0.f, w[8];
+    float f[NB][8], g[NB][8], w[8];
+    uint32_t row[NB];
+    int block[NB];
+    bool valid[NB];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q += f[i] * f[i];
-        if (D == 128) {
-            q = sum16(q);
-        } else {   // 8 lanes: l ^ 4, l ^ 2, l ^ 1
-            q += __shfl_xor(q, 4);
-            q += __shfl_xor(q, 2);
-            q += __shfl_xor(q, 1);
+    for (int u = 0; u < NB; ++u) {
+        const uint32_t n = (blockIdx.x * NB + u) * 16u + (threadIdx.x >> 4);
+        const bool there = n < a.blocks;
+        row[u] = a.by_row.quotient(there ? n : 0u);
+        block[u] = there ? static_cast<int>(n - row[u] * a.per_row) : 0;
+        valid[u] = there && 128 * block[u] + 8 * l < a.cols;
+        const size_t at = static_cast<size_t>(row[u]) * a.cols + 128 * block[u] + 8 * l;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[u][i] = g[u][i] = 0.f;
+        if (valid[u]) {
+            load8(static_cast<const TIO *>(a.x) + at, f[u]);
+            if (D && a.gate) load8(static_cast<const TIO *>(a.gate) + at, g[u]);
         }
-        const float inv = 1.f / sqrtf(q / D + a.eps);
-        load8_kept(a.weight + (8 * l) % D, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] *= inv * w[i];
     }
-    if (a.gate) {
+    if (D && a.weight) load8_kept(a.weight + (8 * l) % (D ? D : 8), w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] *= activated(g[i], a.act);
+    for (int u = 0; u < NB; ++u) {
+        if (D && a.weight) {
+            float q = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q += f[u][i] * f[u][i];
+            if (D == 128) {
+                q = sum16(q);
+            } else {   // 8 lanes: l ^ 4, l ^ 2, l ^ 1
+                q += __shfl_xor(q, 4);
+                q += __shfl_xor(q, 2);
+                q += __shfl_xor(q, 1);
+            }
+            const float inv = 1.f / sqrtf(q / (D ? D : 1) + a.eps);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[u][i] *= inv * w[i];
+        }
+        if (D && a.gate) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[u][i] *= activated(g[u][i], a.act);
+        }
+        store_result(a.o, f[u], valid[u], static_cast<size_t>(row[u]) * a.cols + 128 * block[u] + 8 * l, row[u], block[u]);
     }
-    store_result(a.o, f, valid, at, row, block);
 }
 
-template <int D>
+template <int D, int NB>
 void launch_rows(ProfileScope &ps, const RowsArgs &a, bool f32, hipStream_t stream)
 {
-    const dim3 grid(static_cast<unsigned>((a.blocks + 15) / 16));
-    if (f32) DSLA_LAUNCH(ps, (rows_kernel<D, float>), grid, dim3(256), 0, stream, a);
-    else DSLA_LAUNCH(ps, (rows_kernel<D, bf16_t>), grid, dim3(256), 0, stream, a);
+    const dim3 grid((a.blocks + 16u * NB - 1) / (16u * NB));
+    if (f32) DSLA_LAUNCH(ps, (rows_kernel<D, NB, float>), grid, dim3(256), 0, stream, a);
+    else DSLA_LAUNCH(ps, (rows_kernel<D, NB, bf16_t>), grid, dim3(256), 0, stream, a);
+}
+// Several blocks to 16 lanes where every compute unit has eight workgroups of them.
+template <int D>
+void launch_rows_of(ProfileScope &ps, const RowsArgs &a, bool f32, hipStream_t stream)
+{
+    constexpr int NB = D ? 2 : 4;
+    if (a.blocks >= 8u * 256u * 16u * NB) launch_rows<D, NB>(ps, a, f32, stream);
+    else launch_rows<D, 1>(ps, a, f32, stream);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -308,9 +333,7 @@ __global__ __launch_bounds__(256) void square_kernel(SquareArgs a)
         if (row < a.rows && col < a.cols) load8(static_cast<const TIO *>(a.x) + static_cast<size_t>(row) * a.cols + col, f[c]);
     }
 #pragma unroll
-    for (int c = 0; c < 8; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m = fmaxf(m, finite_magnitude(f[c][i]));
+    for (int c = 0; c < 8; ++c) m = fmaxf(m, largest(f[c]));
     m = max16(m);
     if (l == 0) s_max[r0] = m;
     __syncthreads();
@@ -321,7 +344,7 @@ __global__ __launch_bounds__(256) void square_kernel(SquareArgs a)
         if (row >= a.rows || col >= a.cols) continue;
         float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = in_range(f[c][i], s.inverse);
+        for (int i = 0; i < 8; ++i) v[i] = f[c][i] * s.inverse;
         __builtin_nontemporal_store(u32x2{e4m3x4(v[0], v[1], v[2], v[3]), e4m3x4(v[4], v[5], v[6], v[7])},
                                     reinterpret_cast<u32x2 *>(a.q + static_cast<size_t>(row) * a.cols + col));
     }
@@ -350,10 +373,10 @@ hipError_t launch_residual_norm(const dsla_norm &n, int64_t rows, const void *x,
 hipError_t launch_head_norm(const dsla_heads &n, int64_t rows, const void *o, const void *gate, void *out, void *out_scale, hipStream_t stream)
 {
     const int cols = n.H * n.d, per_row = (cols + 127) / 128;
-    RowsArgs a{o, gate, n.weight, result_of(out, out_scale, n.out_dtype, n.scale_type, cols), rows * per_row, cols, per_row, n.gate_act, n.eps};
+    RowsArgs a{o, gate, n.weight, result_of(out, out_scale, n.out_dtype, n.scale_type, cols), static_cast<uint32_t>(rows * per_row), cols, per_row, n.gate_act, n.eps, Divisor(per_row)};
     ProfileScope ps(DSLA_KERNEL_HEAD_NORM, stream);
-    if (n.d == 128) launch_rows<128>(ps, a, n.io_dtype == DSLA_F32, stream);
-    else launch_rows<64>(ps, a, n.io_dtype == DSLA_F32, stream);
+    if (n.d == 128) launch_rows_of<128>(ps, a, n.io_dtype == DSLA_F32, stream);
+    else launch_rows_of<64>(ps, a, n.io_dtype == DSLA_F32, stream);
     return hipGetLastError();
 }
 
@@ -362,8 +385,8 @@ hipError_t launch_quantize(int64_t rows, int cols, int in_dtype, int block_rows,
     const int per_row = (cols + 127) / 128;
     ProfileScope ps(DSLA_KERNEL_QUANTIZE, stream);
     if (block_rows == 1) {
-        RowsArgs a{x, nullptr, nullptr, result_of(q, scale, DSLA_E4M3, scale_type, cols), rows * per_row, cols, per_row, DSLA_ACT_NONE, 0.f};
-        launch_rows<0>(ps, a, in_dtype == DSLA_F32, stream);
+        RowsArgs a{x, nullptr, nullptr, result_of(q, scale, DSLA_E4M3, scale_type, cols), static_cast<uint32_t>(rows * per_row), cols, per_row, DSLA_ACT_NONE, 0.f, Divisor(per_row)};
+        launch_rows_of<0>(ps, a, in_dtype == DSLA_F32, stream);
     } else {
         const SquareArgs a{x, static_cast<uint8_t *>(q), scale, rows, cols, scale_pitch(cols), per_row};
         const dim3 grid(static_cast<unsigned>((rows + 127) / 128 * per_row));

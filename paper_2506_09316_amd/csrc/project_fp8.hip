@@ -288,24 +288,35 @@ struct Choice {
     int mt, nt;   // 0: the 256 x 256 tiles
     double us;
 };
+// The fewest microseconds by an estimate, fitted to 9600 random products of up to 8192 rows and every pair (rms 15 %; with the XCDs evenly
+// filled less): a round of workgroups over the compute units costs its start, its sums (mt nt), and for every 1024 of K its loads (mt + nt) and
+// products (mt nt); beside that the memory.
+struct Cost {
+    double call, round, sums, loads, products, next;
+};
+constexpr Cost kRowsCost[3] = {{2.6, 0.48, 0.13, 0.117, 0.029, 1.6},     // E8M0
+                               {2.2, 0.83, 0.147, 0.083, 0.074, 1.0},    // fp32 scales: sums by vector instructions
+                               {2.0, 1.2, 0.155, 0.10, 0.11, 0.9}};      // results in fp32: operands in bf16
+constexpr double kTileRound[2][2] = {{7.0, 10.4}, {4.0, 13.0}};           // 256 x 256 tiles, E8M0 and fp32: of a round, and for every 1024 of K
 Choice choose(long long M, int K, int N, int blocks, bool e8m0, bool exact)
 {
     const double k = 128.0 * ((K + 127) / 128) / 1024;
-    const double bytes = (static_cast<double>(M) + N) * K + static_cast<double>(M) * N * (exact ? 4 : 2), memory = bytes / 5.4e6;
+    const double memory = 2.5 + ((static_cast<double>(M) + N) * K + static_cast<double>(M) * N * (exact ? 4 : 2)) / 6.2e6;
+    const auto both = [&](double work) { return work > memory ? work + 0.2 * memory : memory + 0.2 * work; };
+    const Cost &c = kRowsCost[exact ? 2 : (e8m0 ? 0 : 1)];
     Choice best{0, 0, 1e30};
     for (int n = 0; n < (exact ? kExactPairs : static_cast<int>(sizeof(kPairs) / sizeof(Pair))); ++n) {
         const int mt = kPairs[n].mt, nt = kPairs[n].nt;
-        if (mt > 1 && 16 * (mt - 1) >= M) continue;   // rows of tiles that nobody needs
-        const double tiles = static_cast<double>((M + 16 * mt - 1) / (16 * mt)) * ((N + 16 * nt - 1) / (16 * nt)), rounds = __builtin_ceil(tiles / 256);
-        const double p = mt + nt, q = mt * nt;
-        const double work = 3 + rounds * (0.14 * q + (0.19 * p + (exact ? 0.03 : (e8m0 ? 0.006 : 0.02)) * q) * k);
-        const double wait = 2.5 + memory * (1 + 0.3 * (256 * rounds / tiles - 1)) + (rounds - 1);
-        const double us = (work > wait || tiles < 256 ? work : wait) + 0.1 * work;
+        if (mt > 1 && 16LL * (mt - 1) >= M) continue;   // rows of tiles that nobody needs
+        const long long tiles_m = (M + 16 * mt - 1) / (16 * mt), tiles_n = (N + 16 * nt - 1) / (16 * nt);
+        if (tiles_m * tiles_n > 0x70000000LL) continue;
+        const double rounds = static_cast<double>((fp8_rows_per_xcd(tiles_m, tiles_n) + 31) / 32), p = mt + nt, q = mt * nt;
+        const double us = both(c.call + rounds * (c.round + c.sums * q + (c.loads * p + c.products * q) * k) + c.next * (rounds - 1));
         if (us < best.us) best = Choice{mt, nt, us};
     }
     if (!exact) {
         const double tiles = static_cast<double>((M + 255) / 256) * ((blocks + 1) / 2), rounds = __builtin_ceil(tiles / 256);
-        const double work = 3 + rounds * (e8m0 ? 6.5 + 10.9 * k : 5 + 13.5 * k), us = 1.1 * (work > memory ? work : memory);
+        const double us = both(3 + rounds * (kTileRound[!e8m0][0] + kTileRound[!e8m0][1] * k));
         if (us < best.us) best = Choice{0, 0, us};
     }
     return best;

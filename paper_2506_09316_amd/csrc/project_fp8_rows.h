@@ -278,8 +278,7 @@ void launch_few(ProfileScope &ps, const Fp8Args &a, int N, bool e8m0, hipStream_
     // Eight wavefronts where a step of each fits into LDS, and where results are exact also into 256 registers; else four.
     constexpr int NW = Few<MT, NT, 8>::DEPTH >= 1 && (!EXACT || MT + NT <= 8) ? 8 : 4;
     const int tiles_m = static_cast<int>((a.M + 16 * MT - 1) / (16 * MT)), tiles_n = (N + 16 * NT - 1) / (16 * NT);
-    // An XCD has whole columns of tiles: their rows of W come from memory once.
-    const long long per_xcd = ((static_cast<long long>(tiles_m) * tiles_n + 7) / 8 + tiles_m - 1) / tiles_m * tiles_m;
+    const long long per_xcd = fp8_rows_per_xcd(tiles_m, tiles_n);
     const dim3 grid(static_cast<unsigned>(8 * per_xcd));
     if (e8m0) DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, NW, true, EXACT>), grid, dim3(64 * NW), 0, stream, a, N, tiles_m, tiles_n, per_xcd);
     else DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, NW, false, EXACT>), grid, dim3(64 * NW), 0, stream, a, N, tiles_m, tiles_n, per_xcd);

@@ -3,6 +3,7 @@
     python serving_step.py [--layers 16 --B 8 --T 8192 --decode 128]
     python serving_step.py --hybrid [--layers 32 --B 8 --T 8192 --decode 128]
     python serving_step.py --project [--T 16384 --K 4096]
+    python serving_step.py --blocks [--layers 16 --B 8 --T 8192 --K 4096 --decode 128]
     python serving_step.py --multi N [--Hkv 8]
     python serving_step.py --packed {equal,pow2,serving,one_long}
     python serving_step.py --entropy [--B 8 --T 8192]
@@ -428,6 +429,116 @@ def project(M: int, K: int, H: int, d: int):
                       "prefill_kernels_ms": {n: round(v, 4) for n, v in ms.items() if n.startswith("prefill")}}))
 
 
+class Blocks:
+    """Whole blocks of converted layers, their projections in 8 bits: norm, q, k, v, gates and output gate in one product, the layer, norm and
+    gate of its heads, output projection, and the border to the next block.  Weights are quantized once."""
+
+    def __init__(self, L: int, K: int, H: int, d: int, gen):
+        import torch
+        import paper_2506_09316_amd as dsla
+
+        self.dsla, self.torch, self.L, self.K, self.H, self.d = dsla, torch, L, K, H, d
+        width, dev = H * d, "cuda"
+
+        def quantized(rows, cols):
+            w = torch.randn(rows, cols, device=dev, generator=gen) * cols ** -0.5
+            q, s = torch.empty(rows, cols, device=dev, dtype=torch.float8_e4m3fn), torch.empty(-(-rows // 128), dsla.scale_pitch(cols), device=dev, dtype=torch.uint8)
+            s = s.view(torch.float8_e8m0fnu)
+            dsla.dsla_quantize(w, q, s, block_rows=128)
+            return q, s
+
+        def stacked(parts):   # the scales of every output for itself
+            return tuple(torch.cat([p[i].view(torch.uint8) for p in parts]).view(t) for i, t in enumerate((torch.float8_e4m3fn, torch.float8_e8m0fnu)))
+
+        self.inside = [stacked([quantized(width, K) for _ in range(6)]) for _ in range(L)]
+        self.outside = [quantized(K, width) for _ in range(L)]
+        weight = lambda n: 1 + 0.1 * torch.randn(n, device=dev, generator=gen)
+        common = dict(x_dtype=dsla.DSLA_BF16, y_dtype=dsla.DSLA_BF16, eps=1e-5)
+        self.borders = [dsla.make_norm(K, h_dtype=dsla.DSLA_E4M3, pre_weight=weight(K), **common) for _ in range(L)]
+        self.last = dsla.make_norm(K, h_dtype=dsla.DSLA_BF16, pre_weight=weight(K), **common)
+        self.heads = [dsla.make_head_norm(H, d, io_dtype=dsla.DSLA_BF16, out_dtype=dsla.DSLA_E4M3, eps=1e-5, weight=weight(d)) for _ in range(L)]
+
+    def room(self, rows: int):
+        """What a pass over that many tokens writes."""
+        torch, dev, width = self.torch, "cuda", self.H * self.d
+        e4m3 = lambda cols: (torch.empty(rows, cols, device=dev, dtype=torch.float8_e4m3fn),
+                             torch.zeros(rows, self.dsla.scale_pitch(cols), device=dev, dtype=torch.uint8).view(torch.float8_e8m0fnu))
+        bf16 = lambda cols: torch.empty(rows, cols, device=dev, dtype=torch.bfloat16)
+        return dict(h=e4m3(self.K), outs=[bf16(width) for _ in range(6)], o=bf16(width), o8=e4m3(width), y=bf16(self.K), final=bf16(self.K))
+
+    def run(self, x, room, layer):
+        """x [rows, K], updated; layer(l, q, k, v, g1, g2, o) is the call of the layer itself.  Returns the last norm's result."""
+        dsla, y = self.dsla, None
+        for l in range(self.L):
+            dsla.dsla_residual_norm(self.borders[l], x, y, x, room["h"][0], h_scale=room["h"][1])
+            dsla.dsla_project_fp8(*room["h"], *self.inside[l], room["outs"])
+            layer(l, *room["outs"][:5], room["o"])
+            dsla.dsla_head_norm(self.heads[l], room["o"], room["o8"][0], gate=room["outs"][5], out_scale=room["o8"][1])
+            dsla.dsla_project_fp8(*room["o8"], *self.outside[l], [room["y"]])
+            y = room["y"]
+        dsla.dsla_residual_norm(self.last, x, y, x, room["final"])
+        return room["final"]
+
+
+def blocks(L: int, B: int, T: int, K: int, H: int, d: int, decode: int):
+    """Prompt and tokens through L whole blocks of converted layers (without the MLPs), projections in 8 bits; one JSON line."""
+    import time
+    import torch
+    import paper_2506_09316_amd as dsla
+    from paper_2506_09316_amd import binding
+    from paper_2506_09316_amd.binding import DSLA_BF16
+
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(20250609)
+    stack = Blocks(L, K, H, d, gen)
+    make = lambda n, **k: [dsla.make_desc(n, H, d, d, io_dtype=DSLA_BF16, gate_dtype=DSLA_BF16, gamma=0.2 + 0.6 * (l % 7) / 6.0, scale=d ** -0.5, gate_mode=1, **k) for l in range(L)]
+    long, short = make(B, zero_init=True), make(B)
+    S = [[torch.zeros(B, H, d, d, device="cuda") for _ in range(2)] for _ in range(L)]
+    nws = dsla.dsla_prefill_workspace_bytes(long[0], T)
+    ws = torch.empty(max(nws, 256), dtype=torch.uint8, device="cuda")
+    prompt, token = (torch.randn(n, K, device="cuda", generator=gen).to(torch.bfloat16) for n in (B * T, B))
+    x, room, t, small = torch.empty_like(prompt), stack.room(B * T), torch.empty_like(token), stack.room(B)
+
+    def prefill():
+        x.copy_(prompt)
+        return stack.run(x, room, lambda l, *a: dsla.dsla_prefill(long[l], T, *a[:5], *S[l], a[5], ws if nws else None))
+
+    def step():
+        t.copy_(token)
+        return stack.run(t, small, lambda l, *a: dsla.dsla_decode(short[l], *a[:5], *S[l], a[5]))
+
+    def timed(run, reps):
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for _ in range(reps):
+            run()
+        torch.cuda.synchronize()
+        return (time.perf_counter() - t0) / reps * 1e6
+
+    finite = bool(torch.isfinite(prefill().float()).all())
+    prompt_us = timed(prefill, 3)
+    binding.profile_enable(True, 4096)
+    prefill()
+    shares = {n: round(1e3 * ms, 1) for n, (ms, count) in binding.profile_collect().items() if count}
+    binding.profile_enable(False, 0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    timed(step, 3)
+    eager = timed(step, decode)
+    timed(graph.replay, 3)
+    replayed = timed(graph.replay, decode)
+    finite = finite and bool(torch.isfinite(small["final"].float()).all())
+    print(json.dumps({"workload": f"{L} blocks of converted layers without MLPs, width {K}, {H} heads of {d}, {B} requests of {T} tokens, e4m3 projections, bf16 stream",
+                      "prefill_us": round(prompt_us, 1), "prefill_kernels_us": shares, "decode_eager_us": round(eager, 1), "decode_graph_us": round(replayed, 1),
+                      "weight_GBps": round(L * 7 * H * d * K / replayed / 1e3, 1), "finite": finite}))
+
+
 def multi_state(N: int, Hkv: int, B: int, T: int, H: int, d: int):
     """dsla_decode_multi at the batched-decode shape and dsla_prefill_multi at the long-prompt shape for N states and
     H_kv key/value heads; one JSON line."""
@@ -504,7 +615,8 @@ def main():
                     help="the whole hybrid configuration: --layers attention layers (default 32), the conversion logic "
                          "picks the DSLA ones, prompt and decode through every layer")
     ap.add_argument("--project", action="store_true", help="time the projection GEMM of one layer and the prefill behind it")
-    ap.add_argument("--K", type=int, default=4096, help="--project: model width")
+    ap.add_argument("--blocks", action="store_true", help="whole blocks of converted layers, projections in 8 bits, instead")
+    ap.add_argument("--K", type=int, default=4096, help="--project, --blocks: model width")
     ap.add_argument("--multi", type=int, default=0, metavar="N", help="time the N-state decode and prefill calls")
     ap.add_argument("--Hkv", type=int, default=0, help="--multi, --paged-attention: key/value heads (default: H)")
     ap.add_argument("--layers", type=int, default=None)
@@ -519,6 +631,8 @@ def main():
         a.decode = 64 if a.paged_attention else 128
     if a.project:
         return project(16384 if a.T == 8192 else a.T, a.K, a.H, a.d)
+    if a.blocks:
+        return blocks(a.layers or 16, a.B, a.T, a.K, a.H, a.d, a.decode)
     if a.multi:
         return multi_state(a.multi, a.Hkv or a.H, 1 if a.B == 8 else a.B, 16384 if a.T == 8192 else a.T, a.H, a.d)
     if a.hybrid:
