@@ -72,11 +72,12 @@ __device__ __forceinline__ float sum16(float x)
     return x + row_rotate<1>(x);
 }
 
-// Sum over the T threads of a workgroup, or over a wavefront (T = 64).
+// Sum over the T threads of a workgroup, over a wavefront (T = 64) or over 16 lanes.
 template <int T>
 __device__ __forceinline__ float sum_all(float x, float *s)
 {
     x = sum16(x);
+    if (T == 16) return x;
     x += __shfl_xor(x, 16);
     x += __shfl_xor(x, 32);
     if (T == 64) return x;
@@ -144,14 +145,16 @@ struct BorderArgs {
     float eps, residual_scale;
 };
 
-// T threads to a row, NV times 8 values to a thread: value 8 (T c + t) .. + 7 of the row for c < NV.  T = 64: a wavefront to a row, four rows to a workgroup.
+// T threads to a row, NV times 8 values to a thread: value 8 (T c + t) .. + 7 of the row for c < NV.  T = 64 and 16: a wavefront, or 16 lanes, to a
+// row, and 256 threads to a workgroup.
 template <int T, int NV, class TX, class TY>
-__global__ __launch_bounds__(T == 64 ? 256 : T) void residual_norm_kernel(BorderArgs a)
+__global__ __launch_bounds__(T < 256 ? 256 : T) void residual_norm_kernel(BorderArgs a)
 {
-    __shared__ float s_post[T / 64], s_pre[T / 64];
-    const int t = T == 64 ? threadIdx.x & 63 : threadIdx.x;
-    const long long row = T == 64 ? blockIdx.x * 4LL + (threadIdx.x >> 6) : blockIdx.x;
-    if (row >= a.rows) return;   // (wavefronts of T = 64 share nothing)
+    constexpr int ROWS = T < 256 ? 256 / T : 1;
+    __shared__ float s_post[(T + 63) / 64], s_pre[(T + 63) / 64];
+    const int t = threadIdx.x % T;
+    const long long row = static_cast<long long>(blockIdx.x) * ROWS + threadIdx.x / T;
+    if (row >= a.rows) return;   // (rows of one workgroup share nothing)
     const size_t base = static_cast<size_t>(row) * a.D;
     float r[NV][8], u[NV][8], g[NV][8];
 #pragma unroll
@@ -219,7 +222,8 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void residual_norm_kernel(Border
 template <int T, int NV>
 void launch_border(ProfileScope &ps, const BorderArgs &a, bool x32, bool y32, hipStream_t stream)
 {
-    const dim3 grid(static_cast<unsigned>(T == 64 ? (a.rows + 3) / 4 : a.rows)), block(T == 64 ? 256 : T);
+    constexpr int ROWS = T < 256 ? 256 / T : 1;
+    const dim3 grid(static_cast<unsigned>((a.rows + ROWS - 1) / ROWS)), block(T < 256 ? 256 : T);
     if (x32 && y32) DSLA_LAUNCH(ps, (residual_norm_kernel<T, NV, float, float>), grid, block, 0, stream, a);
     else if (x32) DSLA_LAUNCH(ps, (residual_norm_kernel<T, NV, float, bf16_t>), grid, block, 0, stream, a);
     else if (y32) DSLA_LAUNCH(ps, (residual_norm_kernel<T, NV, bf16_t, float>), grid, block, 0, stream, a);
@@ -360,7 +364,8 @@ hipError_t launch_residual_norm(const dsla_norm &n, int64_t rows, const void *x,
     BorderArgs a{x, y, gate, x_out, n.post_weight, n.pre_weight, result_of(h, h_scale, n.h_dtype, n.scale_type, n.D), rows, n.D, n.gate_act, n.eps, n.residual_scale};
     const bool x32 = n.x_dtype == DSLA_F32, y32 = n.y_dtype == DSLA_F32;
     ProfileScope ps(DSLA_KERNEL_RESIDUAL_NORM, stream);
-    if (n.D <= 512) launch_border<64, 1>(ps, a, x32, y32, stream);
+    if (n.D <= 128) launch_border<16, 1>(ps, a, x32, y32, stream);
+    else if (n.D <= 512) launch_border<64, 1>(ps, a, x32, y32, stream);
     else if (n.D <= 1024) launch_border<64, 2>(ps, a, x32, y32, stream);
     else if (n.D <= 2048) launch_border<256, 1>(ps, a, x32, y32, stream);
     else if (n.D <= 4096) launch_border<256, 2>(ps, a, x32, y32, stream);
