@@ -376,7 +376,7 @@ typedef enum { DSLA_ACT_NONE = 0, DSLA_ACT_SIGMOID = 1, DSLA_ACT_SILU = 2 } dsla
 
 /*
  * dsla_residual_norm - the border between two blocks in one pass.  Arithmetic is fp32; both results are rounded once, and h is
- * computed from x' before its rounding.  Norms are of features up to 10^18.
+ * computed from x' before its rounding.  Norms are of features up to 10^18.  Gates are to 2^-18 where no result is in fp32, else to 2^-21.
  *   rows     : tokens, >= 1
  *   x, x_out : [rows][D] of x_dtype; x_out NULL: x' is not kept
  *   y        : [rows][D] of y_dtype, or NULL: x' = x (then no gate, no post_weight)
@@ -402,7 +402,7 @@ DSLA_API dsla_status dsla_residual_norm(const dsla_norm *norm, int64_t rows, con
 
 /*
  * dsla_head_norm - norm and gate of the layer's read-out: every head of o by its own root mean square, times the weight, times
- * act(gate).  fp32 arithmetic, one rounding; features up to 10^18.
+ * act(gate).  fp32 arithmetic, one rounding; features up to 10^18, gates as above.
  *   o, gate : [rows][H][d] of io_dtype; gate NULL: no factor     out : [rows][H d] of out_dtype; may be o or gate where its elements are as large
  *   out_scale : scales of out where out_dtype is DSLA_E4M3 (a block holds one head of 128 or two of 64), else NULL
  */

@@ -89,19 +89,33 @@ __device__ __forceinline__ float sum_all(float x, float *s)
     return t;
 }
 
-// act(z), to 6 ulps: e^-|z| (a large gate does not overflow) as a power of two whose exponent carries the rounding of |z| log2 e along, and an inverse
-// with one step of Newton's.  The library's exponential and quotient are more instructions, which bound the kernels: 16384 rows of 32 heads 82 us
-// with them.
-__device__ __forceinline__ float activated(float z, int act)
+// act(z) by e^-|z|, so that a large gate does not overflow, as a power of two.  exact (results in fp32): to 6 ulps, the exponent carries the rounding of
+// |z| log2 e along, its whole part goes around the instruction, which has no results below 2^-126, and the inverse takes a step of Newton's.
+// Else: to 2^-18, by 16 issue slots instead of 26; the kernels issue vector instructions all the time.  24 is added to the exponent on the way, for the
+// numbers below 2^-126, and comes off again in the last factors.
+__device__ __forceinline__ float activated(float z, int act, bool exact)
 {
     if (act == DSLA_ACT_NONE) return z;
     constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f;
-    const float a = fabsf(z) > 200.f ? -200.f : -fabsf(z);   // (e^-200 is 0; NaN stays)
-    const float p = a * kLog2e, n = rintf(p), rest = fmaf(a, kLog2eRest, fmaf(a, kLog2e, -p));
-    const float t = ldexpf(__builtin_amdgcn_exp2f((p - n) + rest), static_cast<int>(n));   // (the instruction alone has no results below 2^-126)
-    const float d = 1.f + t, y = __builtin_amdgcn_rcpf(d), inverse = fmaf(y, fmaf(-d, y, 1.f), y);
-    const float top = z < 0.f ? t : 1.f;
-    return (act == DSLA_ACT_SIGMOID ? top : z * top) * inverse;
+    if (exact) {
+        const float a = fabsf(z) > 200.f ? -200.f : -fabsf(z);   // (e^-200 is 0; NaN stays)
+        const float p = a * kLog2e, n = rintf(p), rest = fmaf(a, kLog2eRest, fmaf(a, kLog2e, -p));
+        const float t = ldexpf(__builtin_amdgcn_exp2f((p - n) + rest), static_cast<int>(n));
+        const float d = 1.f + t, y = __builtin_amdgcn_rcpf(d), inverse = fmaf(y, fmaf(-d, y, 1.f), y);
+        const float top = z < 0.f ? t : 1.f;
+        return (act == DSLA_ACT_SIGMOID ? top : z * top) * inverse;
+    }
+    const float t = __builtin_amdgcn_exp2f(fmaf(-fabsf(z), kLog2e, 24.f));   // 2^24 e^-|z|
+    const float inverse = 0x1p-24f * __builtin_amdgcn_rcpf(fmaf(t, 0x1p-24f, 1.f)), top = (z < 0.f ? t : 0x1p24f) * inverse;
+    return act == DSLA_ACT_SIGMOID ? top : z * top;
+}
+
+// 1 / sqrt(v) to an ulp: the instruction and a step of Newton's; far from 1 (no square of a number, or an infinite one) the library's.
+__device__ __forceinline__ float inverse_root(float v)
+{
+    if (!(v > 0x1p-100f && v < 0x1p127f)) return 1.f / sqrtf(v);
+    const float y = __builtin_amdgcn_rsqf(v);
+    return fmaf(0.5f * y, fmaf(-v * y, y, 1.f), y);
 }
 
 // 8 values of a lane to where they go: as they are, or as e4m3 with the scale of the block that the lane's row of 16 holds (lanes without
@@ -143,6 +157,7 @@ struct BorderArgs {
     long long rows;
     int D, act;
     float eps, residual_scale;
+    bool exact;   // a result in fp32
 };
 
 // T threads to a row, NV times 8 values to a thread: value 8 (T c + t) .. + 7 of the row for c < NV.  T = 64 and 16: a wavefront, or 16 lanes, to a
@@ -175,7 +190,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_norm_kernel(Border
 #pragma unroll
             for (int i = 0; i < 8; ++i) q += u[c][i] * u[c][i];
         q = sum_all<T>(q, s_post);
-        const float inv = 1.f / sqrtf(q / a.D + a.eps);
+        const float inv = inverse_root(q / a.D + a.eps);
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
             const int col = 8 * (T * c + t);
@@ -193,7 +208,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_norm_kernel(Border
         if (col >= a.D) continue;
         if (a.y) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r[c][i] += factor * (a.gate ? u[c][i] * activated(g[c][i], a.act) : u[c][i]);
+            for (int i = 0; i < 8; ++i) r[c][i] += factor * (a.gate ? u[c][i] * activated(g[c][i], a.act, a.exact) : u[c][i]);
         }
         if (a.x_out) store8(static_cast<TX *>(a.x_out) + base + col, r[c]);
 #pragma unroll
@@ -203,7 +218,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_norm_kernel(Border
     float inv = 1.f;
     if (a.pre_weight) {
         q = sum_all<T>(q, s_pre);
-        inv = 1.f / sqrtf(q / a.D + a.eps);
+        inv = inverse_root(q / a.D + a.eps);
     }
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
@@ -282,13 +297,13 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a)
                 q += __shfl_xor(q, 2);
                 q += __shfl_xor(q, 1);
             }
-            const float inv = 1.f / sqrtf(q / (D ? D : 1) + a.eps);
+            const float inv = inverse_root(q * (1.f / (D ? D : 1)) + a.eps);
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[u][i] *= inv * w[i];
         }
         if (D && a.gate) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[u][i] *= activated(g[u][i], a.act);
+            for (int i = 0; i < 8; ++i) f[u][i] *= activated(g[u][i], a.act, a.o.dtype == DSLA_F32);
         }
         store_result(a.o, f[u], valid[u], static_cast<size_t>(row[u]) * a.cols + 128 * block[u] + 8 * l, row[u], block[u]);
     }
@@ -361,7 +376,8 @@ Result result_of(void *p, void *scale, int dtype, int scale_type, int cols) { re
 hipError_t launch_residual_norm(const dsla_norm &n, int64_t rows, const void *x, const void *y, const void *gate, void *x_out, void *h, void *h_scale,
                                 hipStream_t stream)
 {
-    BorderArgs a{x, y, gate, x_out, n.post_weight, n.pre_weight, result_of(h, h_scale, n.h_dtype, n.scale_type, n.D), rows, n.D, n.gate_act, n.eps, n.residual_scale};
+    BorderArgs a{x, y, gate, x_out, n.post_weight, n.pre_weight, result_of(h, h_scale, n.h_dtype, n.scale_type, n.D), rows, n.D, n.gate_act, n.eps, n.residual_scale,
+                 (x_out && n.x_dtype == DSLA_F32) || (h && n.h_dtype == DSLA_F32)};
     const bool x32 = n.x_dtype == DSLA_F32, y32 = n.y_dtype == DSLA_F32;
     ProfileScope ps(DSLA_KERNEL_RESIDUAL_NORM, stream);
     if (n.D <= 128) launch_border<16, 1>(ps, a, x32, y32, stream);

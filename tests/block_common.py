@@ -4,6 +4,9 @@ U = 2^-24 is half a step of fp32.  A sum of n squares in fp32, whatever its orde
 have one sign: a lane adds up to 32 of its own, 6 across the wavefront, up to 16 across wavefronts, so at most 57 U, half of that under the
 square root, and 4 more for the quotient, eps, the root and the inverse: 33 U on 1 / rms.  Two more products: 35 U on a norm's result.  A
 gate is at most 8 U off (the exponential 4, sum, quotient and product), so the part that is added to x at most 45 U, and the sum 1 U.
+
+Where no result is in fp32 a gate's exponential is that of an exponent rounded once, |z| log2 e - 24 below 128 by 64 U (half a step from 64 on), so its power
+is 64 U ln 2 = 45 U off, 2 U for the instruction, 2 U for the inverse's, 4 roundings: 53 U, and the part that is added 8 U less than 46 + 53.
 """
 import numpy as np
 import torch
@@ -15,6 +18,8 @@ HALF = {"bf16": 2.0 ** -8, "f32": U}
 TORCH = {"bf16": torch.bfloat16, "f32": torch.float32, "e4m3": torch.float8_e4m3fn}
 SCALES = {"f32": torch.float32, "e8m0": torch.float8_e8m0fnu}
 NORM, PART = 35 * U, 46 * U
+GATE = {"f32": 9 * U, "bf16": 54 * U, "e4m3": 54 * U}
+PART_OF = {True: PART, False: PART + 45 * U}   # is a result in fp32?
 
 
 def f64(t):

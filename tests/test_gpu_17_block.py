@@ -6,7 +6,7 @@ import torch
 
 import paper_2506_09316_amd as dsla
 from oracle import block as orc
-from tests.block_common import (HALF, NORM, PART, TORCH, U, assert_quantized, assert_scales_behind_untouched, assert_within, e4m3_room, f64, stored,
+from tests.block_common import (GATE, HALF, NORM, PART, PART_OF, TORCH, U, assert_quantized, assert_scales_behind_untouched, assert_within, e4m3_room, f64, stored,
                                 values)
 
 pytestmark = pytest.mark.gpu
@@ -79,7 +79,7 @@ def border(rows, D, x_dtype, y_dtype, out, *, post=True, pre=True, gate="none", 
     h, hs = e4m3_room(rows, D, scale) if out == "e4m3" else (torch.full((rows, D), float("nan"), device="cuda", dtype=TORCH[out]), None)
     dsla.dsla_residual_norm(norm, x, y, x_out, h, gate=g, h_scale=hs)
     r, want, part = orc.residual_norm(f64(x), f64(y), f64(g), kind, residual, f64(wpost), f64(wpre), EPS)
-    off_r = U * np.abs(r) + PART * np.abs(part)
+    off_r = U * np.abs(r) + PART_OF[(keep and x_dtype == "f32") or out == "f32"] * np.abs(part)
     off = off_r
     if wpre is not None:
         inv = 1 / np.sqrt((r * r).mean(-1, keepdims=True) + EPS) * np.abs(f64(wpre))
@@ -165,7 +165,7 @@ def test_heads(rows, H, d, gate, norm, dtype, out, scale):
     h, hs = e4m3_room(rows, H * d, scale) if out == "e4m3" else (torch.full((rows, H * d), float("nan"), device="cuda", dtype=TORCH[out]), None)
     dsla.dsla_head_norm(heads, o, h, gate=g, out_scale=hs)
     want = orc.head_norm(f64(o), f64(g), kind, f64(w), EPS).reshape(rows, H * d)
-    off = np.abs(want) * (NORM + 9 * U)
+    off = np.abs(want) * (NORM + GATE[out])
     if out == "e4m3":
         assert_quantized("heads", h, hs, want, off)
         assert_scales_behind_untouched(hs, H * d)
@@ -182,7 +182,7 @@ def test_heads_in_place_and_large_gates():
     with np.errstate(over="ignore"):
         want = orc.head_norm(f64(o), f64(g), "silu", np.ones(64), 1e-6).reshape(65, 384)
     # (below 2^-126 numbers have no 24 bits)
-    assert_within("heads", f64(out), want, np.abs(want) * (NORM + 9 * U + 300 * 2 * U + HALF["bf16"]) + 2.0 ** -126)
+    assert_within("heads", f64(out), want, np.abs(want) * (NORM + GATE["bf16"] + HALF["bf16"]) + 2.0 ** -126)
     a, b = o.clone(), g.clone()
     dsla.dsla_head_norm(heads, a, a, gate=g)
     dsla.dsla_head_norm(heads, o, b, gate=b)

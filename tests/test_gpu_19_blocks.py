@@ -10,7 +10,7 @@ import paper_2506_09316_amd as dsla
 import serving_step
 from oracle import block as orc
 from oracle import dsla_oracle
-from tests.block_common import HALF, NORM, PART, U, assert_quantized, assert_within, f64, stored
+from tests.block_common import GATE, HALF, NORM, PART, U, assert_quantized, assert_within, f64, stored
 
 pytestmark = pytest.mark.gpu
 
@@ -55,7 +55,7 @@ def test_a_block_step_by_step(B, T, K, H, d):
     assert np.abs(got - o).max() <= 2e-2 * np.abs(o).max()
     # norm and gate of its heads
     want = orc.head_norm(f64(room["o"]).reshape(-1, H, d), f64(room["outs"][5]).reshape(-1, H, d), "silu", f64(stack.heads[0]._keep[0]), EPS).reshape(-1, width)
-    assert_quantized("heads", *room["o8"], want, np.abs(want) * (NORM + 9 * U))
+    assert_quantized("heads", *room["o8"], want, np.abs(want) * (NORM + GATE["e4m3"]))
     # the output projection and the last border
     (want,), (size,) = orc.project(stored(room["o8"][0]), blocks(room["o8"][1], width), stored(stack.outside[0][0]), blocks(stack.outside[0][1], width), [K], None)
     assert_within("output projection", f64(room["y"]), want, HALF["bf16"] * np.abs(want) + 2.0 ** -11 * size)
