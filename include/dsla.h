@@ -435,7 +435,8 @@ DSLA_API dsla_status dsla_quantize(int64_t rows, int32_t cols, int32_t in_dtype,
  *   W       : the W_j [width_j][K] e4m3 one behind the other; W_scale: their scales for blocks of 128 x 128 one behind the other,
  *             ceil(width_j / 128) rows of DSLA_SCALE_PITCH(K) for each
  *   bias    : fp32, the bias_j [width_j] one behind the other, or NULL
- *   outs    : HOST array [n_out] of DEVICE pointers, [M][width_j] of out_dtype (DSLA_F32 or DSLA_BF16), written
+ *   outs    : HOST array [n_out] of DEVICE pointers, [M][width_j] of out_dtype (DSLA_F32 or DSLA_BF16), written; different from each other
+ *             and from the inputs
  * scale_type is that of x_scale and W_scale; the product of two fp32 scales should be a normal number.  fp32 accumulation, a block's
  * products scaled as a whole; no workspace.  outs in bf16: e4m3 matrix instructions, which add products in groups of eight
  * and keep of each what is above 2^-14 of its group's largest (random operands: 1.5e-5 of a result, against 2e-3 of its rounding); outs

@@ -530,6 +530,11 @@ dsla_status dsla_project_fp8(int64_t M, int32_t K, int32_t n_out, const int32_t 
         if (!outs[j]) return DSLA_ERR_NULL;
         if (!aligned16(outs[j])) return DSLA_ERR_SHAPE;
     }
+    for (int j = 0; j < n_out; ++j) {
+        if (outs[j] == x || outs[j] == W || outs[j] == x_scale || outs[j] == W_scale || outs[j] == bias) return DSLA_ERR_SHAPE;
+        for (int i = 0; i < j; ++i)
+            if (outs[i] == outs[j]) return DSLA_ERR_SHAPE;
+    }
     return hip_status(launch_project_fp8(M, K, n_out, widths, scale_type, x, x_scale, W, W_scale, bias, out_dtype, outs, static_cast<hipStream_t>(stream)));
 }
 

@@ -76,6 +76,7 @@ struct Few {
     static constexpr int SLOTS = ROOM / static_cast<int>(STAGE) == (ROOM - 2 * static_cast<int>(SLOT)) / static_cast<int>(STAGE) ? 2 : 1;
     static constexpr int FIT = (ROOM - SLOTS * static_cast<int>(SLOT)) / static_cast<int>(STAGE), MOST = 1 + 60 / LOADS;   // (the counter of loads in flight ends at 63)
     static constexpr int DEPTH = FIT < MOST ? FIT : MOST, MINE = DEPTH * STAGE + SLOTS * SLOT;
+    static_assert(SLOTS == 1 || DEPTH <= 4, "scales are asked for with a step DEPTH ahead, and have to be those of the next 4 steps then, or of these");
 };
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"

@@ -74,7 +74,8 @@ def test_quantize_refuses(lib, call, want):
     (dict(widths=[16] * 9), UNSUPPORTED), (dict(widths=[64, 0]), SHAPE), (dict(widths=[64, -16]), SHAPE), (dict(widths=[24]), UNSUPPORTED), (dict(widths=[1 << 24, 16]), SHAPE),
     (dict(widths=[(1 << 24) + 16]), SHAPE), (dict(M=2 ** 40, widths=[1 << 20]), SHAPE), (dict(scale_type=2), UNSUPPORTED), (dict(out=2), UNSUPPORTED), (dict(x=None), NULL), (dict(xs=None), NULL),
     (dict(w=None), NULL), (dict(ws=None), NULL), (dict(x=ctypes.c_void_p(8)), SHAPE), (dict(xs=ctypes.c_void_p(8)), SHAPE), (dict(w=ctypes.c_void_p(8)), SHAPE),
-    (dict(ws=ctypes.c_void_p(8)), SHAPE), (dict(bias=ctypes.c_void_p(8)), SHAPE), (dict(outs=[None, 0x1000]), NULL), (dict(outs=[0x1000, 0x1008]), SHAPE)])
+    (dict(ws=ctypes.c_void_p(8)), SHAPE), (dict(bias=ctypes.c_void_p(8)), SHAPE), (dict(outs=[None, 0x1000]), NULL), (dict(outs=[0x1000, 0x1008]), SHAPE), (dict(outs=[0x1000, 0x1000]), SHAPE),
+    (dict(outs=[0x1000, P[0].value]), SHAPE), (dict(outs=[P[2].value, 0x1000]), SHAPE)])
 def test_project_fp8_refuses(lib, call, want):
     a = {**dict(M=4, K=256, widths=[64, 128], scale_type=1, x=P[0], xs=P[1], w=P[2], ws=P[3], bias=None, out=1, outs=[0x100000, 0x200000]), **call}
     n = len(a["widths"])
