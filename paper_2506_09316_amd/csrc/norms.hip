@@ -1,7 +1,11 @@
 // What stands around the layer (include/dsla.h): the norms, gate and residual scale of a block's border, the norm and gate of the
 // read-out's heads, and values to e4m3 with block scales.  All of them are bound by memory: every value is read once, kept in
 // registers and written once, 8 values of a lane at a time; sums and largest magnitudes go through the lanes.  A block of 128
-// columns is 16 lanes of 8, one row of the cross-lane operations.
+// columns is 16 lanes of 8, one row of the cross-lane operations.  A copy with the same non-temporal hints reaches 6.1 to 6.3 TB/s:
+//   border, 16384 rows of 4096, bf16, both norms, gate, e4m3 out   110 us  5.5 TB/s (vector instructions issued 90 % of the time; two sums across
+//                                                                   the workgroup one after the other); without norm of y, gate and 8 bits 5.8; 512 wide 6.1
+//   heads, 16384 rows of 32 of 128, bf16, gate, e4m3 out            61.6 us  5.5 TB/s
+//   quantize, 20480 x 4096 bf16, blocks of 128 x 128                48.8 us  5.2 TB/s (256 bytes of a row at a time)
 #include "fp8_common.h"
 
 namespace dsla {
@@ -316,7 +320,7 @@ void launch_rows(ProfileScope &ps, const RowsArgs &a, bool f32, hipStream_t stre
     if (f32) DSLA_LAUNCH(ps, (rows_kernel<D, NB, float>), grid, dim3(256), 0, stream, a);
     else DSLA_LAUNCH(ps, (rows_kernel<D, NB, bf16_t>), grid, dim3(256), 0, stream, a);
 }
-// Several blocks to 16 lanes where every compute unit has eight workgroups of them.
+// Several blocks to 16 lanes where every compute unit has eight workgroups of them (heads, 16384 rows of 32: one 69 us, two 67.8, four 77.9).
 template <int D>
 void launch_rows_of(ProfileScope &ps, const RowsArgs &a, bool f32, hipStream_t stream)
 {

@@ -29,16 +29,20 @@ struct Operand<true> {
         for (int i = 0; i < 4; ++i) f[i] = wide(x[2 * i], x[2 * i + 1]);
     }
 };
-__device__ __forceinline__ f32x4 product(const Operand<false> &w, const Operand<false> &x)
+// With several fragments of W: neither form waits for the product in front of it.
+template <int NT>
+__device__ __forceinline__ void products(f32x4 (&t)[NT], const Operand<false> (&w)[NT], const Operand<false> &x)
 {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.f, x.f, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, kOne, 0, kOne);
-}
-__device__ __forceinline__ f32x4 product(const Operand<true> &w, const Operand<true> &x)
-{
-    f32x4 t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.f[i], x.f[i], t, 0, 0, 0);
-    return t;
+    for (int j = 0; j < NT; ++j) t[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[j].f, x.f, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, kOne, 0, kOne);
+}
+template <int NT>
+__device__ __forceinline__ void products(f32x4 (&t)[NT], const Operand<true> (&w)[NT], const Operand<true> &x)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) t[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[j].f[i], x.f[i], i ? t[j] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 }
 // What a block's products are multiplied by: two numbers, or 2^exponent (two bytes reach beyond fp32; 255 is NaN).
 template <bool E8M0>
@@ -65,9 +69,14 @@ struct Factor {
 // Few rows: the weights are the traffic
 // ---------------------------------------------------------------------------------------------------------------
 // A workgroup has 16 MT rows and 16 NT columns; its wavefronts take a stretch of K each and share nothing until their sums are added at the
-// end: no barrier stands between a wavefront's loads.  Its steps of 128 go through a ring of its own in LDS, filled by buffer loads that write
-// LDS directly, an instruction 8 rows of 128 bytes.  What counts is the lines that are asked for, and a scale alone would be one: they come
-// as 16 bytes of every row, 12 steps of E8M0 (from a multiple of four down) or four of fp32 at a time.
+// end: no barrier stands between a wavefront's loads, and every byte is written to LDS and read from there once.  Its steps of 128 go through a ring of its
+// own in LDS, filled by buffer loads that write LDS directly, an instruction 8 rows of 128 bytes.  What counts is the lines that are asked for, and a
+// scale alone would be one: they come as 16 bytes of every row, 12 steps of E8M0 (from a multiple of four down) or four of fp32 at a time (300 rows,
+// K = 11008, N = 4096: 25.2 us with a scale of every row in every step, 22.1 so).
+// One row, K = 4096, N = 20480: 15.0 us, 5.6 TB/s of weights.  64 rows 18.9 us.  300 rows, K = 11008, N = 4096: 24 us, 1.1 PFLOP/s; 1024 rows,
+// K = 4096, N = 4096: 23 us, 1.5 PFLOP/s.  Few rows are bound by the memory; tiles of nine and more blocks by what LDS holds of loads on their way, a step of each
+// wavefront, for as long as a line takes from memory (a step takes 2 us, its products 0.3).  Tried: four wavefronts with two steps each on their way
+// (the same within 2 %; fp32 scales 33 instead of 27 us), lines asked for ahead into the L2 (25 -> 36 us: each costs as much as the load itself).
 template <int MT, int NT, int NW>
 struct Few {
     static constexpr int LOADS = 2 * (NT + MT);                            // instructions of a step, scales apart
@@ -84,10 +93,6 @@ struct Few {
 __device__ __forceinline__ void load_to_lds16(uint32_t lds, uint32_t voff, u32x4 res, uint32_t soff)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(voff), "s"(res), "s"(soff) : "m0", "memory");
-}
-__device__ __forceinline__ void load_to_lds4(uint32_t lds, uint32_t voff, u32x4 res, uint32_t soff)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds), "v"(voff), "s"(res), "s"(soff) : "m0", "memory");
 }
 #pragma clang diagnostic pop
 __device__ __forceinline__ u32x4 resource_of(const void *p, size_t offset, uint32_t bytes)
@@ -233,10 +238,14 @@ __global__ __launch_bounds__(64 * NW) void project_fp8_rows_kernel(Fp8Args a, in
         for (int m = 0; m < MT; ++m) {
             Operand<EXACT> ox;
             ox.set(x[m]);
+            if constexpr (E8M0 && !EXACT) {
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                if constexpr (E8M0 && !EXACT) acc[m][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ow[j].f, ox.f, acc[m][j], 0, 0, 0, sw[j], 0, sx[m]);
-                else Factor<E8M0>(sx[m], sw[j]).add(acc[m][j], product(ow[j], ox));
+                for (int j = 0; j < NT; ++j) acc[m][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ow[j].f, ox.f, acc[m][j], 0, 0, 0, sw[j], 0, sx[m]);
+            } else {
+                f32x4 t[NT];
+                products(t, ow, ox);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) Factor<E8M0>(sx[m], sw[j]).add(acc[m][j], t[j]);
             }
         }
     }
@@ -297,9 +306,9 @@ bool launch_few_of(ProfileScope &ps, const Fp8Args &a, int N, int mt, int nt, bo
     PAIR(2, 1) PAIR(2, 2) PAIR(2, 3) PAIR(2, 4) PAIR(2, 5)
     PAIR(3, 2) PAIR(3, 3) PAIR(3, 4) PAIR(3, 5)
     PAIR(4, 2) PAIR(4, 3) PAIR(4, 4) PAIR(4, 5) PAIR(4, 6) PAIR(4, 8)
-    PAIR(5, 4) PAIR(5, 5) PAIR(6, 4) PAIR(6, 5) PAIR(6, 6) PAIR(8, 4) PAIR(8, 5) PAIR(8, 6)
+    PAIR(5, 4) PAIR(5, 5) PAIR(6, 4) PAIR(6, 5) PAIR(6, 6) PAIR(8, 4) PAIR(8, 5)
     if constexpr (!EXACT) {   // (512 registers do not hold the operands in bf16 beside these sums)
-        PAIR(5, 8) PAIR(6, 8) PAIR(8, 8)
+        PAIR(8, 6) PAIR(5, 8) PAIR(6, 8) PAIR(8, 8)
     }
 #undef PAIR
     return false;
