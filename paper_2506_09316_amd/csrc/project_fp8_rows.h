@@ -76,7 +76,8 @@ struct Factor {
 // One row, K = 4096, N = 20480: 15.0 us, 5.6 TB/s of weights.  64 rows 18.9 us.  300 rows, K = 11008, N = 4096: 24 us, 1.1 PFLOP/s; 1024 rows,
 // K = 4096, N = 4096: 23 us, 1.5 PFLOP/s.  Few rows are bound by the memory; tiles of nine and more blocks by what LDS holds of loads on their way, a step of each
 // wavefront, for as long as a line takes from memory (a step takes 2 us, its products 0.3).  Tried: four wavefronts with two steps each on their way
-// (the same within 2 %; fp32 scales 33 instead of 27 us), lines asked for ahead into the L2 (25 -> 36 us: each costs as much as the load itself).
+// (the same within 2 %; fp32 scales 33 instead of 27 us), lines asked for ahead into the L2 (25 -> 36 us: each costs as much as the load itself),
+// the workgroups that share rows in different places of their stretches (24 -> 43 us: together each line comes once).
 template <int MT, int NT, int NW>
 struct Few {
     static constexpr int LOADS = 2 * (NT + MT);                            // instructions of a step, scales apart
