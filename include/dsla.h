@@ -363,7 +363,8 @@ DSLA_API dsla_status dsla_project(int64_t M, int32_t K, int32_t n_out, int32_t w
  *
  * Block scales.  An e4m3 tensor [rows][cols] stands for q * scale, one scale for each block of 128 columns of a row (activations), or of
  * 128 x 128 (weights); the last blocks may be smaller.  Scales are [rows][P], or [ceil(rows / 128)][P], P = DSLA_SCALE_PITCH(cols): a
- * row's ceil(cols / 128) scales, rounded up to a multiple of four; what lies behind them is neither read for a result nor written.
+ * row's ceil(cols / 128) scales, rounded up to a multiple of four; what lies behind them is neither read for a result nor written.  Pointers
+ * to scales are aligned to 4 bytes, so that those of stacked weights can be written where they lie.
  *   DSLA_SCALE_F32  : fp32, amax / 448
  *   DSLA_SCALE_E8M0 : one byte b for 2^(b - 127), 255 = NaN; the smallest power of two that keeps amax within 448.  The matrix
  *                     instructions multiply by it themselves
@@ -376,7 +377,7 @@ typedef enum { DSLA_ACT_NONE = 0, DSLA_ACT_SIGMOID = 1, DSLA_ACT_SILU = 2 } dsla
 
 /*
  * dsla_residual_norm - the border between two blocks in one pass.  Arithmetic is fp32; both results are rounded once, and h is
- * computed from x' before its rounding.  Norms are of features up to 10^18.  Gates are to 2^-18 where no result is in fp32, else to 2^-21.
+ * computed from x' before its rounding.  Norms are of features up to 10^17.  Gates are to 2^-18 where no result is in fp32, else to 2^-21.
  *   rows     : tokens, >= 1
  *   x, x_out : [rows][D] of x_dtype; x_out NULL: x' is not kept
  *   y        : [rows][D] of y_dtype, or NULL: x' = x (then no gate, no post_weight)

@@ -18,6 +18,7 @@ dsla_status hip_status(hipError_t e)
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 dsla_status check_desc(const dsla_desc *d)
 {
@@ -444,7 +445,7 @@ dsla_status check_result(int32_t dtype, int32_t scale_type, const void *scale, i
     if (dtype == DSLA_E4M3) {
         if (!scale_type_ok(scale_type)) return DSLA_ERR_UNSUPPORTED;
         if (!scale) return DSLA_ERR_NULL;
-        if (!aligned16(scale)) return DSLA_ERR_SHAPE;
+        if (!aligned4(scale)) return DSLA_ERR_SHAPE;
     } else if (scale) {
         return DSLA_ERR_SHAPE;
     }
@@ -505,7 +506,7 @@ dsla_status dsla_quantize(int64_t rows, int32_t cols, int32_t in_dtype, int32_t 
     if (cols % 16 != 0 || cols > (1 << 21) || !io_type(in_dtype) || (block_rows != 1 && block_rows != 128) || !scale_type_ok(scale_type)) return DSLA_ERR_UNSUPPORTED;
     if (rows > 0x7fffffffLL / ((cols + 127) / 128)) return DSLA_ERR_SHAPE;
     if (!x || !q || !scale) return DSLA_ERR_NULL;
-    if (!aligned16(x) || !aligned16(q) || !aligned16(scale)) return DSLA_ERR_SHAPE;
+    if (!aligned16(x) || !aligned16(q) || !aligned4(scale)) return DSLA_ERR_SHAPE;
     if (q == x || scale == x || scale == q) return DSLA_ERR_SHAPE;
     return hip_status(launch_quantize(rows, cols, in_dtype, block_rows, scale_type, x, q, scale, static_cast<hipStream_t>(stream)));
 }
@@ -525,7 +526,7 @@ dsla_status dsla_project_fp8(int64_t M, int32_t K, int32_t n_out, const int32_t 
     }
     if (columns > (1 << 24) || (M + 63) / 64 * 2 * blocks > 0x7ffffff0LL) return DSLA_ERR_SHAPE;
     if (!x || !x_scale || !W || !W_scale) return DSLA_ERR_NULL;
-    if (!aligned16(x) || !aligned16(x_scale) || !aligned16(W) || !aligned16(W_scale) || !aligned16(bias)) return DSLA_ERR_SHAPE;
+    if (!aligned16(x) || !aligned4(x_scale) || !aligned16(W) || !aligned4(W_scale) || !aligned16(bias)) return DSLA_ERR_SHAPE;
     for (int j = 0; j < n_out; ++j) {
         if (!outs[j]) return DSLA_ERR_NULL;
         if (!aligned16(outs[j])) return DSLA_ERR_SHAPE;
@@ -551,8 +552,6 @@ dsla_status dsla_attention_prefill(int32_t B, int32_t H, int32_t d, int64_t T, i
 }
 
 namespace {
-bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-
 dsla_status check_cache(const dsla_cache *c)
 {
     if (!c) return DSLA_ERR_NULL;

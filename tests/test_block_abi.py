@@ -35,7 +35,7 @@ def norm_of(**k):
     ({}, dict(h_scale=P[5]), SHAPE), ({}, dict(h=None, h_scale=P[5]), SHAPE), (dict(h_dtype=2), {}, NULL), (dict(h_dtype=2, scale_type=2), dict(h_scale=P[5]), UNSUPPORTED),
     ({}, dict(x=ctypes.c_void_p(0x1008)), SHAPE), ({}, dict(y=ctypes.c_void_p(0x1008)), SHAPE), ({}, dict(gate=ctypes.c_void_p(0x1004)), SHAPE),
     ({}, dict(x_out=ctypes.c_void_p(0x1002)), SHAPE), ({}, dict(h=ctypes.c_void_p(0x1002)), SHAPE), (dict(post_weight=0x9004), {}, SHAPE),
-    (dict(pre_weight=0x9004), {}, SHAPE), (dict(h_dtype=2), dict(h_scale=ctypes.c_void_p(0x1008)), SHAPE),
+    (dict(pre_weight=0x9004), {}, SHAPE), (dict(h_dtype=2), dict(h_scale=ctypes.c_void_p(0x1002)), SHAPE),
     ({}, dict(h=P[2]), SHAPE), (dict(h_dtype=2), dict(h=P[0], h_scale=P[5]), SHAPE), (dict(h_dtype=0), dict(h=P[1]), SHAPE), (dict(x_dtype=0), dict(x_out=P[1]), SHAPE),
     (dict(h_dtype=2), dict(h_scale=P[0]), SHAPE), (dict(h_dtype=2), dict(h_scale=P[4]), SHAPE)])
 def test_residual_norm_refuses(lib, change, call, want):
@@ -63,7 +63,7 @@ def test_structures_are_required(lib):
 @pytest.mark.parametrize("call, want", [
     (dict(rows=0), SHAPE), (dict(cols=0), SHAPE), (dict(cols=24), UNSUPPORTED), (dict(cols=(1 << 21) + 16), UNSUPPORTED), (dict(dtype=2), UNSUPPORTED), (dict(block_rows=64), UNSUPPORTED),
     (dict(scale_type=2), UNSUPPORTED), (dict(rows=2 ** 31), SHAPE), (dict(x=None), NULL), (dict(q=None), NULL), (dict(scale=None), NULL), (dict(x=ctypes.c_void_p(8)), SHAPE),
-    (dict(q=ctypes.c_void_p(8)), SHAPE), (dict(scale=ctypes.c_void_p(8)), SHAPE), (dict(q=P[0]), SHAPE), (dict(scale=P[0]), SHAPE), (dict(scale=P[1]), SHAPE)])
+    (dict(q=ctypes.c_void_p(8)), SHAPE), (dict(scale=ctypes.c_void_p(6)), SHAPE), (dict(q=P[0]), SHAPE), (dict(scale=P[0]), SHAPE), (dict(scale=P[1]), SHAPE)])
 def test_quantize_refuses(lib, call, want):
     a = {**dict(rows=4, cols=256, dtype=1, block_rows=1, scale_type=1, x=P[0], q=P[1], scale=P[2]), **call}
     assert lib.dsla_quantize(a["rows"], a["cols"], a["dtype"], a["block_rows"], a["scale_type"], a["x"], a["q"], a["scale"], None) == want
@@ -73,8 +73,8 @@ def test_quantize_refuses(lib, call, want):
     (dict(M=0), SHAPE), (dict(M=-5), SHAPE), (dict(K=0), SHAPE), (dict(K=72), UNSUPPORTED), (dict(K=(1 << 21) + 16), UNSUPPORTED), (dict(widths=[]), SHAPE),
     (dict(widths=[16] * 9), UNSUPPORTED), (dict(widths=[64, 0]), SHAPE), (dict(widths=[64, -16]), SHAPE), (dict(widths=[24]), UNSUPPORTED), (dict(widths=[1 << 24, 16]), SHAPE),
     (dict(widths=[(1 << 24) + 16]), SHAPE), (dict(M=2 ** 40, widths=[1 << 20]), SHAPE), (dict(scale_type=2), UNSUPPORTED), (dict(out=2), UNSUPPORTED), (dict(x=None), NULL), (dict(xs=None), NULL),
-    (dict(w=None), NULL), (dict(ws=None), NULL), (dict(x=ctypes.c_void_p(8)), SHAPE), (dict(xs=ctypes.c_void_p(8)), SHAPE), (dict(w=ctypes.c_void_p(8)), SHAPE),
-    (dict(ws=ctypes.c_void_p(8)), SHAPE), (dict(bias=ctypes.c_void_p(8)), SHAPE), (dict(outs=[None, 0x1000]), NULL), (dict(outs=[0x1000, 0x1008]), SHAPE), (dict(outs=[0x1000, 0x1000]), SHAPE),
+    (dict(w=None), NULL), (dict(ws=None), NULL), (dict(x=ctypes.c_void_p(8)), SHAPE), (dict(xs=ctypes.c_void_p(6)), SHAPE), (dict(w=ctypes.c_void_p(8)), SHAPE),
+    (dict(ws=ctypes.c_void_p(6)), SHAPE), (dict(bias=ctypes.c_void_p(8)), SHAPE), (dict(outs=[None, 0x1000]), NULL), (dict(outs=[0x1000, 0x1008]), SHAPE), (dict(outs=[0x1000, 0x1000]), SHAPE),
     (dict(outs=[0x1000, P[0].value]), SHAPE), (dict(outs=[P[2].value, 0x1000]), SHAPE)])
 def test_project_fp8_refuses(lib, call, want):
     a = {**dict(M=4, K=256, widths=[64, 128], scale_type=1, x=P[0], xs=P[1], w=P[2], ws=P[3], bias=None, out=1, outs=[0x100000, 0x200000]), **call}
