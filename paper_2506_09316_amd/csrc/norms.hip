@@ -3,7 +3,7 @@
 // registers and written once, 8 values of a lane at a time; sums and largest magnitudes go through the lanes.  A block of 128
 // columns is 16 lanes of 8, one row of the cross-lane operations.  A copy with the same non-temporal hints reaches 6.1 to 6.3 TB/s:
 //   border, 16384 rows of 4096, bf16, both norms, gate, e4m3 out   110 us  5.5 TB/s (vector instructions issued 90 % of the time; two sums across
-//                                                                   the workgroup one after the other); without norm of y, gate and 8 bits 5.8; 512 wide 6.1
+//                                                                   the workgroup one after the other); without norm of y, gate and 8 bits 6.1
 //   heads, 16384 rows of 32 of 128, bf16, gate, e4m3 out            61.6 us  5.5 TB/s
 //   quantize, 20480 x 4096 bf16, blocks of 128 x 128                48.8 us  5.2 TB/s (256 bytes of a row at a time)
 #include "fp8_common.h"
@@ -384,12 +384,15 @@ hipError_t launch_residual_norm(const dsla_norm &n, int64_t rows, const void *x,
                  (x_out && n.x_dtype == DSLA_F32) || (h && n.h_dtype == DSLA_F32)};
     const bool x32 = n.x_dtype == DSLA_F32, y32 = n.y_dtype == DSLA_F32;
     ProfileScope ps(DSLA_KERNEL_RESIDUAL_NORM, stream);
+    // 8 values a lane from 1024 columns on: more rows' loads are in flight at once than with more of them (without norm of y, gate and 8 bits, 8192 rows
+    // of 4096: 256 lanes of 16 values 45.4 us, 512 of 8 44.0, 128 of 32 slower than both; 4096 of 8192: 256 of 32 48.4, 1024 of 8 46.1; 256 of 4096: 4.08, 3.85.
+    // With everything of it, 16384 of 4096: 109.7, 110.5).
     if (n.D <= 128) launch_border<16, 1>(ps, a, x32, y32, stream);
     else if (n.D <= 512) launch_border<64, 1>(ps, a, x32, y32, stream);
     else if (n.D <= 1024) launch_border<64, 2>(ps, a, x32, y32, stream);
     else if (n.D <= 2048) launch_border<256, 1>(ps, a, x32, y32, stream);
-    else if (n.D <= 4096) launch_border<256, 2>(ps, a, x32, y32, stream);
-    else if (n.D <= 8192) launch_border<256, 4>(ps, a, x32, y32, stream);
+    else if (n.D <= 4096) launch_border<512, 1>(ps, a, x32, y32, stream);
+    else if (n.D <= 8192) launch_border<1024, 1>(ps, a, x32, y32, stream);
     else if (n.D <= 16384) launch_border<1024, 2>(ps, a, x32, y32, stream);
     else launch_border<1024, 4>(ps, a, x32, y32, stream);
     return hipGetLastError();
