@@ -524,7 +524,7 @@ dsla_status dsla_project_fp8(int64_t M, int32_t K, int32_t n_out, const int32_t 
         columns += widths[j];
         blocks += (widths[j] + 127) / 128;
     }
-    if (columns > (1 << 24) || (M + 63) / 64 * 2 * blocks > 0x7ffffff0LL) return DSLA_ERR_SHAPE;
+    if (columns > (1 << 24) || M > 0x7ffffff0LL * 32 || (M + 63) / 64 * 2 * blocks > 0x7ffffff0LL) return DSLA_ERR_SHAPE;
     if (!x || !x_scale || !W || !W_scale) return DSLA_ERR_NULL;
     if (!aligned16(x) || !aligned4(x_scale) || !aligned16(W) || !aligned4(W_scale) || !aligned16(bias)) return DSLA_ERR_SHAPE;
     for (int j = 0; j < n_out; ++j) {

@@ -70,7 +70,7 @@ def test_quantize_refuses(lib, call, want):
 
 
 @pytest.mark.parametrize("call, want", [
-    (dict(M=0), SHAPE), (dict(M=-5), SHAPE), (dict(K=0), SHAPE), (dict(K=72), UNSUPPORTED), (dict(K=(1 << 21) + 16), UNSUPPORTED), (dict(widths=[]), SHAPE),
+    (dict(M=0), SHAPE), (dict(M=-5), SHAPE), (dict(M=2 ** 63 - 1), SHAPE), (dict(M=2 ** 58, widths=[1 << 12]), SHAPE), (dict(K=0), SHAPE), (dict(K=72), UNSUPPORTED), (dict(K=(1 << 21) + 16), UNSUPPORTED), (dict(widths=[]), SHAPE),
     (dict(widths=[16] * 9), UNSUPPORTED), (dict(widths=[64, 0]), SHAPE), (dict(widths=[64, -16]), SHAPE), (dict(widths=[24]), UNSUPPORTED), (dict(widths=[1 << 24, 16]), SHAPE),
     (dict(widths=[(1 << 24) + 16]), SHAPE), (dict(M=2 ** 40, widths=[1 << 20]), SHAPE), (dict(scale_type=2), UNSUPPORTED), (dict(out=2), UNSUPPORTED), (dict(x=None), NULL), (dict(xs=None), NULL),
     (dict(w=None), NULL), (dict(ws=None), NULL), (dict(x=ctypes.c_void_p(8)), SHAPE), (dict(xs=ctypes.c_void_p(6)), SHAPE), (dict(w=ctypes.c_void_p(8)), SHAPE),
