@@ -378,7 +378,7 @@ typedef enum { DSLA_ACT_NONE = 0, DSLA_ACT_SIGMOID = 1, DSLA_ACT_SILU = 2 } dsla
 /*
  * dsla_residual_norm - the border between two blocks in one pass.  Arithmetic is fp32; both results are rounded once, and h is
  * computed from x' before its rounding.  Norms are of features up to 10^17.  Gates are to 2^-18 where no result is in fp32, else to 2^-21.
- *   rows     : tokens, >= 1
+ *   rows     : tokens, >= 1; rows * ceil(D / 128) below 2^31 (else DSLA_ERR_SHAPE)
  *   x, x_out : [rows][D] of x_dtype; x_out NULL: x' is not kept
  *   y        : [rows][D] of y_dtype, or NULL: x' = x (then no gate, no post_weight)
  *   gate     : [rows][D] of y_dtype, or NULL: no factor
@@ -406,6 +406,7 @@ DSLA_API dsla_status dsla_residual_norm(const dsla_norm *norm, int64_t rows, con
  * act(gate).  fp32 arithmetic, one rounding; features up to 10^18, gates as above.
  *   o, gate : [rows][H][d] of io_dtype; gate NULL: no factor     out : [rows][H d] of out_dtype; may be o or gate where its elements are as large
  *   out_scale : scales of out where out_dtype is DSLA_E4M3 (a block holds one head of 128 or two of 64), else NULL
+ *   rows : >= 1; rows * ceil(H d / 128) below 2^31 (else DSLA_ERR_SHAPE)
  */
 typedef struct {
     int32_t H, d;          /* H up to 2^16, d in {64, 128}                                          */
@@ -421,7 +422,8 @@ DSLA_API dsla_status dsla_head_norm(const dsla_heads *heads, int64_t rows, const
 
 /*
  * dsla_quantize - x [rows][cols] of in_dtype (DSLA_F32 or DSLA_BF16) to e4m3 with block scales: block_rows = 1 for activations, 128 for
- * weights (each output of a stacked weight by a call of its own where its rows are no multiple of 128).  cols: a multiple of 16, up to 2^21.
+ * weights (each output of a stacked weight by a call of its own where its rows are no multiple of 128).  cols: a multiple of 16, up to 2^21;
+ * rows * ceil(cols / 128) below 2^31 (else DSLA_ERR_SHAPE).
  */
 DSLA_API dsla_status dsla_quantize(int64_t rows, int32_t cols, int32_t in_dtype, int32_t block_rows, int32_t scale_type, const void *x,
                                    void *q, void *scale, void *stream);

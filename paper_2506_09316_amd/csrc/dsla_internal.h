@@ -60,6 +60,16 @@ struct ProfileScope {
         else hipLaunchKernelGGL(kernel, grid, block, shmem, stream, __VA_ARGS__);                                    \
     } while (0)
 
+// A launch has fewer than 2^32 work-items in a dimension.  What needs more workgroups than that goes in rows of 2^16 of them, the last of which is
+// filled up with workgroups that find nothing to do; workgroup_index() counts them the same way in both cases.
+constexpr unsigned kGridRow = 1u << 16;
+inline dim3 grid_of(long long workgroups, unsigned threads)
+{
+    if (workgroups * threads < 1LL << 32) return dim3(static_cast<unsigned>(workgroups));
+    return dim3(kGridRow, static_cast<unsigned>((workgroups + kGridRow - 1) / kGridRow));
+}
+__device__ __forceinline__ uint32_t workgroup_index() { return blockIdx.y * kGridRow + blockIdx.x; }
+
 // ---- launchers (one per kernel family; each returns the launch error) ------------------------
 hipError_t launch_state_init(float *S1, float *S2, size_t elems_per_state, hipStream_t stream);
 

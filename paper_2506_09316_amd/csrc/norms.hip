@@ -172,7 +172,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_norm_kernel(Border
     constexpr int ROWS = T < 256 ? 256 / T : 1;
     __shared__ float s_post[(T + 63) / 64], s_pre[(T + 63) / 64];
     const int t = threadIdx.x % T;
-    const long long row = static_cast<long long>(blockIdx.x) * ROWS + threadIdx.x / T;
+    const long long row = static_cast<long long>(workgroup_index()) * ROWS + threadIdx.x / T;
     if (row >= a.rows) return;   // (rows of one workgroup share nothing)
     const size_t base = static_cast<size_t>(row) * a.D;
     float r[NV][8], u[NV][8], g[NV][8];
@@ -242,7 +242,7 @@ template <int T, int NV>
 void launch_border(ProfileScope &ps, const BorderArgs &a, bool x32, bool y32, hipStream_t stream)
 {
     constexpr int ROWS = T < 256 ? 256 / T : 1;
-    const dim3 grid(static_cast<unsigned>((a.rows + ROWS - 1) / ROWS)), block(T < 256 ? 256 : T);
+    const dim3 block(T < 256 ? 256 : T), grid = grid_of((a.rows + ROWS - 1) / ROWS, block.x);
     if (x32 && y32) DSLA_LAUNCH(ps, (residual_norm_kernel<T, NV, float, float>), grid, block, 0, stream, a);
     else if (x32) DSLA_LAUNCH(ps, (residual_norm_kernel<T, NV, float, bf16_t>), grid, block, 0, stream, a);
     else if (y32) DSLA_LAUNCH(ps, (residual_norm_kernel<T, NV, bf16_t, float>), grid, block, 0, stream, a);
@@ -274,7 +274,7 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a)
     bool valid[NB];
 #pragma unroll
     for (int u = 0; u < NB; ++u) {
-        const uint32_t n = (blockIdx.x * NB + u) * 16u + (threadIdx.x >> 4);
+        const uint32_t n = (workgroup_index() * NB + u) * 16u + (threadIdx.x >> 4);
         const bool there = n < a.blocks;
         row[u] = a.by_row.quotient(there ? n : 0u);
         block[u] = there ? static_cast<int>(n - row[u] * a.per_row) : 0;
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a)
 template <int D, int NB>
 void launch_rows(ProfileScope &ps, const RowsArgs &a, bool f32, hipStream_t stream)
 {
-    const dim3 grid((a.blocks + 16u * NB - 1) / (16u * NB));
+    const dim3 grid = grid_of((a.blocks + 16u * NB - 1) / (16u * NB), 256);
     if (f32) DSLA_LAUNCH(ps, (rows_kernel<D, NB, float>), grid, dim3(256), 0, stream, a);
     else DSLA_LAUNCH(ps, (rows_kernel<D, NB, bf16_t>), grid, dim3(256), 0, stream, a);
 }
@@ -345,12 +345,13 @@ __global__ __launch_bounds__(256) void square_kernel(SquareArgs a)
 {
     __shared__ float s_max[16];
     const int l = threadIdx.x & 15, r0 = threadIdx.x >> 4;
-    const long long brow = blockIdx.x / a.per_row;
-    const int bcol = static_cast<int>(blockIdx.x - brow * a.per_row), col = 128 * bcol + 8 * l;
+    const uint32_t n = workgroup_index(), brow = n / a.per_row;
+    if (128LL * brow >= a.rows) return;
+    const int bcol = static_cast<int>(n - brow * a.per_row), col = 128 * bcol + 8 * l;
     float f[8][8], m = 0.f;
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
-        const long long row = 128 * brow + 16 * c + r0;
+        const long long row = 128LL * brow + 16 * c + r0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[c][i] = 0.f;
         if (row < a.rows && col < a.cols) load8(static_cast<const TIO *>(a.x) + static_cast<size_t>(row) * a.cols + col, f[c]);
@@ -363,7 +364,7 @@ __global__ __launch_bounds__(256) void square_kernel(SquareArgs a)
     const BlockScale<E8M0> s(max16(s_max[l]));
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
-        const long long row = 128 * brow + 16 * c + r0;
+        const long long row = 128LL * brow + 16 * c + r0;
         if (row >= a.rows || col >= a.cols) continue;
         float v[8];
 #pragma unroll
@@ -417,7 +418,7 @@ hipError_t launch_quantize(int64_t rows, int cols, int in_dtype, int block_rows,
         launch_rows_of<0>(ps, a, in_dtype == DSLA_F32, stream);
     } else {
         const SquareArgs a{x, static_cast<uint8_t *>(q), scale, rows, cols, scale_pitch(cols), per_row};
-        const dim3 grid(static_cast<unsigned>((rows + 127) / 128 * per_row));
+        const dim3 grid = grid_of((rows + 127) / 128 * per_row, 256);
         if (in_dtype == DSLA_F32 && scale_type == DSLA_SCALE_E8M0) DSLA_LAUNCH(ps, (square_kernel<float, true>), grid, dim3(256), 0, stream, a);
         else if (in_dtype == DSLA_F32) DSLA_LAUNCH(ps, (square_kernel<float, false>), grid, dim3(256), 0, stream, a);
         else if (scale_type == DSLA_SCALE_E8M0) DSLA_LAUNCH(ps, (square_kernel<bf16_t, true>), grid, dim3(256), 0, stream, a);

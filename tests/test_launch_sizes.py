@@ -1,0 +1,42 @@
+"""The largest calls around a layer are launches that the runtime takes: fewer than 2^32 work-items in a dimension.  (Launches stubbed out.)"""
+from tests.launch_sizes import run_checked
+
+NORMS = r"""
+def covers(call, needed):
+    '''One launch, of at least the workgroups that are needed and of hardly more.'''
+    launched(call)
+    got = stub.launch_stub_workgroups()
+    assert needed <= got <= needed + (0 if got == stub.launch_stub_row() else 65535), (needed, got)
+
+lanes = lambda D: 16 if D <= 128 else 64 if D <= 1024 else 256 if D <= 2048 else 512 if D <= 4096 else 1024
+for D in (16, 128, 144, 512, 1024, 1040, 2048, 4096, 8192, 16384, 32768):
+    most, at_once = 0x7fffffff // -(-D // 128), max(1, 256 // lanes(D))
+    border = (1 << 32) // lanes(D)   # rows from which a dimension holds no launch
+    for rows in {r for r in (1, 1 << 20, border - 1, border, border + 1, most - 1, most) if r <= most}:
+        for x in (0, 1):
+            for h in (0, 1, 2):
+                covers(residual_norm(rows, D, x, 1, h), -(-rows // at_once))
+    assert residual_norm(most + 1, D) == ERR_SHAPE
+for H, d in ((1, 64), (1, 128), (5, 64), (32, 128), (65536, 64), (65536, 128)):
+    per = -(-H * d // 128)
+    most = 0x7fffffff // per
+    for rows in {r for r in (1, 4097, (1 << 29) // per, (1 << 29) // per + 1, most) if 1 <= r <= most}:
+        for out in (0, 1, 2):
+            blocks = rows * per
+            covers(head_norm(rows, H, d, 1, out), -(-blocks // (32 if blocks >= 65536 else 16)))
+    assert head_norm(most + 1, H, d) == ERR_SHAPE
+for cols in (16, 128, 4112, 1 << 21):
+    per = -(-cols // 128)
+    most = 0x7fffffff // per
+    for rows in {r for r in (1, (1 << 30) // per, (1 << 30) // per + 1, most - 127, most) if 1 <= r <= most}:
+        for io in (0, 1):
+            for scale in (0, 1):
+                blocks = rows * per
+                covers(quantize(rows, cols, 1, io, scale), -(-blocks // (64 if blocks >= 131072 else 16)))
+                covers(quantize(rows, cols, 128, io, scale), -(-rows // 128) * per)
+    assert quantize(most + 1, cols, 1) == ERR_SHAPE
+"""
+
+
+def test_norms_and_quantization(tmp_path):
+    run_checked(tmp_path, NORMS)
