@@ -432,7 +432,8 @@ DSLA_API dsla_status dsla_quantize(int64_t rows, int32_t cols, int32_t in_dtype,
  * dsla_project_fp8 - dsla_project with e4m3 operands and block scales; the outputs may differ in width (fewer key/value heads, an
  * output projection):
  *     out_j[m][c] = sum_k x[m][k] W_j[c][k] (+ bias_j[c]),     j = 0 .. n_out - 1
- *   M       : rows of x, >= 1              K : a multiple of 16, up to 2^21
+ *   M       : rows of x, >= 1; ceil(M / 64) * (the sum of all ceil(width_j / 128)) up to 2^30 - 8 (else DSLA_ERR_SHAPE)
+ *   K       : a multiple of 16, up to 2^21
  *   widths  : HOST array [n_out], columns of every output, multiples of 16, up to 2^24 in all; n_out = 1 .. DSLA_MAX_PROJECTIONS
  *   x       : [M][K] e4m3 with scales for 128 columns of a row
  *   W       : the W_j [width_j][K] e4m3 one behind the other; W_scale: their scales for blocks of 128 x 128 one behind the other,

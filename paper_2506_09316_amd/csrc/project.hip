@@ -123,8 +123,8 @@ __global__ __launch_bounds__(256, Q == 4 ? 1 : 2) void project_tile_kernel(const
     __shared__ __attribute__((aligned(1024))) char st3[STAGEB];
     int tm, tn;
     if (Q > 1 || group > 0) {
-        if (!tile_of(tiles_m, tiles_n, group, per_xcd, tm, tn)) return;
-    } else if (!tile_of(tiles_n, tiles_m, -group, per_xcd, tn, tm)) {
+        if (!tile_of(blockIdx.x, tiles_m, tiles_n, group, per_xcd, tm, tn)) return;
+    } else if (!tile_of(blockIdx.x, tiles_n, tiles_m, -group, per_xcd, tn, tm)) {
         return;
     }
     const long long m0 = static_cast<long long>(tm) * BM;
@@ -278,7 +278,7 @@ __global__ __launch_bounds__(256) void project_kernel(const bf16_t *__restrict__
     __shared__ __attribute__((aligned(16))) bf16_t sB[2][TN * PITCH];
 
     int tm, tn;
-    if (!tile_of(tiles_m, tiles_n, group, (static_cast<long long>(tiles_m) * tiles_n + 7) / 8, tm, tn)) return;
+    if (!tile_of(blockIdx.x, tiles_m, tiles_n, group, (static_cast<long long>(tiles_m) * tiles_n + 7) / 8, tm, tn)) return;
     const long long m0 = static_cast<long long>(tm) * TM;
     const int n0 = tn * TN;
 

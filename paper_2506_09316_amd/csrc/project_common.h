@@ -17,10 +17,11 @@ __device__ __forceinline__ void wait_loads()   // at most N of this wavefront's 
 // 16: 1.98, 1.99, 2.09, 2.24 ms.  Each group reads all of W, so a last group of one or two row tiles after a single full
 // one is worth avoiding (group_rows()): M = 1060, K = 11008, N = 20480 in 4 + 1 and 5 row tiles 562 and 509 us.
 // False: no tile for this workgroup.
-__device__ __forceinline__ bool tile_of(int tiles_m, int tiles_n, int GM, long long per_xcd, int &tm, int &tn)
+__device__ __forceinline__ bool tile_of(uint32_t workgroup, int tiles_m, int tiles_n, int GM, long long per_xcd, int &tm, int &tn)
 {
     const long long ntiles = static_cast<long long>(tiles_m) * tiles_n;
-    const long long lin = static_cast<long long>(blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+    if (workgroup / 8 >= per_xcd) return false;
+    const long long lin = static_cast<long long>(workgroup % 8) * per_xcd + workgroup / 8;
     if (lin >= ntiles) return false;
     const long long per_group = static_cast<long long>(GM) * tiles_n;
     const int first_m = static_cast<int>(lin / per_group) * GM;

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
     __shared__ __attribute__((aligned(1024))) char st0[2 * OPB];
     __shared__ __attribute__((aligned(1024))) char st1[2 * OPB];
     int tm, tn;
-    if (!tile_of(tiles_m, tiles_n, group, per_xcd, tm, tn)) return;
+    if (!tile_of(workgroup_index(), tiles_m, tiles_n, group, per_xcd, tm, tn)) return;
     const long long m0 = 256LL * tm;
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
@@ -365,10 +365,10 @@ hipError_t launch_project_fp8(int64_t M, int K, int n_out, const int32_t *widths
     }
     const int tiles_m = static_cast<int>((M + 255) / 256), tiles_n = (blocks + 1) / 2;
     const long long per_xcd = (static_cast<long long>(tiles_m) * tiles_n + 7) / 8;
-    const dim3 grid(static_cast<unsigned>(8 * per_xcd));
+    const dim3 block(e8m0 ? 256 : 512), grid = grid_of(8 * per_xcd, block.x);
     const int group = tiles_m <= 5 ? tiles_m : 4;
-    if (e8m0) DSLA_LAUNCH(ps, project_fp8_tile_kernel<true>, grid, dim3(256), 0, stream, a, tiles_m, tiles_n, blocks, group, per_xcd);
-    else DSLA_LAUNCH(ps, project_fp8_tile_kernel<false>, grid, dim3(512), 0, stream, a, tiles_m, tiles_n, blocks, group, per_xcd);
+    if (e8m0) DSLA_LAUNCH(ps, project_fp8_tile_kernel<true>, grid, block, 0, stream, a, tiles_m, tiles_n, blocks, group, per_xcd);
+    else DSLA_LAUNCH(ps, project_fp8_tile_kernel<false>, grid, block, 0, stream, a, tiles_m, tiles_n, blocks, group, per_xcd);
     return hipGetLastError();
 }
 

@@ -124,7 +124,7 @@ __global__ __launch_bounds__(64 * NW) void project_fp8_rows_kernel(Fp8Args a, in
     constexpr int DEPTH = F::DEPTH, SB = E8M0 ? 1 : 4;
     __shared__ __attribute__((aligned(1024))) char ring[NW * F::MINE];
     int tm, tn;
-    if (!tile_of(tiles_m, tiles_n, tiles_m, per_xcd, tm, tn)) return;
+    if (!tile_of(workgroup_index(), tiles_m, tiles_n, tiles_m, per_xcd, tm, tn)) return;
     const int n0 = tn * 16 * NT, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     const long long m0 = 16LL * MT * tm;
@@ -290,7 +290,7 @@ void launch_few(ProfileScope &ps, const Fp8Args &a, int N, bool e8m0, hipStream_
     constexpr int NW = Few<MT, NT, 8>::DEPTH >= 1 && (!EXACT || MT + NT <= 8) ? 8 : 4;
     const int tiles_m = static_cast<int>((a.M + 16 * MT - 1) / (16 * MT)), tiles_n = (N + 16 * NT - 1) / (16 * NT);
     const long long per_xcd = fp8_rows_per_xcd(tiles_m, tiles_n);
-    const dim3 grid(static_cast<unsigned>(8 * per_xcd));
+    const dim3 grid = grid_of(8 * per_xcd, 64 * NW);
     if (e8m0) DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, NW, true, EXACT>), grid, dim3(64 * NW), 0, stream, a, N, tiles_m, tiles_n, per_xcd);
     else DSLA_LAUNCH(ps, (project_fp8_rows_kernel<MT, NT, NW, false, EXACT>), grid, dim3(64 * NW), 0, stream, a, N, tiles_m, tiles_n, per_xcd);
 }

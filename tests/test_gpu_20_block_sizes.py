@@ -5,7 +5,7 @@ import torch
 
 import paper_2506_09316_amd as dsla
 from oracle import block as orc
-from tests.block_common import HALF, NORM, U, assert_within, f64, stored, values
+from tests.block_common import HALF, NORM, TORCH, U, assert_within, f64, stored, values
 
 pytestmark = pytest.mark.gpu
 
@@ -75,3 +75,20 @@ def test_quantize_many_rows(rows, block_rows):
     assert all_but(q, some, 0x78)
     scales = s[:, :1].contiguous()
     assert all_but(scales, last, 119) and not any(bool(c.any()) for c in s[:, 1:].split(1 << 28))
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("extra", [-64, 71])
+def test_product_of_many_rows(extra, out):
+    """Rows of ones times a weight of ones, and a few others."""
+    M, K, N = 2 ** 29 + extra, 16, 16
+    some = [0, 65536 * 64, M // 2, M - 2, M - 1]
+    x = torch.full((M, K), 0x38, device="cuda", dtype=torch.uint8)   # 1.0
+    xs = torch.full((M, 4), 127, device="cuda", dtype=torch.uint8)
+    wq, ws = torch.full((N, K), 0x38, device="cuda", dtype=torch.uint8), torch.full((1, 4), 127, device="cuda", dtype=torch.uint8)
+    for i, r in enumerate(some):
+        x[r, i] = 0x40 + 8 * i   # 2, 4, 8 ..
+    y = torch.zeros(M, N, device="cuda", dtype=TORCH[out])
+    dsla.dsla_project_fp8(x.view(torch.float8_e4m3fn), xs.view(torch.float8_e8m0fnu), wq.view(torch.float8_e4m3fn), ws.view(torch.float8_e8m0fnu), [y])
+    assert f64(taken(y, some)).tolist() == [[15.0 + 2 ** (i + 1)] * N for i in range(len(some))]
+    assert all_but(y, some, 16.0)

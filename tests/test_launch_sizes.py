@@ -40,3 +40,27 @@ for cols in (16, 128, 4112, 1 << 21):
 
 def test_norms_and_quantization(tmp_path):
     run_checked(tmp_path, NORMS)
+
+
+PRODUCTS = r"""
+for M, K, widths in ((1 << 33, 16, [16]), ((1 << 29) - 64, 16, [16]), ((1 << 29) + 64, 16, [16]), (1 << 30, 128, [16] * 8), (1 << 30, 16, [16]), (1 << 25, 128, [4096]),
+                     (3 << 28, 400, [16, 16]), (1 << 33, 128, [128])):
+    for scale in (0, 1):
+        for out in (0, 1):
+            kernel = launched(project(M, K, widths, scale, out))
+            got = stub.launch_stub_workgroups()
+            pair = re.search(r"project_fp8_rows_kernelILi(\d)ELi(\d)E", kernel)
+            if pair:
+                mt, nt = (int(n) for n in pair.groups())
+                tiles = -(-M // (16 * mt)) * -(-sum(widths) // (16 * nt))
+            else:
+                assert "project_fp8_tile_kernel" in kernel
+                tiles = -(-M // 256) * -(-sum(-(-w // 128) for w in widths) // 2)
+            assert tiles <= got <= tiles + 8 * 31 + 7 + (0 if got == stub.launch_stub_row() else 65535), (M, K, widths, scale, out, kernel, tiles, got)
+too_many = (0x7ffffff0 // 2 + 1) * 64   # rows, for one block of columns
+assert project(too_many, 16, [16]) == ERR_SHAPE and project(too_many // 2, 16, [16] * 2) == ERR_SHAPE
+"""
+
+
+def test_products(tmp_path):
+    run_checked(tmp_path, PRODUCTS)
