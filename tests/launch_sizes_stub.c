@@ -22,6 +22,8 @@ void __hipRegisterFunction(void **modules, const void *kernel, char *stub_name, 
     }
 }
 const char *launch_stub_kernel(void) { return last_name; }
+int launch_stub_known(void) { return known; }
+const char *launch_stub_kernel_of(int i) { return kernels[i].name; }
 uint64_t launch_stub_workgroups(void) { return (uint64_t)grid.x * grid.y * grid.z; }
 uint32_t launch_stub_row(void) { return grid.x; }
 
