@@ -64,3 +64,17 @@ assert project(too_many, 16, [16]) == ERR_SHAPE and project(too_many // 2, 16, [
 
 def test_products(tmp_path):
     run_checked(tmp_path, PRODUCTS)
+
+
+SEVERAL = r"""
+for rows, H, d in ((21850, 5, 64), (21850, 3, 128), (65537, 1, 64), (16389, 4, 128)):
+    assert f"rows_kernelILi{d}ELi2E" in launched(head_norm(rows, H, d))
+    assert f"rows_kernelILi{d}ELi1E" in launched(head_norm(rows // 8, H, d))
+for rows, cols in ((32773, 400), (131075, 64)):
+    assert "rows_kernelILi0ELi4E" in launched(quantize(rows, cols, 1)) and "rows_kernelILi0ELi1E" in launched(quantize(rows // 8, cols, 1))
+"""
+
+
+def test_several_blocks_to_16_lanes(tmp_path):
+    """What the tests of many blocks are about: sizes that take several at a time."""
+    run_checked(tmp_path, SEVERAL)
