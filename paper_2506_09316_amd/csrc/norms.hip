@@ -93,14 +93,15 @@ __device__ __forceinline__ float sum_all(float x, float *s)
     return t;
 }
 
-// act(z) by e^-|z|, so that a large gate does not overflow, as a power of two.  exact (results in fp32): to 6 ulps, the exponent carries the rounding of
+// act(z) as a power of two.  exact (results in fp32), by e^-|z|, so that a large gate does not overflow: to 6 ulps, the exponent carries the rounding of
 // |z| log2 e along, its whole part goes around the instruction, which has no results below 2^-126, and the inverse takes a step of Newton's.
-// Else: to 2^-18, by 16 issue slots instead of 26; the kernels issue vector instructions all the time.  24 is added to the exponent on the way, for the
-// numbers below 2^-126, and comes off again in the last factors.
+// Else by 2^-32 e^-z, which overflows where the gate is below all numbers (the instructions take and give none below 2^-126): to 2^-18, by 15 issue slots
+// instead of 26; the kernels issue vector instructions all the time.  The exponent is rounded once, below 128 by 2^-18, 44 U of the power; what the fp32 log2 e
+// lacks, up to 20 U at z = -87, a factor puts back (for z > 0 it would be of no weight, and is 1).
 __device__ __forceinline__ float activated(float z, int act, bool exact)
 {
     if (act == DSLA_ACT_NONE) return z;
-    constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f;
+    constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f, kLn2 = 0.693147182f;
     if (exact) {
         const float a = fabsf(z) > 200.f ? -200.f : -fabsf(z);   // (e^-200 is 0; NaN stays)
         const float p = a * kLog2e, n = rintf(p), rest = fmaf(a, kLog2eRest, fmaf(a, kLog2e, -p));
@@ -109,9 +110,9 @@ __device__ __forceinline__ float activated(float z, int act, bool exact)
         const float top = z < 0.f ? t : 1.f;
         return (act == DSLA_ACT_SIGMOID ? top : z * top) * inverse;
     }
-    const float t = __builtin_amdgcn_exp2f(fmaf(-fabsf(z), kLog2e, 24.f));   // 2^24 e^-|z|
-    const float inverse = 0x1p-24f * __builtin_amdgcn_rcpf(fmaf(t, 0x1p-24f, 1.f)), top = (z < 0.f ? t : 0x1p24f) * inverse;
-    return act == DSLA_ACT_SIGMOID ? top : z * top;
+    const float t = __builtin_amdgcn_exp2f(fmaf(-z, kLog2e, -32.f)), back = __builtin_amdgcn_fmed3f(fmaf(z, kLog2eRest * kLn2, 1.f), 0.f, 1.f);
+    const float sigmoid = 0x1p-32f * __builtin_amdgcn_rcpf(t + 0x1p-32f) * back;
+    return act == DSLA_ACT_SIGMOID ? sigmoid : z * sigmoid;
 }
 
 // 1 / sqrt(v) to an ulp: the instruction and a step of Newton's; far from 1 (no square of a number, or an infinite one) the library's.
