@@ -385,7 +385,7 @@ typedef enum { DSLA_ACT_NONE = 0, DSLA_ACT_SIGMOID = 1, DSLA_ACT_SILU = 2 } dsla
  *   gate     : [rows][D] of y_dtype, or NULL: no factor
  *   h        : [rows][D] of h_dtype, or NULL: only x' is wanted (one of x_out and h is required; pre_weight is then not used)
  *   h_scale  : scales of h where h_dtype is DSLA_E4M3, else NULL
- * An output may be the buffer of an input whose elements are as large; otherwise nothing overlaps.
+ * x_out and h may each be the buffer of x, y or gate where its elements are as large; otherwise nothing overlaps.
  */
 typedef struct {
     int32_t D;                 /* width, a multiple of 16 up to 32768                                 */

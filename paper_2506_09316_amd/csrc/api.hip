@@ -475,10 +475,13 @@ dsla_status dsla_residual_norm(const dsla_norm *n, int64_t rows, const void *x, 
                           static_cast<const void *>(n->pre_weight)})
         if (!aligned16(p)) return DSLA_ERR_SHAPE;
     const size_t bx = type_bytes(n->x_dtype), by = type_bytes(n->y_dtype), bh = type_bytes(n->h_dtype);
+    const void *post = n->post_weight, *pre = n->pre_weight;   // (read after the first results are written)
     if (h && h == x_out) return DSLA_ERR_SHAPE;
+    for (const void *w : {post, pre})
+        if (w && (w == x_out || w == h || w == h_scale)) return DSLA_ERR_SHAPE;
     if (h_scale && (h_scale == h || h_scale == x_out || h_scale == x || h_scale == y || h_scale == gate)) return DSLA_ERR_SHAPE;
-    for (const void *in : {x, y, gate})
-        if (!in_place_ok(x_out, bx, in, in == x ? bx : by) || !in_place_ok(h, bh, in, in == x ? bx : by)) return DSLA_ERR_SHAPE;
+    if (!in_place_ok(x_out, bx, x, bx) || !in_place_ok(x_out, bx, y, by) || !in_place_ok(x_out, bx, gate, by)) return DSLA_ERR_SHAPE;
+    if (!in_place_ok(h, bh, x, bx) || !in_place_ok(h, bh, y, by) || !in_place_ok(h, bh, gate, by)) return DSLA_ERR_SHAPE;
     return hip_status(launch_residual_norm(*n, rows, x, y, gate, x_out, h, h_scale, static_cast<hipStream_t>(stream)));
 }
 
@@ -494,6 +497,7 @@ dsla_status dsla_head_norm(const dsla_heads *n, int64_t rows, const void *o, con
     if (n->weight && !good_eps(n->eps)) return DSLA_ERR_SHAPE;
     if (!aligned16(o) || !aligned16(gate) || !aligned16(out) || !aligned16(n->weight)) return DSLA_ERR_SHAPE;
     if (out_scale && (out_scale == o || out_scale == gate || out_scale == out)) return DSLA_ERR_SHAPE;
+    if (n->weight && (n->weight == out || n->weight == out_scale)) return DSLA_ERR_SHAPE;
     const size_t bo = type_bytes(n->out_dtype), bi = type_bytes(n->io_dtype);
     if (!in_place_ok(out, bo, o, bi) || !in_place_ok(out, bo, gate, bi)) return DSLA_ERR_SHAPE;
     return hip_status(launch_head_norm(*n, rows, o, gate, out, out_scale, static_cast<hipStream_t>(stream)));
