@@ -20,7 +20,6 @@ __device__ __forceinline__ void wait_loads()   // at most N of this wavefront's 
 __device__ __forceinline__ bool tile_of(uint32_t workgroup, int tiles_m, int tiles_n, int GM, long long per_xcd, int &tm, int &tn)
 {
     const long long ntiles = static_cast<long long>(tiles_m) * tiles_n;
-    if (workgroup / 8 >= per_xcd) return false;
     const long long lin = static_cast<long long>(workgroup % 8) * per_xcd + workgroup / 8;
     if (lin >= ntiles) return false;
     const long long per_group = static_cast<long long>(GM) * tiles_n;

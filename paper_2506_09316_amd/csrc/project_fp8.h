@@ -57,6 +57,13 @@ __device__ __forceinline__ i32x8 join(u32x4 a, u32x4 b)
                  static_cast<int>(b[0]), static_cast<int>(b[1]), static_cast<int>(b[2]), static_cast<int>(b[3])};
 }
 
+// tile_of() of a launch that may be filled up (grid_of()).
+__device__ __forceinline__ bool tile_here(int tiles_m, int tiles_n, int GM, long long per_xcd, int &tm, int &tn)
+{
+    const uint32_t workgroup = workgroup_index();
+    return workgroup / 8 < per_xcd && tile_of(workgroup, tiles_m, tiles_n, GM, per_xcd, tm, tn);
+}
+
 }  // namespace
 
 // Tiles of an XCD: whole columns, whose rows of W then come from memory once, where that takes no further round over its 32 compute units (a

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(E8M0 ? 256 : 512) void project_fp8_tile_kernel(Fp8A
     __shared__ __attribute__((aligned(1024))) char st0[2 * OPB];
     __shared__ __attribute__((aligned(1024))) char st1[2 * OPB];
     int tm, tn;
-    if (!tile_of(workgroup_index(), tiles_m, tiles_n, group, per_xcd, tm, tn)) return;
+    if (!tile_here(tiles_m, tiles_n, group, per_xcd, tm, tn)) return;
     const long long m0 = 256LL * tm;
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;

@@ -124,7 +124,7 @@ __global__ __launch_bounds__(64 * NW) void project_fp8_rows_kernel(Fp8Args a, in
     constexpr int DEPTH = F::DEPTH, SB = E8M0 ? 1 : 4;
     __shared__ __attribute__((aligned(1024))) char ring[NW * F::MINE];
     int tm, tn;
-    if (!tile_of(workgroup_index(), tiles_m, tiles_n, tiles_m, per_xcd, tm, tn)) return;
+    if (!tile_here(tiles_m, tiles_n, tiles_m, per_xcd, tm, tn)) return;
     const int n0 = tn * 16 * NT, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     const long long m0 = 16LL * MT * tm;
