@@ -377,7 +377,8 @@ typedef enum { DSLA_ACT_NONE = 0, DSLA_ACT_SIGMOID = 1, DSLA_ACT_SILU = 2 } dsla
 
 /*
  * dsla_residual_norm - the border between two blocks in one pass.  Arithmetic is fp32; both results are rounded once, and h is
- * computed from x' before its rounding.  Norms are of features up to 10^17.  Gates are to 2^-18 where no result is in fp32, else to 2^-21
+ * computed from x' before its rounding.  Norms are of features up to 10^17, eps from 10^-30 on (below it shows
+ * what squares of small features lose in fp32).  Gates are to 2^-18 where no result is in fp32, else to 2^-21
  * (where 1 / (1 + e^-z) is below 2^-126: of 2^-126).
  *   rows     : tokens, >= 1; rows * ceil(D / 128) below 2^31 (else DSLA_ERR_SHAPE)
  *   x, x_out : [rows][D] of x_dtype; x_out NULL: x' is not kept

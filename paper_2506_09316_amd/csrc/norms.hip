@@ -2,9 +2,9 @@
 // read-out's heads, and values to e4m3 with block scales.  All of them are bound by memory: every value is read once, kept in
 // registers and written once, 8 values of a lane at a time; sums and largest magnitudes go through the lanes.  A block of 128
 // columns is 16 lanes of 8, one row of the cross-lane operations.  A copy with the same non-temporal hints reaches 6.1 to 6.3 TB/s:
-//   border, 16384 rows of 4096, bf16, both norms, gate, e4m3 out   110 us  5.5 TB/s (vector instructions issued 90 % of the time; two sums across
-//                                                                   the workgroup one after the other); without norm of y, gate and 8 bits 6.1
-//   heads, 16384 rows of 32 of 128, bf16, gate, e4m3 out            61.6 us  5.5 TB/s
+//   border, 16384 rows of 4096, bf16, both norms, gate, e4m3 out   112 to 114 us  5.3 to 5.4 TB/s (vector instructions issued 86 % of the time; two sums
+//                                                                   across the workgroup one after the other); without norm of y, gate and 8 bits 6.0
+//   heads, 16384 rows of 32 of 128, bf16, gate, e4m3 out            58.6 to 60.8 us  5.6 to 5.8 TB/s
 //   quantize, 20480 x 4096 bf16, blocks of 128 x 128                48.8 us  5.2 TB/s (256 bytes of a row at a time)
 #include "fp8_common.h"
 
@@ -386,9 +386,11 @@ hipError_t launch_residual_norm(const dsla_norm &n, int64_t rows, const void *x,
                  (x_out && n.x_dtype == DSLA_F32) || (h && n.h_dtype == DSLA_F32)};
     const bool x32 = n.x_dtype == DSLA_F32, y32 = n.y_dtype == DSLA_F32;
     ProfileScope ps(DSLA_KERNEL_RESIDUAL_NORM, stream);
-    // 8 values a lane from 1024 columns on: more rows' loads are in flight at once than with more of them (without norm of y, gate and 8 bits, 8192 rows
-    // of 4096: 256 lanes of 16 values 45.4 us, 512 of 8 44.0, 128 of 32 slower than both; 4096 of 8192: 256 of 32 48.4, 1024 of 8 46.1; 256 of 4096: 4.08, 3.85.
-    // With everything of it, 16384 of 4096: 109.7, 110.5).
+    // 8 values a lane above 1024 and up to 8192 columns: more rows' loads are in flight at once than with more of them.  Up to 4096 columns 256 lanes of 16
+    // values / 512 of 8, above 256 of 32 / 1024 of 8 (us), without norm of y, gate and 8 bits: 8192 rows of 4096 46.0 / 44.6 (128 of 32 slower than both),
+    // 256 of 4096 4.08 / 3.85, 16384 of 2560 57.4 / 55.8, 16384 of 2064 51.0 / 51.5, 8192 of 5120 62.0 / 60.4, 4096 of 7168 43.8 / 41.5, 4096 of 8192
+    // 48.9 / 46.2.  With all of it the lanes that have no values and the larger barrier weigh more: 16384 of 4096 110.2 / 112.4, of 2560 81.8 / 85.8, of
+    // 2064 77.5 / 83.8, but 8192 of 5120 96.6 / 83.1, of 8192 134.8 / 114.5.
     if (n.D <= 128) launch_border<16, 1>(ps, a, x32, y32, stream);
     else if (n.D <= 512) launch_border<64, 1>(ps, a, x32, y32, stream);
     else if (n.D <= 1024) launch_border<64, 2>(ps, a, x32, y32, stream);

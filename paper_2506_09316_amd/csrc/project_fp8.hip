@@ -29,10 +29,10 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const uint8_t *p, si
 // E8M0: four wavefronts, one to a SIMD, with 128 x 128 results in 256 accumulation registers: 64 MFMAs a step for 32 LDS reads of 16 bytes.  fp32
 // scales: the sums take vector instructions, which have no access to those registers: eight wavefronts with 128 x 64 results each.
 // 16 x 16 x 128 products: registers only, random operands, they sustain 4.45 PFLOP/s, 32 x 32 x 64 4.1.
-// M = 16384, K = 4096, N = 20480, E8M0: 0.99 ms (2790 TFLOP/s; a library product of that shape without block scales 0.96).  Bound by power: the chip
-// runs it at 1.74 GHz with the matrix pipes 66 % busy.  On the way: loads of a step in one go behind a barrier 1.24 ms (they keep the address unit busy for
+// M = 16384, K = 4096, N = 20480, E8M0: 0.99 to 1.05 ms from box to box (2620 to 2790 TFLOP/s; a library product of that shape without block scales 0.96);
+// with fp32 scales 1.22.  Bound by power: the chip runs it at 1.72 GHz with the matrix pipes 67 % busy.  On the way: loads of a step in one go behind a barrier 1.24 ms (they keep the address unit busy for
 // longer than the products they stand among, and the wavefront with them), spread over two thirds of the step 1.14, results 16 rows at a time through LDS
-// without checks in whole tiles 1.07, scales through LDS by 16 bytes of a row instead of one at a time from memory 1.01 (with fp32 scales 1.93 -> 1.43 ms:
+// without checks in whole tiles 1.07, scales through LDS by 16 bytes of a row instead of one at a time from memory 1.01 (with fp32 scales 1.93 -> 1.23 ms:
 // an instruction that asks for one scale of 16 rows costs as much as two that fill 8 rows), read in front of the loads 1.23.  One barrier a step instead of
 // two, which gives a load 1.4 steps instead of one to arrive, is the same: latency is not what bounds it.  K = 128: 10 us a tile, of which 6 are the start.
 // The product of two fragments added to what stands in the accumulation registers, with scales from byte B of two registers.  (The
@@ -301,8 +301,9 @@ struct Choice {
     int mt, nt;   // 0: the 256 x 256 tiles
     double us;
 };
-// The fewest microseconds by an estimate, fitted to 9600 random products of up to 8192 rows and every pair (rms 15 %; with the XCDs evenly
-// filled less): a round of workgroups over the compute units costs its start, its sums (mt nt), and for every 1024 of K its loads (mt + nt) and
+// The fewest microseconds by an estimate, fitted to 9600 timings of random products of up to 8192 rows and pairs.  Of 13579 others, of the kernels as they are,
+// it is 9 to 13 % off (rms) for the pairs and 30 % too long for the 256 x 256 tiles; what it chooses takes 1.01 of the best's time (geometric mean of 1569
+// products, the worst 1.35).  A round of workgroups over the compute units costs its start, its sums (mt nt), and for every 1024 of K its loads (mt + nt) and
 // products (mt nt); beside that the memory.
 struct Cost {
     double call, round, sums, loads, products, next;

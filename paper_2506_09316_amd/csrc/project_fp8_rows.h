@@ -72,9 +72,9 @@ struct Factor {
 // end: no barrier stands between a wavefront's loads, and every byte is written to LDS and read from there once.  Its steps of 128 go through a ring of its
 // own in LDS, filled by buffer loads that write LDS directly, an instruction 8 rows of 128 bytes.  What counts is the lines that are asked for, and a
 // scale alone would be one: they come as 16 bytes of every row, 12 steps of E8M0 (from a multiple of four down) or four of fp32 at a time (300 rows,
-// K = 11008, N = 4096: 25.2 us with a scale of every row in every step, 22.1 so).
-// One row, K = 4096, N = 20480: 15.0 us, 5.6 TB/s of weights.  64 rows 18.9 us.  300 rows, K = 11008, N = 4096: 24 us, 1.1 PFLOP/s; 1024 rows,
-// K = 4096, N = 4096: 23 us, 1.5 PFLOP/s.  Few rows are bound by the memory; tiles of nine and more blocks by what LDS holds of loads on their way, a step of each
+// K = 11008, N = 4096: 3 us more with a scale of every row in every step).
+// One row, K = 4096, N = 20480: 15.0 us, 5.6 TB/s of weights.  64 rows 18.7 us (five outputs of 4096: 19.5 to 20.0).  300 rows, K = 11008, N = 4096: 24.2 us, 1.1 PFLOP/s; 1024 rows,
+// K = 4096, N = 4096: 25.5 us, 1.35 PFLOP/s.  Few rows are bound by the memory; tiles of nine and more blocks by what LDS holds of loads on their way, a step of each
 // wavefront, for as long as a line takes from memory (a step takes 2 us, its products 0.3).  Tried: four wavefronts with two steps each on their way
 // (the same within 2 %; fp32 scales 33 instead of 27 us), lines asked for ahead into the L2 (25 -> 36 us: each costs as much as the load itself),
 // the workgroups that share rows in different places of their stretches (24 -> 43 us: together each line comes once).
