@@ -78,3 +78,12 @@ for rows, cols in ((32773, 400), (131075, 64)):
 def test_several_blocks_to_16_lanes(tmp_path):
     """What the tests of many blocks are about: sizes that take several at a time."""
     run_checked(tmp_path, SEVERAL)
+
+
+def test_the_launch_tests_have_their_helper():
+    """test_block_launches takes each_launch() out of another test's source: all of it, and nothing else."""
+    import ast
+    from tests.test_block_launches import EACH
+    (helper,) = ast.parse(EACH).body
+    assert helper.name == "each_launch" and isinstance(helper.body[-1], ast.For) and len(helper.body) == 3
+    assert EACH.count("assert") == 3 and "launch_stub_reset(n)" in EACH and "n + 1" in EACH
